@@ -53,7 +53,7 @@ extern "C" {
 
 #define MVK_PRIME 2147483647u
 #define MVK_PRIME_BABYBEAR 2013265921u
-#define MVK_ABI_VERSION 9
+#define MVK_ABI_VERSION 10
 
 typedef int32_t mvk_status;
 #define MVK_OK 0
@@ -668,6 +668,152 @@ void mvk_st_free(mvk_st *st);
 mvk_status mvk_decode_verify_seeded(const mvk_key *key, const mvk_st *st, const uint32_t *Xhat,
                                     const uint32_t *Yhat, uint32_t t_y, uint32_t ell, uint64_t chal_seed,
                                     uint32_t *Y, uint32_t *vL, uint32_t *vR, uint32_t *accept, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * The client's attention: what runs on decrypted queries, keys and values
+ * between the delegated projections (Sec. 7.2: nonlinear operations stay with
+ * the client), around one paged cache of keys and values.
+ *
+ * Values are floats (types below) or, where a call says so, field elements of
+ * fixed-point numbers: the centred residue (p - x stands for -x) times a scale.
+ * Unlike the rest of this library these calls round; sums, softmax statistics
+ * and angles are held in 32 bits or more, every output is rounded once.
+ */
+#define MVK_TYPE_BF16 0
+#define MVK_TYPE_F16 1
+#define MVK_TYPE_F32 2
+#define MVK_TYPE_FIELD 3 /* uint32 field elements */
+
+/* Rows of heads: element d of head h of token t lies at data[t*token + h*head + d]
+ * (strides in elements, at least dim apart or equal where memory is shared). */
+typedef struct mvk_rows {
+    void *data;      /* device */
+    int32_t type;    /* MVK_TYPE_* */
+    uint64_t token;
+    uint64_t head;
+} mvk_rows;
+
+/* A paged cache of one layer: pools of `pages` pages of page_size entries (a
+ * power of two) for kv_heads heads of dim values; entry e of head h of page i
+ * lies at K[i*k_page + h*k_head + e*k_entry] (V likewise; strides in elements). */
+typedef struct mvk_kv {
+    void *K, *V; /* device */
+    int32_t type; /* MVK_TYPE_BF16, _F16 or _F32 */
+    uint32_t pages, kv_heads, page_size, dim;
+    uint64_t k_page, k_head, k_entry;
+    uint64_t v_page, v_head, v_entry;
+} mvk_kv;
+
+/* `count` sequences.  Entry j of sequence s lies in page table[s*table_stride +
+ * j / page_size] at j % page_size; lens[s] entries are in use, the new tokens'
+ * among them.  The new tokens of sequence s are rows q_start[s] .. q_start[s+1]-1
+ * of the call's token rows, the last entries of the sequence in that order
+ * (q_start: count + 1 words; NULL where a call has no token rows).  max_new: no
+ * sequence has more new tokens than this.  All arrays are device int32 and are
+ * read when the work runs.  Lengths are clamped to the table's width, page
+ * numbers outside the pool are read as the nearest page and never written. */
+typedef struct mvk_seqs {
+    const int32_t *table;
+    uint64_t table_stride;
+    uint32_t count;
+    uint32_t width;  /* pages a row of the table holds */
+    const int32_t *lens;
+    const int32_t *q_start;
+    uint32_t max_new;
+} mvk_seqs;
+
+#define MVK_ROTARY_HALF 0        /* pair i: elements i and i + rot/2 of the head */
+#define MVK_ROTARY_INTERLEAVED 1 /* pair i: elements 2i and 2i + 1 */
+
+#define MVK_SCALE_NONE 0
+#define MVK_SCALE_LINEAR 1 /* every frequency divided by factor (position interpolation) */
+#define MVK_SCALE_BASE 2   /* base * factor^(rot / (rot - 2)) (NTK-aware) */
+#define MVK_SCALE_PARTS 3  /* by wavelength: f/factor below slow turns within original_len, f above fast,
+                              linear between; cosines and sines times 0.1 ln(factor) + 1
+                              (NTK-by-parts, Peng et al. 2023) */
+
+/* Largest dim of a head for the calls below, and largest rot. */
+#define MVK_MAX_HEAD_DIM 512u
+
+/*
+ * The table of rotary positions: row t (of `rows`) holds rot/2 cosines, then
+ * rot/2 sines of the angles t * f_i, f_i = base^(-2i/rot) changed as `scaling`
+ * says; angles in 64 bits.  table: device, rows x rot floats.
+ * factor, original_len, slow, fast: of the scaling (ignored where it has none).
+ * Errors: MVK_EINVAL (null, rot odd or zero, base <= 0, factor < 1, slow >= fast),
+ * MVK_ERANGE (rot > MVK_MAX_HEAD_DIM, rows above 2^31 - 1).
+ */
+mvk_status mvk_rotary_table(uint32_t rot, uint32_t rows, double base, int32_t scaling, double factor,
+                            double original_len, double slow, double fast, float *table, void *stream);
+
+/*
+ * Rotary positions on T new tokens, and the append of their keys and values.
+ * The first rot elements of every head of q and k are rotated pair by pair,
+ * (a, b) -> (a cos - b sin, b cos + a sin) with the row positions[t] of the
+ * table (clamped to its rows), the others pass; v passes.  q goes to q_out, k
+ * and v to their entries of the cache (a new token without one, or whose page
+ * is outside the pool, is not written).
+ *   q, q_out       : T x heads x dim; both NULL: keys and values only.  q_out
+ *                    may be q itself (same type and strides) and else shares
+ *                    no memory with an input.
+ *   k, v           : T x cache->kv_heads x cache->dim, types as q's or others;
+ *                    NULL (with cache and seqs): queries only.
+ *   field_scale    : value of 1 in field inputs.
+ * Types: inputs any, q_out BF16, F16 or F32, equal to the cache's where both are given.
+ * Errors: MVK_EINVAL, MVK_ERANGE (dim > MVK_MAX_HEAD_DIM, buffers above 2^62 bytes).
+ */
+mvk_status mvk_rotary_append(const mvk_rows *q, const mvk_rows *k, const mvk_rows *v, uint32_t T, uint32_t heads,
+                             uint32_t dim, uint32_t rot, int32_t layout, const int32_t *positions,
+                             const float *table, uint32_t table_rows, float field_scale, const mvk_rows *q_out,
+                             const mvk_kv *cache, const mvk_seqs *seqs, void *stream);
+
+/*
+ * Attention of the new tokens over their sequences' entries: new token i (of c)
+ * of a sequence of n entries sees the entries j <= n - c + i; query head h reads
+ * kv head h / (heads / kv_heads).
+ *   o = sum_j p_j v_j,  p = softmax_j(scale q . k_j)
+ * A row that sees no entry (a sequence shorter than its new tokens) is zero.
+ * Places that a row does not see, and unused places of a page, do not reach it
+ * whatever they hold; a not-a-number in a place that it sees does.
+ *   q          : T x heads x dim, the cache's type
+ *   out        : T x heads x dim: BF16, F16, F32, or FIELD: o / field_scale
+ *                rounded to the nearest integer and embedded in F_p (a
+ *                magnitude above (p-1)/2 is clamped to it).  Rows that belong
+ *                to no sequence are left alone.
+ *   lse        : NULL, or T x heads floats: ln sum_j exp(scale q . k_j), -inf for a row without entries
+ *   w_out      : NULL, or the entries' collected weights, count x kv_heads x (a row
+ *                of at least width * page_size): entry j of the sequence gets
+ *                (j < n - c ? w_in : 0) + the sum of p_j over the sequence's new
+ *                tokens and the kv head's query heads; places j >= n are left alone.
+ *                w_in: same strides, NULL for zeros, may be w_out.
+ * Sums have a fixed order: the same inputs give the same bits.
+ * Errors: MVK_EINVAL, MVK_ERANGE (dim > MVK_MAX_HEAD_DIM, buffers above 2^62
+ * bytes, T * heads above 2^31 - 1), MVK_ENOMEM, MVK_ECAPTURE (workspace).
+ */
+mvk_status mvk_paged_attention(const mvk_rows *q, uint32_t T, uint32_t heads, const mvk_kv *cache,
+                               const mvk_seqs *seqs, float scale, const mvk_rows *out, float field_scale, float *lse,
+                               const float *w_in, float *w_out, uint64_t w_seq, uint64_t w_head, void *stream);
+
+/*
+ * Eviction by collected weight: of the n entries of each sequence and kv head,
+ * m = min(n, budget) are kept: the first `sinks`, the last `recent`, and of the
+ * others the heaviest (ties: the lowest index; not-a-number is lighter than any
+ * number).  They are copied in order to entries 0 .. m-1 of pages of `dst`
+ * (dst_table: count x dst_width), which share no memory with the pages read:
+ * pages of a common prefix may belong to several sequences, so none is altered.
+ *   w          : count x kv_heads x (a row of at least width * page_size) floats, strides w_seq, w_head
+ *   w_out      : NULL, or the kept entries' weights (rows of at least budget, strides o_seq, o_head)
+ *   kept       : count x kv_heads x budget int32, the kept entries' indices, -1 beyond m
+ *   lens_out   : count int32, m of each sequence
+ * dst has src's type, kv_heads, dim and any page size; dst_width * page_size of
+ * dst is at least min(budget, width * page_size of src).  seqs->q_start is not used.
+ * Errors: MVK_EINVAL (sinks + recent > budget, budget 0, mismatched caches),
+ * MVK_ERANGE (dim > MVK_MAX_HEAD_DIM, count or kv_heads > 65535, buffers above 2^62 bytes).
+ */
+mvk_status mvk_cache_evict(const mvk_kv *src, const mvk_seqs *seqs, const float *w, uint64_t w_seq, uint64_t w_head,
+                           uint32_t budget, uint32_t recent, uint32_t sinks, const mvk_kv *dst,
+                           const int32_t *dst_table, uint64_t dst_table_stride, uint32_t dst_width, float *w_out,
+                           uint64_t o_seq, uint64_t o_head, int32_t *kept, int32_t *lens_out, void *stream);
 
 #ifdef __cplusplus
 }

@@ -799,3 +799,11 @@ def sample_sparse(count: int, N: int, t: int, seed: int, tag: int, p: int = P):
     _lib.check("mvk_sample_sparse", _lib.load(p).mvk_sample_sparse(count, N, t, seed & 0xFFFFFFFFFFFFFFFF, tag,
                                                                    ptr(idx), ptr(val)))
     return idx, val
+
+
+# The client's attention (attention.py takes the helpers above, so it comes last)
+from .attention import (FIELD, KVCache, Sequences, cache_evict, paged_attention, rotary, rotary_append,  # noqa: E402
+                        rotary_table)
+
+__all__ += ["FIELD", "KVCache", "Sequences", "rotary_table", "rotary", "rotary_append", "paged_attention",
+            "cache_evict"]

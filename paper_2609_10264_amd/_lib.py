@@ -32,7 +32,7 @@ MVK_SEEDED_MAX_T = 4096
 MVK_STATIC_SCRATCH_BYTES = 32 << 20
 MVK_MAX_GROUP = 4
 MVK_MAX_PREP = 8
-ABI_VERSION = 9
+ABI_VERSION = 10
 # field modulus -> library built over that field
 LIB_PATHS = {MVK_PRIME: LIB_PATH, MVK_PRIME_BABYBEAR: LIB_PATH_BB}
 
@@ -81,6 +81,10 @@ EXPORTS = (
     "mvk_stream_create_cu_range",
     "mvk_stream_destroy",
     "mvk_decode_verify_encode_masked",
+    "mvk_rotary_table",
+    "mvk_rotary_append",
+    "mvk_paged_attention",
+    "mvk_cache_evict",
 )
 
 
@@ -112,6 +116,58 @@ class MvkSparse(ctypes.Structure):
         ("val", ctypes.c_void_p),
         ("t", ctypes.c_uint32),
         ("count", ctypes.c_uint32),
+    ]
+
+
+MVK_TYPE_BF16 = 0
+MVK_TYPE_F16 = 1
+MVK_TYPE_F32 = 2
+MVK_TYPE_FIELD = 3
+MVK_ROTARY_HALF = 0
+MVK_ROTARY_INTERLEAVED = 1
+MVK_SCALE_NONE = 0
+MVK_SCALE_LINEAR = 1
+MVK_SCALE_BASE = 2
+MVK_SCALE_PARTS = 3
+MVK_MAX_HEAD_DIM = 512
+
+
+class MvkRows(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("type", ctypes.c_int32),
+        ("token", ctypes.c_uint64),
+        ("head", ctypes.c_uint64),
+    ]
+
+
+class MvkKv(ctypes.Structure):
+    _fields_ = [
+        ("K", ctypes.c_void_p),
+        ("V", ctypes.c_void_p),
+        ("type", ctypes.c_int32),
+        ("pages", ctypes.c_uint32),
+        ("kv_heads", ctypes.c_uint32),
+        ("page_size", ctypes.c_uint32),
+        ("dim", ctypes.c_uint32),
+        ("k_page", ctypes.c_uint64),
+        ("k_head", ctypes.c_uint64),
+        ("k_entry", ctypes.c_uint64),
+        ("v_page", ctypes.c_uint64),
+        ("v_head", ctypes.c_uint64),
+        ("v_entry", ctypes.c_uint64),
+    ]
+
+
+class MvkSeqs(ctypes.Structure):
+    _fields_ = [
+        ("table", ctypes.c_void_p),
+        ("table_stride", ctypes.c_uint64),
+        ("count", ctypes.c_uint32),
+        ("width", ctypes.c_uint32),
+        ("lens", ctypes.c_void_p),
+        ("q_start", ctypes.c_void_p),
+        ("max_new", ctypes.c_uint32),
     ]
 
 
@@ -237,6 +293,17 @@ def load(p: int = MVK_PRIME) -> ctypes.CDLL:
     L.mvk_decode_verify_encode_masked.argtypes = [ctypes.POINTER(MvkKey), vp, vp, u32, vp, u32, vp, vp, vp, vp, vp,
                                                   vp, vp, u32, vp, vp, vp, u32, u32, vp, vp]
     L.mvk_decode_verify_encode_masked.restype = st
+    f64, f32, u64 = ctypes.c_double, ctypes.c_float, ctypes.c_uint64
+    i32 = ctypes.c_int32
+    rows, kv, seqs = ctypes.POINTER(MvkRows), ctypes.POINTER(MvkKv), ctypes.POINTER(MvkSeqs)
+    L.mvk_rotary_table.argtypes = [u32, u32, f64, i32, f64, f64, f64, f64, vp, vp]
+    L.mvk_rotary_table.restype = st
+    L.mvk_rotary_append.argtypes = [rows, rows, rows, u32, u32, u32, u32, i32, vp, vp, u32, f32, rows, kv, seqs, vp]
+    L.mvk_rotary_append.restype = st
+    L.mvk_paged_attention.argtypes = [rows, u32, u32, kv, seqs, f32, rows, f32, vp, vp, vp, u64, u64, vp]
+    L.mvk_paged_attention.restype = st
+    L.mvk_cache_evict.argtypes = [kv, seqs, vp, u64, u64, u32, u32, u32, kv, vp, u64, u32, vp, u64, u64, vp, vp, vp]
+    L.mvk_cache_evict.restype = st
     if L.mvk_abi_version() != ABI_VERSION:
         raise ImportError(f"{path}: ABI version mismatch; rebuild the library")
     if L.mvk_field_modulus() != p:

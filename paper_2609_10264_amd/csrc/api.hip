@@ -8,6 +8,7 @@
 #include <sys/random.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdlib>
 #include <initializer_list>
 #include <map>
@@ -17,6 +18,7 @@
 
 #include "mvk.h"
 #include "field.h"
+#include "kv.h"
 #include "mvk_internal.h"
 
 namespace mvk {
@@ -1215,6 +1217,178 @@ mvk_status mvk_decode_verify_seeded(const mvk_key* key, const mvk_st* st, const 
     if (s0) return s0;
     const ChallengeDraw draw{chal_seed};
     return decode_verify_run(key, Xhat, Yhat, B, &ey, Y, vL, vR, accept, s, &st->ex, &draw);
+}
+
+// ---------------------------------------------------------------------------
+// The client's attention
+// ---------------------------------------------------------------------------
+}  // extern "C"
+
+namespace {
+
+inline size_t type_size(int32_t type) { return type == MVK_TYPE_BF16 || type == MVK_TYPE_F16 ? 2 : 4; }
+inline bool is_float_type(int32_t type) { return type >= MVK_TYPE_BF16 && type <= MVK_TYPE_F32; }
+
+// a rows with stride sa and b of sb within, elements of size elem: beyond 2^62 bytes?
+inline bool span_too_big(uint64_t a, uint64_t sa, uint64_t b, uint64_t sb, uint64_t elem) {
+    if (too_big(a, sa, elem) || too_big(b, sb, elem)) return true;
+    return a * sa + b * sb > (1ull << 62) / elem;
+}
+
+mvk_status check_rows(const mvk_rows* r, uint64_t T, uint64_t heads) {
+    if (!r || (!r->data && T) || r->type < MVK_TYPE_BF16 || r->type > MVK_TYPE_FIELD) return MVK_EINVAL;
+    if ((uintptr_t)r->data % type_size(r->type) != 0) return MVK_EINVAL;
+    return span_too_big(T, r->token, heads, r->head, type_size(r->type)) ? MVK_ERANGE : MVK_OK;
+}
+
+mvk_status check_kv(const mvk_kv* kv) {
+    if (!kv || !kv->K || !kv->V || !is_float_type(kv->type)) return MVK_EINVAL;
+    if (!kv->pages || !kv->kv_heads || !kv->dim || !kv->page_size || (kv->page_size & (kv->page_size - 1)))
+        return MVK_EINVAL;
+    const size_t e = type_size(kv->type);
+    if ((uintptr_t)kv->K % e != 0 || (uintptr_t)kv->V % e != 0) return MVK_EINVAL;
+    if (kv->dim > MVK_MAX_HEAD_DIM || kv->kv_heads > 65535u || kv->pages > 0x7fffffffu) return MVK_ERANGE;
+    if (span_too_big(kv->pages, kv->k_page, kv->kv_heads, kv->k_head, e) || too_big(kv->page_size, kv->k_entry, e) ||
+        span_too_big(kv->pages, kv->v_page, kv->kv_heads, kv->v_head, e) || too_big(kv->page_size, kv->v_entry, e))
+        return MVK_ERANGE;
+    return MVK_OK;
+}
+
+// rows: the call has token rows, so q_start is read.
+mvk_status check_seqs(const mvk_seqs* sq, const mvk_kv* kv, bool rows) {
+    if (!sq || !sq->count || !sq->width || !sq->table || !sq->lens || (rows && !sq->q_start)) return MVK_EINVAL;
+    if (sq->table_stride < sq->width && sq->count > 1) return MVK_EINVAL;
+    // entries are counted in 31 bits, sequences are a grid dimension
+    if (sq->count > 65535u || (uint64_t)sq->width * kv->page_size > 0x7fffffffull) return MVK_ERANGE;
+    return too_big(sq->count, sq->table_stride, 4) ? MVK_ERANGE : MVK_OK;
+}
+
+Rows view_of(const mvk_rows* r) { return Rows{r->data, (size_t)r->token, (size_t)r->head, r->type}; }
+
+KvView view_of(const mvk_kv* kv) {
+    return KvView{kv->K, kv->V, (size_t)kv->k_page, (size_t)kv->k_head, (size_t)kv->k_entry, (size_t)kv->v_page,
+                  (size_t)kv->v_head, (size_t)kv->v_entry, kv->pages, kv->kv_heads,
+                  (uint32_t)__builtin_ctz(kv->page_size), kv->dim};
+}
+
+SeqView view_of(const mvk_seqs* sq) {
+    return SeqView{sq->table, sq->lens, sq->q_start, (size_t)sq->table_stride, sq->count, sq->width};
+}
+
+}  // namespace
+
+extern "C" {
+
+mvk_status mvk_rotary_table(uint32_t rot, uint32_t rows, double base, int32_t scaling, double factor,
+                            double original_len, double slow, double fast, float* table, void* stream) {
+    if (!rot || rot % 2 || !(base > 0) || scaling < MVK_SCALE_NONE || scaling > MVK_SCALE_PARTS) return MVK_EINVAL;
+    if (scaling != MVK_SCALE_NONE && !(factor >= 1)) return MVK_EINVAL;
+    if (scaling == MVK_SCALE_BASE && rot < 4) return MVK_EINVAL;
+    if (scaling == MVK_SCALE_PARTS && !(original_len > 0 && slow < fast)) return MVK_EINVAL;
+    if (rot > MVK_MAX_HEAD_DIM || rows > 0x7fffffffu) return MVK_ERANGE;
+    if (rows == 0) return MVK_OK;
+    if (!table) return MVK_EINVAL;
+    double f[MVK_MAX_HEAD_DIM / 2], mag = 1.0;
+    if (scaling == MVK_SCALE_BASE) base *= std::pow(factor, (double)rot / (rot - 2));
+    for (uint32_t i = 0; i < rot / 2; ++i) {
+        f[i] = std::pow(base, -2.0 * i / rot);
+        if (scaling == MVK_SCALE_LINEAR) f[i] /= factor;
+        if (scaling == MVK_SCALE_PARTS) {
+            // turns over the original context: few are interpolated, many left alone
+            const double turns = original_len * f[i] / (2 * 3.14159265358979323846);
+            const double keep = std::min(1.0, std::max(0.0, (turns - slow) / (fast - slow)));
+            f[i] = f[i] / factor * (1 - keep) + f[i] * keep;
+        }
+    }
+    if (scaling == MVK_SCALE_PARTS) mag = 0.1 * std::log(factor) + 1;
+    return hip_status(launch_rotary_table(f, rot / 2, rows, mag, table, (hipStream_t)stream));
+}
+
+mvk_status mvk_rotary_append(const mvk_rows* q, const mvk_rows* k, const mvk_rows* v, uint32_t T, uint32_t heads,
+                             uint32_t dim, uint32_t rot, int32_t layout, const int32_t* positions,
+                             const float* table, uint32_t table_rows, float field_scale, const mvk_rows* q_out,
+                             const mvk_kv* cache, const mvk_seqs* seqs, void* stream) {
+    if (!q != !q_out || !k != !v || !k != !cache || !k != !seqs || (!q && !k)) return MVK_EINVAL;
+    if (layout != MVK_ROTARY_HALF && layout != MVK_ROTARY_INTERLEAVED) return MVK_EINVAL;
+    if (!dim || rot % 2 || rot > dim || (rot && (!positions || !table || !table_rows))) return MVK_EINVAL;
+    if (dim > MVK_MAX_HEAD_DIM || T > 0x7fffffffu) return MVK_ERANGE;
+    mvk_status st = MVK_OK;
+    if (q) {
+        if (!heads) return MVK_EINVAL;
+        if (heads > 65535u) return MVK_ERANGE;
+        if ((st = check_rows(q, T, heads)) || (st = check_rows(q_out, T, heads))) return st;
+        if (!is_float_type(q_out->type)) return MVK_EINVAL;
+        // in place only element for element
+        if (q->data == q_out->data && (q->type != q_out->type || q->token != q_out->token || q->head != q_out->head))
+            return MVK_EINVAL;
+    }
+    if (k) {
+        if ((st = check_kv(cache)) || (st = check_seqs(seqs, cache, true))) return st;
+        if ((st = check_rows(k, T, cache->kv_heads)) || (st = check_rows(v, T, cache->kv_heads))) return st;
+        if (cache->dim != dim || k->type != v->type) return MVK_EINVAL;
+        if (q && (q->type != k->type || q_out->type != cache->type)) return MVK_EINVAL;
+    }
+    const int src = q ? q->type : k->type, dst = q ? q_out->type : cache->type;
+    if (src == MVK_TYPE_FIELD && !std::isfinite(field_scale)) return MVK_EINVAL;
+    if (T == 0) return MVK_OK;
+    Rows rq, rk, rv, ro;
+    KvView kv;
+    SeqView sq;
+    if (q) rq = view_of(q), ro = view_of(q_out);
+    if (k) rk = view_of(k), rv = view_of(v), kv = view_of(cache), sq = view_of(seqs);
+    return hip_status(launch_rotary(q ? &rq : nullptr, k ? &rk : nullptr, k ? &rv : nullptr, src, dst, T, heads, dim,
+                                    rot, layout == MVK_ROTARY_HALF, positions, table, table_rows, field_scale,
+                                    q ? &ro : nullptr, k ? &kv : nullptr, k ? &sq : nullptr, (hipStream_t)stream));
+}
+
+mvk_status mvk_paged_attention(const mvk_rows* q, uint32_t T, uint32_t heads, const mvk_kv* cache,
+                               const mvk_seqs* seqs, float scale, const mvk_rows* out, float field_scale, float* lse,
+                               const float* w_in, float* w_out, uint64_t w_seq, uint64_t w_head, void* stream) {
+    mvk_status st = check_kv(cache);
+    if (st || (st = check_seqs(seqs, cache, true))) return st;
+    if (!heads || heads % cache->kv_heads || !std::isfinite(scale)) return MVK_EINVAL;
+    if ((uint64_t)T * heads > 0x7fffffffull) return MVK_ERANGE;
+    if ((st = check_rows(q, T, heads)) || (st = check_rows(out, T, heads))) return st;
+    if (q->type != cache->type) return MVK_EINVAL;
+    if (out->type == MVK_TYPE_FIELD && !(std::isfinite(field_scale) && field_scale > 0)) return MVK_EINVAL;
+    const uint64_t cap = (uint64_t)seqs->width * cache->page_size;
+    if (w_in && !w_out) return MVK_EINVAL;
+    if (w_out && ((cache->kv_heads > 1 && w_head < cap) || (seqs->count > 1 && w_seq < cap))) return MVK_EINVAL;
+    if (w_out && span_too_big(seqs->count, w_seq, cache->kv_heads, w_head, 4)) return MVK_ERANGE;
+    if (T == 0 && !w_out) return MVK_OK;
+    hipStream_t s = (hipStream_t)stream;
+    if (w_out && !lse && T) {
+        void* ws = nullptr;
+        if ((st = workspace(s, (size_t)T * heads * sizeof(float), &ws))) return st;
+        lse = (float*)ws;
+    }
+    return hip_status(launch_attend(view_of(q), T, heads, view_of(cache), view_of(seqs), scale, view_of(out),
+                                    out->type == MVK_TYPE_FIELD ? 1.f / field_scale : 1.f, lse, w_in, w_out, w_seq,
+                                    w_head, s));
+}
+
+mvk_status mvk_cache_evict(const mvk_kv* src, const mvk_seqs* seqs, const float* w, uint64_t w_seq, uint64_t w_head,
+                           uint32_t budget, uint32_t recent, uint32_t sinks, const mvk_kv* dst,
+                           const int32_t* dst_table, uint64_t dst_table_stride, uint32_t dst_width, float* w_out,
+                           uint64_t o_seq, uint64_t o_head, int32_t* kept, int32_t* lens_out, void* stream) {
+    mvk_status st = check_kv(src);
+    if (st || (st = check_kv(dst)) || (st = check_seqs(seqs, src, false))) return st;
+    if (src->type != dst->type || src->kv_heads != dst->kv_heads || src->dim != dst->dim) return MVK_EINVAL;
+    if (!w || !kept || !lens_out || !dst_table || !dst_width || !budget) return MVK_EINVAL;
+    if ((uint64_t)sinks + recent > budget) return MVK_EINVAL;
+    const uint64_t cap = (uint64_t)seqs->width * src->page_size, most = std::min<uint64_t>(cap, budget);
+    const bool heads = src->kv_heads > 1, many = seqs->count > 1;
+    if ((heads && w_head < cap) || (many && w_seq < cap)) return MVK_EINVAL;
+    if (w_out && ((heads && o_head < most) || (many && o_seq < most))) return MVK_EINVAL;
+    if ((many && dst_table_stride < dst_width) || (uint64_t)dst_width * dst->page_size < most) return MVK_EINVAL;
+    if (budget > 0x7fffffffu || (uint64_t)dst_width * dst->page_size > 0x7fffffffull) return MVK_ERANGE;
+    if (span_too_big(seqs->count, w_seq, src->kv_heads, w_head, 4) ||
+        span_too_big(seqs->count, o_seq, src->kv_heads, o_head, 4) || too_big(seqs->count, dst_table_stride, 4) ||
+        too_big((uint64_t)seqs->count * src->kv_heads, budget, 4))
+        return MVK_ERANGE;
+    return hip_status(launch_evict(view_of(src), view_of(seqs), type_size(src->type), w, w_seq, w_head, budget, recent,
+                                   sinks, view_of(dst), dst_table, dst_table_stride, dst_width, w_out, o_seq, o_head,
+                                   kept, lens_out, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -271,6 +271,28 @@ void sample_sparse_host(uint32_t count, uint32_t N, uint32_t t, uint64_t seed, u
 hipError_t launch_sample_sparse(uint64_t seed, uint64_t tag, uint32_t count, uint32_t N, uint32_t t, uint32_t* idx,
                                 uint32_t* val, hipStream_t s);
 
+// rotary.hip, attention.hip, evict.hip (views: kv.h) --------------------------
+struct Rows;
+struct KvView;
+struct SeqView;
+// freq: half frequencies in radians a position; mag: factor of cosines and sines.
+hipError_t launch_rotary_table(const double* freq, uint32_t half, uint32_t rows, double mag, float* out,
+                               hipStream_t s);
+// q with qo, or k, v, kv with sq, may be null; src, dst: types of the inputs and of qo and the cache.
+hipError_t launch_rotary(const Rows* q, const Rows* k, const Rows* v, int src, int dst, uint32_t T, uint32_t heads,
+                         uint32_t dim, uint32_t rot, bool half, const int32_t* positions, const float* table,
+                         uint32_t table_rows, float scale, const Rows* qo, const KvView* kv, const SeqView* sq,
+                         hipStream_t s);
+// lse: tokens x heads floats, null only without w_out.
+hipError_t launch_attend(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
+                         float scale, const Rows& out, float inv_scale, float* lse, const float* w_in, float* w_out,
+                         size_t w_seq, size_t w_head, hipStream_t s);
+// elem: bytes of a value of the caches.
+hipError_t launch_evict(const KvView& src, const SeqView& sq, size_t elem, const float* w, size_t w_seq, size_t w_head,
+                        uint32_t budget, uint32_t recent, uint32_t sinks, const KvView& dst, const int32_t* dtable,
+                        size_t dts, uint32_t dwidth, float* wo, size_t o_seq, size_t o_head, int32_t* kept,
+                        int32_t* lens_out, hipStream_t s);
+
 inline uint32_t ceil_div(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
 
 }  // namespace mvk
