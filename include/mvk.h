@@ -708,8 +708,9 @@ typedef struct mvk_kv {
  * j / page_size] at j % page_size; lens[s] entries are in use, the new tokens'
  * among them.  The new tokens of sequence s are rows q_start[s] .. q_start[s+1]-1
  * of the call's token rows, the last entries of the sequence in that order
- * (q_start: count + 1 words; NULL where a call has no token rows).  max_new: no
- * sequence has more new tokens than this.  All arrays are device int32 and are
+ * (q_start: count + 1 words; NULL where a call has no token rows).  max_new: most
+ * new tokens of a sequence, as far as the caller knows (it chooses the kernel,
+ * not the result).  All arrays are device int32 and are
  * read when the work runs.  Lengths are clamped to the table's width, page
  * numbers outside the pool are read as the nearest page and never written. */
 typedef struct mvk_seqs {

@@ -1357,14 +1357,24 @@ mvk_status mvk_paged_attention(const mvk_rows* q, uint32_t T, uint32_t heads, co
     if (w_out && span_too_big(seqs->count, w_seq, cache->kv_heads, w_head, 4)) return MVK_ERANGE;
     if (T == 0 && !w_out) return MVK_OK;
     hipStream_t s = (hipStream_t)stream;
-    if (w_out && !lse && T) {
-        void* ws = nullptr;
-        if ((st = workspace(s, (size_t)T * heads * sizeof(float), &ws))) return st;
-        lse = (float*)ws;
-    }
-    return hip_status(launch_attend(view_of(q), T, heads, view_of(cache), view_of(seqs), scale, view_of(out),
-                                    out->type == MVK_TYPE_FIELD ? 1.f / field_scale : 1.f, lse, w_in, w_out, w_seq,
-                                    w_head, s));
+    const Rows rq = view_of(q), ro = view_of(out);
+    const KvView kv = view_of(cache);
+    const SeqView sq = view_of(seqs);
+    const float inv_scale = out->type == MVK_TYPE_FIELD ? 1.f / field_scale : 1.f;
+    const bool tile = attend_tile_fits(rq, T, heads, kv, sq);
+    const bool split = attend_tile_split(std::min(seqs->max_new, T), heads, kv);
+    const size_t lse_bytes = w_out && !lse ? align_up((size_t)T * heads * sizeof(float)) : 0;
+    const size_t bytes = lse_bytes + (tile ? attend_tile_bytes(kv, split) : 0);
+    void* ws = nullptr;
+    if (bytes && (st = workspace(s, bytes, &ws))) return st;
+    if (lse_bytes) lse = (float*)ws;
+    hipError_t e = hipSuccess;
+    if (tile)
+        e = launch_attend_tile(rq, T, heads, kv, sq, scale, ro, inv_scale, lse, split, (char*)ws + lse_bytes, s);
+    else if (T)
+        e = launch_attend_any(rq, T, heads, kv, sq, scale, ro, inv_scale, lse, s);
+    if (e == hipSuccess && w_out) e = launch_weights_any(rq, T, heads, kv, sq, scale, lse, w_in, w_out, w_seq, w_head, s);
+    return hip_status(e);
 }
 
 mvk_status mvk_cache_evict(const mvk_kv* src, const mvk_seqs* seqs, const float* w, uint64_t w_seq, uint64_t w_head,

@@ -124,34 +124,36 @@ __global__ __launch_bounds__(256) void weights_any(Rows q, uint32_t tokens, uint
     }
 }
 
-template <typename T>
-hipError_t launch_t(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq, float scale,
-                    const Rows& out, float inv_scale, float* lse, const float* w_in, float* w_out, size_t w_seq,
-                    size_t w_head, hipStream_t s) {
-    hipLaunchKernelGGL(attend_any<T>, dim3((uint32_t)(((uint64_t)tokens * heads + 3) / 4)), dim3(256), 0, s, q, tokens,
-                       heads, kv, sq, scale * kLog2e, out, inv_scale, lse);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !w_out) return e;
-    const uint64_t cap = (uint64_t)sq.width << kv.shift;
-    const uint32_t grid = (uint32_t)((cap + 255) / 256 < 65536 ? (cap + 255) / 256 : 65536);
-    hipLaunchKernelGGL(weights_any<T>, dim3(grid, kv.heads, sq.count), dim3(256), 0, s, q, tokens, heads, kv, sq,
-                       scale * kLog2e, lse, w_in, w_out, w_seq, w_head);
-    return hipGetLastError();
-}
-
 }  // namespace
 
-hipError_t launch_attend(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
-                         float scale, const Rows& out, float inv_scale, float* lse, const float* w_in, float* w_out,
-                         size_t w_seq, size_t w_head, hipStream_t s) {
+hipError_t launch_attend_any(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
+                             float scale, const Rows& out, float inv_scale, float* lse, hipStream_t s) {
+    const dim3 grid((uint32_t)(((uint64_t)tokens * heads + 3) / 4));
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, q, tokens, heads, kv, sq, scale * kLog2e, out, inv_scale, lse);
+        return hipGetLastError();
+    };
     switch (q.type) {
-        case MVK_TYPE_BF16:
-            return launch_t<__bf16>(q, tokens, heads, kv, sq, scale, out, inv_scale, lse, w_in, w_out, w_seq, w_head, s);
-        case MVK_TYPE_F16:
-            return launch_t<_Float16>(q, tokens, heads, kv, sq, scale, out, inv_scale, lse, w_in, w_out, w_seq, w_head,
-                                      s);
-        default:
-            return launch_t<float>(q, tokens, heads, kv, sq, scale, out, inv_scale, lse, w_in, w_out, w_seq, w_head, s);
+        case MVK_TYPE_BF16: return go(attend_any<__bf16>);
+        case MVK_TYPE_F16: return go(attend_any<_Float16>);
+        default: return go(attend_any<float>);
+    }
+}
+
+hipError_t launch_weights_any(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
+                              float scale, const float* lse, const float* w_in, float* w_out, size_t w_seq,
+                              size_t w_head, hipStream_t s) {
+    const uint64_t cap = (uint64_t)sq.width << kv.shift;
+    const dim3 grid((uint32_t)((cap + 255) / 256 < 65536 ? (cap + 255) / 256 : 65536), kv.heads, sq.count);
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, q, tokens, heads, kv, sq, scale * kLog2e, lse, w_in, w_out,
+                           w_seq, w_head);
+        return hipGetLastError();
+    };
+    switch (q.type) {
+        case MVK_TYPE_BF16: return go(weights_any<__bf16>);
+        case MVK_TYPE_F16: return go(weights_any<_Float16>);
+        default: return go(weights_any<float>);
     }
 }
 

@@ -283,10 +283,21 @@ hipError_t launch_rotary(const Rows* q, const Rows* k, const Rows* v, int src, i
                          uint32_t dim, uint32_t rot, bool half, const int32_t* positions, const float* table,
                          uint32_t table_rows, float scale, const Rows* qo, const KvView* kv, const SeqView* sq,
                          hipStream_t s);
-// lse: tokens x heads floats, null only without w_out.
-hipError_t launch_attend(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
-                         float scale, const Rows& out, float inv_scale, float* lse, const float* w_in, float* w_out,
-                         size_t w_seq, size_t w_head, hipStream_t s);
+// Any types, dims and strides; tokens > 0; lse (tokens x heads floats) may be null.
+hipError_t launch_attend_any(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
+                             float scale, const Rows& out, float inv_scale, float* lse, hipStream_t s);
+hipError_t launch_weights_any(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
+                              float scale, const float* lse, const float* w_in, float* w_out, size_t w_seq,
+                              size_t w_head, hipStream_t s);
+// attention_tile.hip: on the matrix cores where the problem fits.  split: the
+// form for few rows a sequence and kv head (max_new says how many; either form
+// is right for every problem).  ws: attend_tile_bytes, 16-byte aligned.
+bool attend_tile_fits(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq);
+bool attend_tile_split(uint32_t max_new, uint32_t heads, const KvView& kv);
+size_t attend_tile_bytes(const KvView& kv, bool split);
+hipError_t launch_attend_tile(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
+                              float scale, const Rows& out, float inv_scale, float* lse, bool split, void* ws,
+                              hipStream_t s);
 // elem: bytes of a value of the caches.
 hipError_t launch_evict(const KvView& src, const SeqView& sq, size_t elem, const float* w, size_t w_seq, size_t w_head,
                         uint32_t budget, uint32_t recent, uint32_t sinks, const KvView& dst, const int32_t* dtable,
