@@ -2,10 +2,10 @@
 //
 // Per (sequence, kv head) of n entries: keep the first `sinks`, the last
 // `recent` and the r = m - sinks - recent heaviest others, m = min(n, budget),
-// in order.  Two launches: evict_select finds the r-th largest weight by a
-// radix descent over order-preserving 32-bit keys and writes the kept indices;
-// evict_copy moves the kept rows.  Ties at the threshold go to the lowest
-// indices, counted in order, so the choice does not depend on timing.
+// in order.  Two launches: evict_select finds the r-th largest weight, as an
+// order-preserving 32-bit key, and writes the kept indices; evict_copy moves
+// the kept rows.  Ties at the threshold go to the lowest indices, counted in
+// order, so the choice does not depend on timing.
 #include "kv.h"
 #include "mvk_internal.h"
 
@@ -32,27 +32,147 @@ struct EvictArgs {
     int32_t* lens_out;
 };
 
-// Exclusive rank of this thread among the set flags of the workgroup, and their count.
-__device__ __forceinline__ uint32_t block_rank(bool f, uint32_t* sm, uint32_t& total) {
-    const uint64_t b = __ballot(f);
-    const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    __syncthreads();
-    if (lane == 0) sm[wave] = (uint32_t)__popcll(b);
-    __syncthreads();
-    uint32_t before = 0, sum = 0;
+// The largest key x such that at least `want` of the candidates' keys are >= x
+// (want >= 1, at most the candidates), one bit a step from the top.  count(x):
+// this wave's candidates with keys >= x.  Ends early where a count is exactly
+// `want`: then the kept are those >= x.
+template <typename Count>
+__device__ __forceinline__ uint32_t find_threshold(Count count, uint32_t want, uint32_t (*sm)[kSelWaves], bool& exact) {
+    const uint32_t wave = threadIdx.x >> 6;
+    uint32_t x = 0;
+    exact = false;
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t cand = x | (1u << bit);
+        const uint32_t mine = count(cand);
+        uint32_t* s = sm[bit & 1];  // two in turn: one barrier a step
+        if ((threadIdx.x & 63) == 0) s[wave] = mine;
+        __syncthreads();
+        uint32_t sum = 0;
 #pragma unroll
-    for (uint32_t i = 0; i < kSelWaves; ++i) {
-        const uint32_t c = sm[i];
-        if (i < wave) before += c;
-        sum += c;
+        for (uint32_t i = 0; i < kSelWaves; ++i) sum += s[i];
+        if (sum >= want) x = cand;
+        if (sum == want) {
+            exact = true;
+            break;
+        }
     }
-    total = sum;
-    return before + (uint32_t)__popcll(b & ((1ull << lane) - 1));
+    return x;
+}
+
+// Exclusive prefix sums of sm[0, kCount), in place, and the total (wave 0 scans).
+template <uint32_t kCount>
+__device__ __forceinline__ uint32_t scan_counts(uint32_t* sm, uint32_t* total) {
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        constexpr uint32_t kPer = (kCount + 63) / 64;
+        const uint32_t lane = threadIdx.x;
+        uint32_t c[kPer], sum = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kPer; ++i) {
+            const uint32_t at = lane * kPer + i;
+            c[i] = at < kCount ? sm[at] : 0u;
+            sum += c[i];
+        }
+        uint32_t incl = sum;
+#pragma unroll
+        for (uint32_t s = 1; s < 64; s <<= 1) {
+            const uint32_t y = (uint32_t)__shfl_up((int)incl, s);
+            if (lane >= s) incl += y;
+        }
+        uint32_t run = incl - sum;
+#pragma unroll
+        for (uint32_t i = 0; i < kPer; ++i) {
+            const uint32_t at = lane * kPer + i;
+            if (at < kCount) sm[at] = run;
+            run += c[i];
+        }
+        if (lane == 63) *total = incl;
+    }
+    __syncthreads();
+    return *total;
+}
+
+// Rows of up to kEach * kSelThreads entries: the keys stay in registers, entry
+// i * kSelThreads + tid in register i, so a step of the search is a compare and
+// the count of a lane mask for each.
+template <uint32_t kEach>
+__device__ __forceinline__ void select_in_registers(const EvictArgs& a, const float* w, float* wo, int32_t* kept,
+                                                    uint32_t n, uint32_t want, uint32_t (*sm)[kSelWaves],
+                                                    uint32_t* counts, uint32_t* tied, uint32_t* total) {
+    const uint32_t tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c0 = a.sinks, c1 = n - a.recent;
+    uint32_t k[kEach];
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+        const uint32_t e = i * kSelThreads + tid;
+        // 0 stands for what is no candidate, so the least candidate key is 1
+        k[i] = __float_as_uint(e < n ? w[e] : 0.f);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+        const uint32_t e = i * kSelThreads + tid;
+        k[i] = e >= c0 && e < c1 ? max(weight_key(__uint_as_float(k[i])), 1u) : 0u;
+    }
+    uint32_t thr = 0xffffffffu;
+    bool exact = true;
+    if (want)
+        thr = find_threshold(
+            [&](uint32_t c) {
+                uint32_t s = 0;
+#pragma unroll
+                for (uint32_t i = 0; i < kEach; ++i) s += (uint32_t)__popcll(__ballot(k[i] >= c));
+                return s;
+            },
+            want, sm, exact);
+    const uint64_t below = (1ull << lane) - 1;
+    uint32_t ties = 0xffffffffu;  // how many of the keys equal to thr are kept
+    if (!exact) {
+        // keys above thr are kept, and the first of those equal to it
+        uint32_t more = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) {
+            more += (uint32_t)__popcll(__ballot(k[i] > thr));
+            const uint32_t c = (uint32_t)__popcll(__ballot(k[i] == thr));
+            if (lane == 0) tied[i * kSelWaves + wave] = c;
+        }
+        __syncthreads();
+        if (lane == 0) sm[0][wave] = more;
+        scan_counts<kEach * kSelWaves>(tied, total);
+        uint32_t sum = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kSelWaves; ++i) sum += sm[0][i];
+        ties = want - sum;
+    }
+    auto keep = [&](uint32_t i) {
+        const uint32_t e = i * kSelThreads + tid;
+        bool f = want && (exact ? k[i] >= thr : k[i] > thr);
+        if (!exact) {
+            const uint64_t b = __ballot(k[i] == thr);
+            f |= k[i] == thr && tied[i * kSelWaves + wave] + (uint32_t)__popcll(b & below) < ties;
+        }
+        return e < n && (e < c0 || e >= c1 || f);
+    };
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+        const uint32_t c = (uint32_t)__popcll(__ballot(keep(i)));
+        if (lane == 0) counts[i * kSelWaves + wave] = c;
+    }
+    scan_counts<kEach * kSelWaves>(counts, total);
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+        const bool f = keep(i);
+        const uint64_t b = __ballot(f);
+        if (f) {
+            const uint32_t e = i * kSelThreads + tid;
+            const uint32_t r = counts[i * kSelWaves + wave] + (uint32_t)__popcll(b & below);
+            kept[r] = (int32_t)e;
+            if (wo) wo[r] = w[e];
+        }
+    }
 }
 
 __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a, SeqView sq) {
-    __shared__ uint32_t hist[256], sm[2 * kSelWaves], pick[2];
-    const uint32_t h = blockIdx.x, s = blockIdx.y, tid = threadIdx.x;
+    __shared__ uint32_t sm[2][kSelWaves], counts[32 * kSelWaves], tied[32 * kSelWaves], total;
+    const uint32_t h = blockIdx.x, s = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const uint32_t n = seq_entries(sq, a.shift, s), m = min(n, a.budget);
     const float* w = a.w + (size_t)s * a.w_seq + (size_t)h * a.w_head;
     float* wo = a.wo ? a.wo + (size_t)s * a.o_seq + (size_t)h * a.o_head : nullptr;
@@ -67,49 +187,63 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a, SeqView
         return;
     }
     // here n > budget >= sinks + recent
+    const uint32_t want = m - a.sinks - a.recent;
+    if (n <= 4 * kSelThreads) return select_in_registers<4>(a, w, wo, kept, n, want, sm, counts, tied, &total);
+    if (n <= 32 * kSelThreads) return select_in_registers<32>(a, w, wo, kept, n, want, sm, counts, tied, &total);
+    // longer rows: each step reads the weights again (they stay in L2)
     const uint32_t c0 = a.sinks, c1 = n - a.recent;
-    uint32_t want = m - a.sinks - a.recent, prefix = 0;  // the want-th largest of the keys that begin with prefix
-    if (want) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (tid < 256) hist[tid] = 0;
-            __syncthreads();
-            for (uint32_t i = c0 + tid; i < c1; i += kSelThreads) {
-                const uint32_t k = weight_key(w[i]);
-                if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1u);
-            }
-            __syncthreads();
-            if (tid == 0) {
-                uint32_t left = want, d = 255;
-                while (left > hist[d]) left -= hist[d--];  // the digits' counts sum to at least want
-                pick[0] = d;
-                pick[1] = left;
-            }
-            __syncthreads();
-            prefix |= pick[0] << shift;
-            want = pick[1];
+    auto key = [&](uint32_t e) { return e >= c0 && e < c1 ? max(weight_key(w[e]), 1u) : 0u; };
+    auto count_if = [&](auto pick) {
+        uint32_t c = 0;
+        for (uint32_t e0 = 0; e0 < n; e0 += kSelThreads) {
+            const uint32_t e = e0 + tid;
+            c += (uint32_t)__popcll(__ballot(e < n && pick(key(min(e, n - 1)))));
         }
+        return c;
+    };
+    uint32_t thr = 0xffffffffu, ties = 0xffffffffu;
+    bool exact = true;
+    if (want) thr = find_threshold([&](uint32_t c) { return count_if([c](uint32_t k) { return k >= c; }); }, want, sm, exact);
+    __syncthreads();
+    if (!exact) {
+        const uint32_t more = count_if([thr](uint32_t k) { return k > thr; });
+        if (lane == 0) sm[0][wave] = more;
+        __syncthreads();
+        uint32_t sum = 0;
+        for (uint32_t i = 0; i < kSelWaves; ++i) sum += sm[0][i];
+        ties = want - sum;
+        __syncthreads();
     }
-    // keys above prefix are kept, and the first `want` keys equal to it
-    uint32_t base = 0, ties = 0;
-    for (uint32_t i0 = 0; i0 < n; i0 += kSelThreads) {
-        const uint32_t i = i0 + tid;
-        const float x = i < n ? w[i] : 0.f;
-        const bool fixed = i < c0 || i >= c1;
-        const uint32_t k = weight_key(x);
-        const bool other = i < n && !fixed && m > a.sinks + a.recent;
-        uint32_t nt, nk;
-        const bool tie = other && k == prefix;
-        const uint32_t rt = block_rank(tie, sm, nt);
-        const bool keep = i < n && (fixed || (other && (k > prefix || (tie && ties + rt < want))));
-        const uint32_t rk = block_rank(keep, sm + kSelWaves, nk);
-        if (keep) {
-            kept[base + rk] = (int32_t)i;
-            if (wo) wo[base + rk] = x;
+    uint32_t base = 0, seen = 0;  // kept entries and ties before this block of entries
+    const uint64_t below = (1ull << lane) - 1;
+    for (uint32_t e0 = 0; e0 < n; e0 += kSelThreads) {
+        const uint32_t e = e0 + tid;
+        const uint32_t k = e < n ? key(e) : 0u;
+        const bool fixed = e < n && (e < c0 || e >= c1);
+        uint32_t rank = 0;
+        if (!exact) {
+            const uint64_t b = __ballot(k == thr);
+            if (lane == 0) counts[wave] = (uint32_t)__popcll(b);
+            const uint32_t nt = scan_counts<kSelWaves>(counts, &total);
+            rank = seen + counts[wave] + (uint32_t)__popcll(b & below);
+            seen += nt;
+            __syncthreads();
+        }
+        const bool f = fixed || (want && k && (exact ? k >= thr : k > thr || (k == thr && rank < ties)));
+        const uint64_t b = __ballot(f);
+        if (lane == 0) counts[wave] = (uint32_t)__popcll(b);
+        const uint32_t nk = scan_counts<kSelWaves>(counts, &total);
+        if (f) {
+            const uint32_t r = base + counts[wave] + (uint32_t)__popcll(b & below);
+            kept[r] = (int32_t)e;
+            if (wo) wo[r] = w[e];
         }
         base += nk;
-        ties += nt;
+        __syncthreads();
     }
 }
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 struct CopyArgs {
     KvView src, dst;
@@ -120,25 +254,53 @@ struct CopyArgs {
     const int32_t* kept;
 };
 
-// One thread per element (T: the element's size) or 16-byte granule of a kept row.
+// kRowsEach rows a group of threads that holds one, T (an element or a 16-byte
+// granule) a thread; their loads are in flight together.  dims: T's a row.
+constexpr uint32_t kRowsEach = 4;
 template <typename T>
-__global__ __launch_bounds__(256) void evict_copy(CopyArgs a, uint32_t per) {
+__global__ __launch_bounds__(256) void evict_copy(CopyArgs a, uint32_t dims, uint32_t per) {
     const uint32_t h = blockIdx.y, s = blockIdx.z;
     const uint32_t m = min(seq_entries(a.sq, a.src.shift, s), a.budget);
-    const size_t count = (size_t)m * per;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (size_t)gridDim.x * 256) {
-        const uint32_t r = (uint32_t)(i / per), c = (uint32_t)(i % per);
-        const uint32_t e = (uint32_t)a.kept[((size_t)s * gridDim.y + h) * a.budget + r];
-        if ((r >> a.dst.shift) >= a.dwidth) continue;
-        const int32_t dp = a.dtable[(size_t)s * a.dts + (r >> a.dst.shift)];
-        if (dp < 0 || (uint32_t)dp >= a.dst.pages) continue;
-        const uint32_t sp = seq_page(a.sq, a.src, s, e);
-        const uint32_t se = e & ((1u << a.src.shift) - 1), de = r & ((1u << a.dst.shift) - 1);
-        ((T*)a.dst.K)[dp * a.dst.kp + h * a.dst.kh + de * a.dst.ke + c] =
-            ((const T*)a.src.K)[sp * a.src.kp + h * a.src.kh + se * a.src.ke + c];
-        ((T*)a.dst.V)[dp * a.dst.vp + h * a.dst.vh + de * a.dst.ve + c] =
-            ((const T*)a.src.V)[sp * a.src.vp + h * a.src.vh + se * a.src.ve + c];
+    const uint32_t group = threadIdx.x / per, rows = 256 / per;  // rows at once: per threads each
+    const uint32_t r0 = blockIdx.x * rows * kRowsEach + group;
+    if (group >= rows || r0 >= m) return;
+    const int32_t* kept = a.kept + ((size_t)s * gridDim.y + h) * a.budget;
+    size_t ks[kRowsEach], vs[kRowsEach], kd[kRowsEach], vd[kRowsEach];
+    bool on[kRowsEach];
+#pragma unroll
+    for (uint32_t u = 0; u < kRowsEach; ++u) {
+        const uint32_t r = r0 + u * rows, e = (uint32_t)kept[min(r, m - 1)], slot = min(r, m - 1) >> a.dst.shift;
+        const uint32_t sp = seq_page(a.sq, a.src, s, e), se = e & ((1u << a.src.shift) - 1);
+        const int32_t dp = slot < a.dwidth ? a.dtable[(size_t)s * a.dts + slot] : -1;
+        on[u] = r < m && dp >= 0 && (uint32_t)dp < a.dst.pages;
+        const uint32_t de = r & ((1u << a.dst.shift) - 1);
+        ks[u] = sp * a.src.kp + h * a.src.kh + se * a.src.ke;
+        vs[u] = sp * a.src.vp + h * a.src.vh + se * a.src.ve;
+        kd[u] = dp * a.dst.kp + h * a.dst.kh + de * a.dst.ke;
+        vd[u] = dp * a.dst.vp + h * a.dst.vh + de * a.dst.ve;
     }
+    for (uint32_t c = threadIdx.x % per; c < dims; c += per) {
+        T k[kRowsEach], v[kRowsEach];
+#pragma unroll
+        for (uint32_t u = 0; u < kRowsEach; ++u) {
+            k[u] = ((const T*)a.src.K)[ks[u] + c];
+            v[u] = ((const T*)a.src.V)[vs[u] + c];
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < kRowsEach; ++u)
+            if (on[u]) {
+                ((T*)a.dst.K)[kd[u] + c] = k[u];
+                ((T*)a.dst.V)[vd[u] + c] = v[u];
+            }
+    }
+}
+
+// The view with strides in granules of `per` values; false where they are not whole.
+bool in_granules(KvView& v, uint32_t per) {
+    if ((uintptr_t)v.K % 16 || (uintptr_t)v.V % 16 || v.dim % per || (v.kp | v.kh | v.ke | v.vp | v.vh | v.ve) % per)
+        return false;
+    v.kp /= per, v.kh /= per, v.ke /= per, v.vp /= per, v.vh /= per, v.ve /= per;
+    return true;
 }
 
 }  // namespace
@@ -151,15 +313,20 @@ hipError_t launch_evict(const KvView& src, const SeqView& sq, size_t elem, const
     hipLaunchKernelGGL(evict_select, dim3(src.heads, sq.count), dim3(kSelThreads), 0, s, e, sq);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    const CopyArgs c = {src, dst, sq, dtable, dts, dwidth, budget, kept};
     const uint64_t cap = (uint64_t)sq.width << src.shift;
-    const uint64_t most = (cap < budget ? cap : budget) * src.dim;
-    const uint32_t grid = (uint32_t)(most / 256 + 1 < 4096 ? most / 256 + 1 : 4096);
-    if (elem == 2)
-        hipLaunchKernelGGL(evict_copy<uint16_t>, dim3(grid, src.heads, sq.count), dim3(256), 0, s, c, src.dim);
-    else
-        hipLaunchKernelGGL(evict_copy<uint32_t>, dim3(grid, src.heads, sq.count), dim3(256), 0, s, c, src.dim);
-    return hipGetLastError();
+    const uint32_t most = (uint32_t)(cap < budget ? cap : budget);
+    CopyArgs c = {src, dst, sq, dtable, dts, dwidth, budget, kept};
+    auto go = [&](auto kernel, uint32_t dims) {
+        uint32_t per = 1;
+        while (per < dims && per < 256) per *= 2;
+        const uint32_t each = 256 / per * kRowsEach;
+        hipLaunchKernelGGL(kernel, dim3((most + each - 1) / each, src.heads, sq.count), dim3(256), 0, s, c, dims, per);
+        return hipGetLastError();
+    };
+    const uint32_t per = (uint32_t)(16 / elem);
+    if (in_granules(c.src, per) && in_granules(c.dst, per)) return go(evict_copy<u32x4>, src.dim / per);
+    c.src = src, c.dst = dst;
+    return elem == 2 ? go(evict_copy<uint16_t>, src.dim) : go(evict_copy<uint32_t>, src.dim);
 }
 
 }  // namespace mvk
