@@ -609,6 +609,90 @@ __global__ __launch_bounds__(256) void attend_join(TileArgs a) {
     }
 }
 
+// Collected weights: a workgroup owns kWeightKeys entries of one (sequence, kv
+// head), 32 a wave, and adds the probabilities of all rows that see them, in
+// order: S = Q K^T (rows down, keys across, so that a lane sums its own key),
+// p = exp(scale S - lse).  K is read once; each wave reads the rows for itself.
+constexpr uint32_t kWeightKeys = 128;
+template <typename T, uint32_t kDim>
+__global__ __launch_bounds__(256) void weights_tile(TileArgs a, const float* __restrict__ lse, const float* w_in,
+                                                    float* w_out, size_t w_seq, size_t w_head) {
+    typedef typename Mma<T>::V8 V8;
+    __shared__ float row_lse[4][32];
+    __shared__ uint32_t row_lim[4][32];
+    const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const uint32_t kh = blockIdx.y, s = blockIdx.z, live = a.kv.dim / 8;
+    const SeqSpan sp = seq_span(a.sq, a.kv.shift, s, a.tokens);
+    const uint32_t j0 = blockIdx.x * kWeightKeys + 32 * wave;
+    if (j0 >= sp.n) return;  // no barrier below spans waves
+    const int64_t base = (int64_t)sp.n - sp.c;
+    const uint32_t j = j0 + col, jc = min(j, sp.n - 1);
+    V8 k[kDim / 16];
+    {
+        const size_t page = seq_page(a.sq, a.kv, s, jc), at = jc & ((1u << a.kv.shift) - 1);
+        const T* kr = (const T*)a.kv.K + page * a.kv.kp + kh * a.kv.kh + at * a.kv.ke;
+#pragma unroll
+        for (uint32_t t = 0; t < kDim / 16; ++t) {
+            u32x4 v = {0, 0, 0, 0};
+            const uint32_t g = 2 * t + half;
+            if (g < live) v = *(const u32x4*)(kr + 8 * g);
+            k[t] = __builtin_bit_cast(V8, v);
+        }
+    }
+    const uint32_t rows = sp.c * a.grp;
+    // rows of the first token that sees entry j0, from a whole 32 on
+    uint32_t r0 = j0 > base ? (uint32_t)((int64_t)j0 - base) * a.grp / 32 * 32 : 0u;
+    float sum = 0.f;
+    u32x4 q[kDim / 16];
+    float z = 0.f;
+    uint32_t lim = 0;
+    auto load = [&](uint32_t r) {
+        const uint32_t row = r + col;
+        const uint32_t tok = row / a.grp, head = kh * a.grp + row % a.grp;
+        z = INFINITY;
+        lim = 0;
+#pragma unroll
+        for (uint32_t t = 0; t < kDim / 16; ++t) q[t] = u32x4{0, 0, 0, 0};
+        if (row < rows) {
+            const int64_t see = base + tok + 1;
+            lim = see > 0 ? (uint32_t)see : 0u;
+            z = lse[(size_t)(sp.q0 + tok) * a.heads + head] * kLog2e;
+            if (z == -INFINITY) z = INFINITY;  // a row without a sum gives nothing
+            const T* qr = (const T*)a.q.p + (size_t)(sp.q0 + tok) * a.q.token + (size_t)head * a.q.head;
+#pragma unroll
+            for (uint32_t t = 0; t < kDim / 16; ++t) {
+                const uint32_t g = 2 * t + half;
+                if (g < live) q[t] = *(const u32x4*)(qr + 8 * g) ^ a.flip;
+            }
+        }
+    };
+    if (r0 < rows) load(r0);
+    for (; r0 < rows; r0 += 32) {
+        if (half == 0) row_lse[wave][col] = z, row_lim[wave][col] = lim;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        f32x16 x = {};
+#pragma unroll
+        for (uint32_t t = 0; t < kDim / 16; ++t) x = Mma<T>::mul(__builtin_bit_cast(V8, q[t]), k[t], x);
+        const bool masked = j0 + 32 > (uint32_t)__builtin_amdgcn_readfirstlane((int)lim) || r0 + 32 > rows;
+        if (r0 + 32 < rows) load(r0 + 32);
+#pragma unroll
+        for (uint32_t i = 0; i < 16; ++i) {
+            const uint32_t r = 8 * (i / 4) + 4 * half + i % 4;
+            float p = __builtin_amdgcn_exp2f(x[i] * a.sl2 - row_lse[wave][r]);
+            if (masked && j >= row_lim[wave][r]) p = 0.f;
+            sum += p;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    sum = sum_halves(sum);
+    if (half == 0 && j < sp.n) {
+        const size_t o = (size_t)s * w_seq + (size_t)kh * w_head + j;
+        w_out[o] = ((int64_t)j < base && w_in ? w_in[o] : 0.f) + sum;
+    }
+}
+
 constexpr uint32_t kGroups = 512;  // two workgroups a compute unit
 
 template <typename T, uint32_t kDim, bool kSplit>
@@ -664,15 +748,41 @@ bool attend_tile_split(uint32_t max_new, uint32_t heads, const KvView& kv) {
     return (uint64_t)max_new * (heads / kv.heads) <= 32;
 }
 
-hipError_t launch_attend_tile(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
-                              float scale, const Rows& out, float inv_scale, float* lse, bool split, void* ws,
-                              hipStream_t s) {
+namespace {
+
+TileArgs tile_args(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq, float scale) {
     TileArgs a = {};
-    a.q = q, a.out = out, a.kv = kv, a.sq = sq, a.tokens = tokens, a.heads = heads, a.grp = heads / kv.heads;
+    a.q = q, a.kv = kv, a.sq = sq, a.tokens = tokens, a.heads = heads, a.grp = heads / kv.heads;
     // the sign goes to q; a scale of zero as one that no score survives, so that masked places stay at -inf
     const float mag = scale < 0 ? -scale : scale;
     a.sl2 = mag < 1e-30f ? 1e-30f : mag * kLog2e;
     a.flip = scale < 0 ? 0x80008000u : 0u;
+    return a;
+}
+
+}  // namespace
+
+hipError_t launch_weights_tile(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
+                               float scale, const float* lse, const float* w_in, float* w_out, size_t w_seq,
+                               size_t w_head, hipStream_t s) {
+    const TileArgs a = tile_args(q, tokens, heads, kv, sq, scale);
+    const uint64_t cap = (uint64_t)sq.width << kv.shift;
+    const dim3 grid((uint32_t)((cap + kWeightKeys - 1) / kWeightKeys), kv.heads, sq.count);
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, lse, w_in, w_out, w_seq, w_head);
+        return hipGetLastError();
+    };
+    const uint32_t d = kv.dim <= 64 ? 0 : kv.dim <= 128 ? 1 : 2;
+    if (q.type == MVK_TYPE_BF16)
+        return d == 0 ? go(weights_tile<__bf16, 64>) : d == 1 ? go(weights_tile<__bf16, 128>) : go(weights_tile<__bf16, 256>);
+    return d == 0 ? go(weights_tile<_Float16, 64>) : d == 1 ? go(weights_tile<_Float16, 128>) : go(weights_tile<_Float16, 256>);
+}
+
+hipError_t launch_attend_tile(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
+                              float scale, const Rows& out, float inv_scale, float* lse, bool split, void* ws,
+                              hipStream_t s) {
+    TileArgs a = tile_args(q, tokens, heads, kv, sq, scale);
+    a.out = out;
     a.inv_scale = inv_scale, a.lse = lse;
     a.wide_out = (out.type == MVK_TYPE_BF16 || out.type == MVK_TYPE_F16) && (uintptr_t)out.p % 8 == 0 &&
                  (out.token | out.head) % 4 == 0;

@@ -298,6 +298,9 @@ size_t attend_tile_bytes(const KvView& kv, bool split);
 hipError_t launch_attend_tile(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
                               float scale, const Rows& out, float inv_scale, float* lse, bool split, void* ws,
                               hipStream_t s);
+hipError_t launch_weights_tile(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
+                               float scale, const float* lse, const float* w_in, float* w_out, size_t w_seq,
+                               size_t w_head, hipStream_t s);
 // elem: bytes of a value of the caches.
 hipError_t launch_evict(const KvView& src, const SeqView& sq, size_t elem, const float* w, size_t w_seq, size_t w_head,
                         uint32_t budget, uint32_t recent, uint32_t sinks, const KvView& dst, const int32_t* dtable,
