@@ -1366,11 +1366,15 @@ mvk_status mvk_paged_attention(const mvk_rows* q, uint32_t T, uint32_t heads, co
     const size_t lse_bytes = w_out && !lse ? align_up((size_t)T * heads * sizeof(float)) : 0;
     const size_t bytes = lse_bytes + (tile ? attend_tile_bytes(kv, split) : 0);
     void* ws = nullptr;
-    if (bytes && (st = workspace(s, bytes, &ws))) return st;
+    uint32_t* ctrl = nullptr;
+    if (bytes && (st = workspace(s, bytes, &ws, &ctrl, kCtrlBase + (tile ? attend_tile_ctrl_bytes() : 0)))) return st;
+    // the tile counters follow the first kCtrlBase bytes of the control region
+    uint32_t* counters = ctrl ? (uint32_t*)((char*)ctrl + kCtrlBase) : nullptr;
     if (lse_bytes) lse = (float*)ws;
     hipError_t e = hipSuccess;
     if (tile)
-        e = launch_attend_tile(rq, T, heads, kv, sq, scale, ro, inv_scale, lse, split, (char*)ws + lse_bytes, s);
+        e = launch_attend_tile(rq, T, heads, kv, sq, scale, ro, inv_scale, lse, split, (char*)ws + lse_bytes,
+                               counters, s);
     else if (T)
         e = launch_attend_any(rq, T, heads, kv, sq, scale, ro, inv_scale, lse, s);
     if (e == hipSuccess && w_out)

@@ -23,13 +23,17 @@
 //   chunks  (kSplit false): 128 rows, the 4 waves share each tile of keys;
 //   tokens  (kSplit true): 32 rows at most, each wave has keys of its own and
 //           the waves' results are joined in LDS.  Bound by the cache's read.
+// K and V go from memory straight to LDS, 16 bytes a lane; the order of the
+// granules that the reads want comes from which granule a lane asks for.  The
+// chunks form keeps two tiles, one in flight; the tokens form one, whose K half
+// is asked for again as soon as S is formed and whose V half when O is.
 //
 // Work split.  A unit is one step over kUnit keys of one tile; all units of the
 // call, in the order (sequence, kv head, tile, keys), are cut into equal
 // contiguous ranges, one per workgroup, whatever the sequences' lengths are
 // (they are read on the device).  A tile that a cut divides leaves parts
-// (unnormalised sums with their maxima) that attend_join adds in order, so the
-// result does not depend on timing.
+// (unnormalised sums with their maxima); the workgroup that counts itself last
+// on it adds them in order, so the result does not depend on timing.
 #include "kv.h"
 #include "mvk_internal.h"
 
@@ -62,23 +66,21 @@ struct Mma<_Float16> {
     static constexpr uint32_t kExp = 0x7c00u;
 };
 
-// sum_{i < n} floor((a i + b) / m), by the Euclidean descent.
-__device__ uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b) {
-    uint64_t sum = 0;
+// sum_{i < n} floor((a i + b) / m), by the Euclidean descent; a n + b and the
+// sum are below 2^32 (attend_tile_fits).
+__device__ __forceinline__ uint32_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
+    uint32_t sum = 0;
+#pragma unroll 1
     for (;;) {
-        if (a >= m) {
-            sum += n * (n - 1) / 2 * (a / m);
-            a %= m;
-        }
-        if (b >= m) {
-            sum += n * (b / m);
-            b %= m;
-        }
-        const uint64_t y = a * n + b;
+        const uint32_t qa = a / m, qb = b / m;
+        sum += (uint32_t)((uint64_t)n * (n - 1) / 2) * qa + n * qb;
+        a -= qa * m;
+        b -= qb * m;
+        const uint32_t y = a * n + b;
         if (y < m) return sum;
         n = y / m;
-        b = y % m;
-        const uint64_t t = m;
+        b = y - n * m;
+        const uint32_t t = m;
         m = a;
         a = t;
     }
@@ -91,18 +93,18 @@ struct Tiles {
     uint32_t grp;
     __device__ Tiles(const SeqSpan& sp, uint32_t grp) : c(sp.c), n(sp.n), grp(grp) {
         base = n > c ? n - c : 0;
-        count = (uint32_t)(((uint64_t)c * grp + kRows - 1) / kRows);
+        count = (c * grp + kRows - 1) / kRows;
         last = (base + c + kUnit - 1) / kUnit;
     }
     // units of tile t: its last row is a row of token ((t + 1) kRows - 1) / grp
     __device__ uint32_t units(uint32_t t) const {
         if (t + 1 >= count) return last;
-        return (base + (uint32_t)(((uint64_t)(t + 1) * kRows - 1) / grp) + kUnit) / kUnit;
+        return (base + ((t + 1) * kRows - 1) / grp + kUnit) / kUnit;
     }
     // units of the tiles before t (t < count)
     __device__ uint32_t before(uint32_t t) const {
         if (t == 0) return 0;
-        return (uint32_t)floor_sum(t, (uint64_t)grp * kUnit, kRows, (uint64_t)grp * (base + kUnit) + kRows - 1);
+        return floor_sum(t, grp * kUnit, kRows, grp * (base + kUnit) + kRows - 1);
     }
     __device__ uint32_t all() const { return count == 0 ? 0 : before(count - 1) + last; }
 };
@@ -117,7 +119,8 @@ struct TileArgs {
     float inv_scale;
     float* lse;
     float* part;    // 2 parts a workgroup: kRows x kDim sums, then kRows (maximum, sum)
-    uint4* split;   // per workgroup: the tile whose first part is its last (sequence, kv head, tile, parts)
+    uint32_t* counters;  // one a workgroup, kCounterStride words apart: zero before and after
+    bool whole_page;     // a tile of keys lies in one page, its offsets in 32 bits, and dim is kDim
     bool wide_out;  // out takes 8-byte stores of 4 16-bit values
 };
 
@@ -130,6 +133,8 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
     }
     return x;
 }
+
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
 
 // What a workgroup begins with.
 struct Start {
@@ -152,28 +157,27 @@ __device__ __forceinline__ uint32_t range_of(uint32_t x, uint32_t total, uint32_
 // Every wave by itself: the units of all sequences, and where range w begins.
 template <uint32_t kRows, uint32_t kUnit>
 __device__ __forceinline__ Start find_start(const TileArgs& a, uint32_t w, uint32_t groups) {
-    const uint32_t lane = threadIdx.x & 63, hk = a.kv.heads;
+    const uint32_t lane = threadIdx.x & 63, hk = a.kv.heads, chunks = (a.sq.count + 63) / 64;
     Start st = {};
-    uint32_t first = 0;  // units of sequence `lane`: kept, as most calls have at most 64 sequences
-    for (uint32_t s0 = 0; s0 < a.sq.count; s0 += 64) {
-        const uint32_t s = s0 + lane;
-        uint32_t u = 0;
-        if (s < a.sq.count) u = Tiles<kRows, kUnit>(seq_span(a.sq, a.kv.shift, s, a.tokens), a.grp).all() * hk;
-        if (s0 == 0) first = u;
-        st.total += (uint32_t)__shfl((int)wave_scan(u), 63);
-    }
-    const uint32_t x = range_at(w, st.total, groups);
-    st.left = range_at(w + 1, st.total, groups) - x;
-    if (st.left == 0) return st;
-    uint32_t seen = 0;
-    for (uint32_t s0 = 0; s0 < a.sq.count; s0 += 64) {
-        const uint32_t s = s0 + lane;
-        uint32_t u = first;
-        if (s0) {
+    uint32_t x = 0, seen = 0, u = 0, incl = 0;
+    // the sequences, 64 at a time, for the sum, then up to the one that holds unit x
+#pragma unroll 1
+    for (uint32_t it = 0; it < 2 * chunks; ++it) {
+        const uint32_t s0 = 64 * (it < chunks ? it : it - chunks), s = s0 + lane;
+        if (chunks > 1 || it == 0) {
             u = 0;
             if (s < a.sq.count) u = Tiles<kRows, kUnit>(seq_span(a.sq, a.kv.shift, s, a.tokens), a.grp).all() * hk;
+            incl = wave_scan(u);
         }
-        const uint32_t incl = wave_scan(u);
+        const uint32_t sum = (uint32_t)__shfl((int)incl, 63);
+        if (it < chunks) {
+            st.total += sum;
+            if (it + 1 < chunks) continue;
+            x = range_at(w, st.total, groups);
+            st.left = range_at(w + 1, st.total, groups) - x;
+            if (st.left == 0) return st;
+            continue;
+        }
         const uint64_t past = __ballot(seen + incl > x);
         if (past) {
             const int at = __ffsll((unsigned long long)past) - 1;
@@ -181,22 +185,24 @@ __device__ __forceinline__ Start find_start(const TileArgs& a, uint32_t w, uint3
             const uint32_t us = (uint32_t)__shfl((int)u, at), before = seen + (uint32_t)__shfl((int)incl, at) - us;
             const uint32_t per = us / hk, in = x - before;
             st.kh = in / per;
-            const uint32_t rem = in % per;
+            st.unit = in % per;
             const Tiles<kRows, kUnit> t(seq_span(a.sq, a.kv.shift, st.s, a.tokens), a.grp);
-            // the last tile whose units begin at or before rem: 64 candidates at a time
-            uint32_t lo = 0, hi = t.count;
+            // the last tile whose units begin at or before that: 64 candidates at a time
+            uint32_t lo = 0, hi = t.count, first = 0;
+#pragma unroll 1
             while (hi - lo > 1) {
                 const uint32_t step = (hi - lo + 63) / 64, cand = lo + lane * step;
-                const uint64_t ok = __ballot(cand < hi && t.before(cand) <= rem);
-                const uint32_t k = (uint32_t)__popcll(ok) - 1;  // (lane 0 always: before(lo) <= rem)
+                const uint32_t b = cand < hi ? t.before(cand) : 0xffffffffu;
+                const uint32_t k = (uint32_t)__popcll(__ballot(b <= st.unit)) - 1;  // (lane 0 always)
                 lo += k * step;
                 hi = min(hi, lo + step);
+                first = (uint32_t)__shfl((int)b, (int)k);
             }
             st.tile = lo;
-            st.unit = rem - t.before(lo);
+            st.unit -= first;
             return st;
         }
-        seen += (uint32_t)__shfl((int)incl, 63);
+        seen += sum;
     }
     st.left = 0;  // (not reached: the range begins below the total)
     return st;
@@ -225,21 +231,48 @@ __device__ __forceinline__ float sum_halves(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Any exponent of two packed values all ones (infinities, not-a-numbers)?
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t x) {
+    constexpr uint32_t e = Mma<T>::kExp * 0x10001u, one = (Mma<T>::kExp & (0u - Mma<T>::kExp)) * 0x10001u;
+    return ((x & e) + one) & 0x80008000u;
+}
+
+// A weight of 0 does not hide an infinity or a not-a-number from a product, so
+// a tile of V that some row does not see in full loses them here (granules
+// first, first + step, ...; true if there were any); the rows that do see them
+// get them back at the end, from the cache.
+template <typename T>
+__device__ __forceinline__ bool clean(u32x4* lv, uint32_t first, uint32_t step, uint32_t count) {
+    bool found = false;
+#pragma unroll 1
+    for (uint32_t i = first; i < count; i += step) {
+        u32x4 x = lv[i];
+        if ((not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) | not_finite<T>(x[3])) == 0) continue;
+        found = true;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t b = not_finite<T>(x[k]);
+            x[k] &= (b & 0x8000u ? 0u : 0xffffu) | (b & 0x80000000u ? 0u : 0xffff0000u);
+        }
+        lv[i] = x;
+    }
+    return found;
+}
+
 // The state of a wave's 32 rows: lane l has row l % 32 (l / 32: which half of
 // the keys of a block, and of the dims of a product, it holds).
-template <typename T, uint32_t kDim>
+template <typename T, uint32_t kDim, uint32_t kBlocks>
 struct WaveRows {
     typedef typename Mma<T>::V8 V8;
     V8 q[kDim / 16];
     f32x16 o[kDim / 32];  // O^T: register i of tile d: dim 32 d + 8 (i / 4) + 4 (l / 32) + i % 4
+    f32x16 s[kBlocks];    // S^T, then P^T: register i of block b: key 32 b + 8 (i / 4) + 4 (l / 32) + i % 4
     float m, l;           // maximum of q . k so far; this lane's part of the sum
     uint32_t lim;         // entries that the row sees
 
-    // One step over 32 kBlocks keys, the first of them entry j0, in LDS.
-    template <uint32_t kBlocks>
-    __device__ __forceinline__ void step(const u32x4* lk, const u32x4* lv, uint32_t j0, bool masked, float sl2) {
+    __device__ __forceinline__ void scores(const u32x4* lk) {
         const uint32_t lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
-        f32x16 s[kBlocks];
 #pragma unroll
         for (uint32_t b = 0; b < kBlocks; ++b) {
             s[b] = f32x16{};
@@ -249,6 +282,11 @@ struct WaveRows {
                 s[b] = Mma<T>::mul(k, q[t], s[b]);
             }
         }
+    }
+
+    // Scores of keys from entry j0 on into weights; the sums rescaled to the new maximum.
+    __device__ __forceinline__ void softmax(uint32_t j0, bool masked, float sl2) {
+        const uint32_t half = (threadIdx.x & 63) >> 5;
         if (masked) {
 #pragma unroll
             for (uint32_t b = 0; b < kBlocks; ++b)
@@ -280,7 +318,10 @@ struct WaveRows {
                 s[b][i] = __builtin_amdgcn_exp2f(s[b][i] * sl2 - base);
                 l += s[b][i];
             }
-        uint32_t bad = 0;
+    }
+
+    __device__ __forceinline__ void values(const u32x4* lv) {
+        const uint32_t lane = threadIdx.x & 63, half = lane >> 5;
 #pragma unroll
         for (uint32_t t = 0; t < 2 * kBlocks; ++t) {
             V8 p;
@@ -298,59 +339,61 @@ struct WaveRows {
                     v[w] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                         (__attribute__((address_space(3))) s16x4*)((const s16x4*)at + (lane & 1)));
                 }
-                if (masked) {
-                    // 0 * inf is not 0: infinities and not-a-numbers are taken out here, see below
-#pragma unroll
-                    for (uint32_t w = 0; w < 2; ++w)
-#pragma unroll
-                        for (uint32_t e = 0; e < 4; ++e)
-                            if (((uint32_t)v[w][e] & Mma<T>::kExp) == Mma<T>::kExp) {
-                                v[w][e] = 0;
-                                bad = 1;
-                            }
-                }
-                const V8 vv = __builtin_bit_cast(V8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                o[d] = Mma<T>::mul(vv, p, o[d]);
-            }
-        }
-        if (masked && __any(bad)) {
-            // the rows that see such a value get p v, the others nothing
-            for (uint32_t k = 0; k < 32 * kBlocks; ++k) {
-                const uint32_t b = k / 32, i = 4 * ((k % 32) / 8) + k % 4, owner = (k % 8) / 4;
-                float p = 0.f;
-#pragma unroll
-                for (uint32_t u = 0; u < 16 * kBlocks; ++u)
-                    if (u == 16 * b + i) p = s[u / 16][u % 16];
-                p = __shfl(p, (int)(col + 32 * owner));
-                if (j0 + k >= lim) continue;
-                const T* row = (const T*)lv;
-#pragma unroll
-                for (uint32_t d = 0; d < kDim / 32; ++d)
-#pragma unroll
-                    for (uint32_t u = 0; u < 16; ++u) {
-                        const uint32_t e = 32 * d + 8 * (u / 4) + 4 * half + u % 4;
-                        const T x = row[8 * v_at<kDim>(k, e / 8) + e % 8];
-                        if ((__builtin_bit_cast(uint16_t, x) & Mma<T>::kExp) == Mma<T>::kExp) o[d][u] += p * (float)x;
-                    }
+                o[d] = Mma<T>::mul(__builtin_bit_cast(V8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7)), p,
+                                   o[d]);
             }
         }
     }
 };
 
-// kBlocks: 32-key blocks of one tile of keys in LDS (shared, or one wave's).
 template <typename T, uint32_t kDim, bool kSplit>
 struct Shape {
-    static constexpr uint32_t kThreads = 256;
     static constexpr uint32_t kRows = kSplit ? 32 : 128;
-    static constexpr uint32_t kBlocks = kSplit ? 1 : 2;
-    static constexpr uint32_t kKeys = 32 * kBlocks;                       // keys of one LDS tile
-    static constexpr uint32_t kUnit = kSplit ? 4 * kKeys : kKeys;         // keys of one unit
-    static constexpr uint32_t kLoaders = kSplit ? 64 : kThreads;          // threads that fill a tile
-    static constexpr uint32_t kGranules = kKeys * (kDim / 8);             // of K, and of V
-    static constexpr uint32_t kPer = kGranules / kLoaders;                // granules a thread
-    static constexpr uint32_t kLds = (kSplit ? 4 : 2) * 2 * kGranules;    // granules: a wave's, or two stages
-    static constexpr uint32_t kPart = kRows * kDim + 2 * kRows;           // floats of a part
+    static constexpr uint32_t kBlocks = kSplit || kDim > 128 ? 1 : 2;  // 32-key blocks of an LDS tile
+    static constexpr uint32_t kKeys = 32 * kBlocks;
+    static constexpr uint32_t kUnit = kSplit ? 4 * kKeys : kKeys;    // keys of one unit
+    static constexpr uint32_t kGranules = kKeys * (kDim / 8);        // of K, and of V
+    static constexpr uint32_t kLoads = kGranules / 64 / (kSplit ? 1 : 4);  // of K, and of V, a wave
+    // a tile a wave, or two; the waves' results take their place
+    static constexpr uint32_t kTiles = (kSplit ? 4 : 2) * 2 * kGranules, kLds = kTiles > 32 * kDim ? kTiles : 32 * kDim;
+    static constexpr uint32_t kPart = kRows * kDim + 2 * kRows;      // floats of a part
 };
+
+// 16 zero bytes: what lanes beyond the head's dim load.
+__device__ const u32x4 kZeroGranule = {0, 0, 0, 0};
+
+// 16 bytes a lane from global memory to LDS at byte `to` (the wave's) + 16 lane,
+// from an address a lane, or from a base that the wave shares and an offset a
+// lane.  By hand: with the builtin every later LDS read waits for all loads in
+// flight, which ends the overlap.  The compiler does not count these loads;
+// wait_loads comes before their data is read.  (m0 is written and used inside
+// the statement; nothing else in this file uses it.)
+__device__ __forceinline__ void load_lds(const void* from, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+}
+__device__ __forceinline__ void load_lds(const void* base, uint32_t offset, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to)
+                 : "memory");
+}
+// All but the kNewest last loads of this wave have landed.
+template <uint32_t kNewest>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kNewest) : "memory");
+}
+
+// The LDS reads of this wave are done: their place may be filled again.
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Parts are written and read past the L2s, which do not see each other's lines.
+__device__ __forceinline__ void put_part(float* p, float x, float y) {
+    const u32x2 v = {__float_as_uint(x), __float_as_uint(y)};
+    __hip_atomic_store((uint64_t*)p, __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get_part(const float* p) {
+    const u32x2 v = __builtin_bit_cast(
+        u32x2, __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+    return {__uint_as_float(v[0]), __uint_as_float(v[1])};
+}
 
 // Four consecutive values of a row of the output.
 __device__ __forceinline__ void put4(const TileArgs& a, size_t at, f32x4 x) {
@@ -363,203 +406,291 @@ __device__ __forceinline__ void put4(const TileArgs& a, size_t at, f32x4 x) {
         *(u32x2*)((uint16_t*)a.out.p + at) = v;
         return;
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) store_as(a.out.p, a.out.type, at + i, x[i], a.inv_scale);
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+        const float y = i == 0 ? x[0] : i == 1 ? x[1] : i == 2 ? x[2] : x[3];
+        store_as(a.out.p, a.out.type, at + i, y, a.inv_scale);
+    }
 }
+
+// Four values y (not yet divided by the sum l) of row `row` of (sequence, kv head), dims 4 g and on.
+__device__ __forceinline__ void put_row(const TileArgs& a, const SeqSpan& sp, uint32_t kh, uint32_t row, uint32_t g,
+                                        f32x4 y, float m, float l) {
+    const uint32_t t = sp.q0 + row / a.grp, h = kh * a.grp + row % a.grp;
+    // (a sum that is not a number stays one; a row without entries is zero)
+    const float inv = l > 0.f ? 1.f / l : l;
+    put4(a, (size_t)t * a.out.token + (size_t)h * a.out.head + 4 * g, l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : y * inv);
+    if (a.lse && g == 0) a.lse[(size_t)t * a.heads + h] = l > 0.f ? (m * a.sl2 + log2f(l)) * kLn2 : l == 0.f ? -INFINITY : l;
+}
+
+constexpr uint32_t kCounterStride = 16;
 
 template <typename T, uint32_t kDim, bool kSplit>
 __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs a) {
     typedef Shape<T, kDim, kSplit> Sh;
     typedef typename Mma<T>::V8 V8;
+    constexpr uint32_t G = kDim / 8;  // granules a row
     __shared__ u32x4 lds[Sh::kLds];
     __shared__ float red[4][32][2];
-    const uint32_t tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, half = lane >> 5;
+    __shared__ uint32_t last_one, cleaned[2];  // (cleaned: of this segment and the next)
+    const uint32_t tid = threadIdx.x, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6)), lane = tid & 63;
+    const uint32_t col = lane & 31, half = lane >> 5;
     const uint32_t dim = a.kv.dim, live = dim / 8;  // granules of a row that hold data
     // consecutive ranges on one XCD, whose L2 then holds the keys they share
     const uint32_t groups = gridDim.x, xcds = groups % 8 == 0 ? 8 : 1;
     const uint32_t w = (blockIdx.x % xcds) * (groups / xcds) + blockIdx.x / xcds;
     Start st = find_start<Sh::kRows, Sh::kUnit>(a, w, groups);
-    if (tid == 0) a.split[w] = uint4{0, 0, 0, 0};
-    const uint32_t loader = kSplit ? lane : tid;
-    const uint32_t lg = loader % (kDim / 8), lr = loader / (kDim / 8);        // first granule of this thread
-    constexpr uint32_t kRowStep = Sh::kLoaders / (kDim / 8);                  // rows between its granules
+    st = {uniform(st.s), uniform(st.kh), uniform(st.tile), uniform(st.unit), uniform(st.left), uniform(st.total)};
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
     u32x4* const mine = kSplit ? lds + wave * 2 * Sh::kGranules : lds;
+    // load i of this wave fills 64 granules from granule 64 (i + kLoads wave) of the tile on
+    const uint32_t part0 = kSplit ? 0 : 64 * Sh::kLoads * wave;
 
-    uint32_t done = 0;
+    if (tid == 0) cleaned[0] = 0;
+    __syncthreads();
+    uint32_t done = 0, turn = 0;
+#pragma unroll 1
     while (done < st.left) {
-        const SeqSpan sp = seq_span(a.sq, a.kv.shift, st.s, a.tokens);
+        SeqSpan sp = seq_span(a.sq, a.kv.shift, st.s, a.tokens);
+        sp = {uniform(sp.q0), uniform(sp.c), uniform(sp.n)};
         const Tiles<Sh::kRows, Sh::kUnit> tiles(sp, a.grp);
         const uint32_t units = tiles.units(st.tile);
         const uint32_t u0 = st.unit, u1 = min(units, u0 + (st.left - done));
 
         // rows
-        const uint32_t rows = sp.c * a.grp, row0 = st.tile * Sh::kRows + (kSplit ? 0 : 32 * wave);
-        const uint32_t row = row0 + col, known = min(row, rows - 1);
-        const bool valid = row < rows;
-        const uint32_t tok = sp.q0 + known / a.grp, head = st.kh * a.grp + known % a.grp;
-        WaveRows<T, kDim> x;
+        const uint32_t rows = sp.c * a.grp, tile0 = st.tile * Sh::kRows, row0 = tile0 + (kSplit ? 0 : 32 * wave);
+        const uint32_t known = min(row0 + col, rows - 1);
+        WaveRows<T, kDim, Sh::kBlocks> x;
         {
-            const int64_t see = (int64_t)sp.n - sp.c + known / a.grp + 1;
+            const uint32_t tok = known / a.grp, head = st.kh * a.grp + known % a.grp;
+            const int64_t see = (int64_t)sp.n - sp.c + tok + 1;
             x.lim = see > 0 ? (uint32_t)see : 0u;
-            const T* qr = (const T*)a.q.p + (size_t)tok * a.q.token + (size_t)head * a.q.head;
+            const T* qr = (const T*)a.q.p + (size_t)(sp.q0 + tok) * a.q.token + (size_t)head * a.q.head;
+            u32x4 v[kDim / 16];  // (rows and granules that are not there: zeros, so that all loads are in flight at once)
 #pragma unroll
             for (uint32_t t = 0; t < kDim / 16; ++t) {
-                u32x4 v = {0, 0, 0, 0};
                 const uint32_t g = 2 * t + half;
-                if (valid && g < live) v = *(const u32x4*)(qr + 8 * g) ^ a.flip;
-                x.q[t] = __builtin_bit_cast(V8, v);
+                v[t] = *(row0 + col < rows && g < live ? (const u32x4*)(qr + 8 * g) : &kZeroGranule);
             }
+#pragma unroll
+            for (uint32_t t = 0; t < kDim / 16; ++t) x.q[t] = __builtin_bit_cast(V8, v[t] ^ a.flip);
 #pragma unroll
             for (uint32_t d = 0; d < kDim / 32; ++d) x.o[d] = f32x16{};
             x.m = -INFINITY;
             x.l = 0.f;
         }
         // limits of the wave's rows: rows are in order, so lane 0 sees least
-        const uint32_t lim_lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)x.lim);
+        const uint32_t lim_lo = uniform(x.lim);
         const uint32_t lim_hi = (uint32_t)__builtin_amdgcn_readlane((int)x.lim, 31);
+        const uint32_t lim_0 = (uint32_t)max((int64_t)sp.n - sp.c + tile0 / a.grp + 1, (int64_t)0);  // of the tile's rows
         const bool idle = !kSplit && row0 >= rows;  // a wave without rows
 
-        const T* const kb = (const T*)a.kv.K + (size_t)st.kh * a.kv.kh;
-        const T* const vb = (const T*)a.kv.V + (size_t)st.kh * a.kv.vh;
-        u32x4 rk[Sh::kPer], rv[Sh::kPer];
-        uint32_t pg[Sh::kPer];
+        // keys
+        const char* const kb = (const char*)((const T*)a.kv.K + (size_t)st.kh * a.kv.kh);
+        const char* const vb = (const char*)((const T*)a.kv.V + (size_t)st.kh * a.kv.vh);
         const uint32_t mask = (1u << a.kv.shift) - 1;
         const uint32_t first = u0 * Sh::kUnit + (kSplit ? wave * Sh::kKeys : 0);
         const uint32_t stop = min(u1 * Sh::kUnit, sp.n);  // entries at and beyond it are not needed
-        // entries beyond the last are loaded as the last (and masked): no address leaves the sequence
+        uint32_t ids = 0, id0 = 0, id1 = 0;  // lane i: the page of the sequence's pages id0 + i, of id0 .. id1 - 1
+        // before the loads of the tile at j0: its pages are known (places beyond the
+        // last page in use are read in that page, so no address leaves the pool)
         auto pages = [&](uint32_t j0) {
-            if (j0 < stop) {
-#pragma unroll
-                for (uint32_t i = 0; i < Sh::kPer; ++i) pg[i] = seq_page(a.sq, a.kv, st.s, min(j0 + lr + i * kRowStep, sp.n - 1));
+            if ((min(j0 + Sh::kKeys, sp.n) - 1) >> a.kv.shift >= id1) {
+                id0 = j0 >> a.kv.shift;
+                id1 = id0 + 64;
+                ids = seq_page(a.sq, a.kv, st.s, min((id0 + lane) << a.kv.shift, sp.n - 1));
             }
         };
-        auto load = [&](uint32_t j0) {
-            if (j0 < stop) {
+        // load i of the wave: granules part0 + 64 i + lane of the tile, that is rows kStep i + lane / G on
+        constexpr uint32_t kStep = 64 / G > 0 ? 64 / G : 1;
+        const uint32_t lane_row = part0 / G + lane / G;
+        auto granule = [&](bool is_v, uint32_t r) { return (is_v ? v_at<kDim>(r, lane % G) : k_at<kDim>(r, lane % G)) % G; };
+        auto load = [&](const char* base, size_t page_stride, size_t entry_stride, bool is_v, uint32_t j0, uint32_t to) {
+            if (a.whole_page) {
+                // a base that the wave shares, and 32-bit offsets of which a few differ
+                const uint32_t pg = (uint32_t)__builtin_amdgcn_readlane((int)ids, (int)((j0 >> a.kv.shift) - id0));
+                const char* b = base + ((size_t)pg * page_stride + (size_t)(j0 & mask) * entry_stride) * sizeof(T);
 #pragma unroll
-                for (uint32_t i = 0; i < Sh::kPer; ++i) {
-                    const uint32_t e = min(j0 + lr + i * kRowStep, sp.n - 1) & mask;
-                    rk[i] = rv[i] = u32x4{0, 0, 0, 0};
-                    if (lg < live) {
-                        rk[i] = *(const u32x4*)(kb + pg[i] * a.kv.kp + e * a.kv.ke + 8 * lg);
-                        rv[i] = *(const u32x4*)(vb + pg[i] * a.kv.vp + e * a.kv.ve + 8 * lg);
-                    }
+                for (uint32_t i = 0; i < Sh::kLoads; ++i)
+                    load_lds(b + (size_t)(kStep * i * (uint32_t)entry_stride * sizeof(T)),
+                             (uint32_t)((lane_row * (uint32_t)entry_stride + 8 * granule(is_v, kStep * i + lane_row)) * sizeof(T)),
+                             to + 1024 * i);
+            } else {
+                const uint32_t used = (sp.n - 1) >> a.kv.shift;
+#pragma unroll 1
+                for (uint32_t i = 0; i < Sh::kLoads; ++i) {
+                    const uint32_t r = kStep * i + lane_row, g = granule(is_v, r), j = j0 + r;
+                    const size_t pg = (uint32_t)__shfl((int)ids, (int)(min(j >> a.kv.shift, used) - id0));
+                    const void* from = base + (pg * page_stride + (size_t)(j & mask) * entry_stride + 8 * g) * sizeof(T);
+                    load_lds(g < live ? from : (const void*)&kZeroGranule, to + 1024 * i);
                 }
             }
         };
-        auto store = [&](u32x4* to) {
-#pragma unroll
-            for (uint32_t i = 0; i < Sh::kPer; ++i) {
-                to[k_at<kDim>(lr + i * kRowStep, lg)] = rk[i];
-                to[Sh::kGranules + v_at<kDim>(lr + i * kRowStep, lg)] = rv[i];
-            }
+        auto load_k = [&](uint32_t j0, uint32_t stage) {
+            load(kb, a.kv.kp, a.kv.ke, false, j0, lds0 + 16 * ((kSplit ? wave : stage) * 2 * Sh::kGranules + part0));
         };
-        pages(first);
-        load(first);
-        pages(first + Sh::kUnit);
-        uint32_t stage = 0;
-        for (uint32_t j0 = first; j0 < stop; j0 += Sh::kUnit) {
-            u32x4* const buf = kSplit ? mine : mine + stage * 2 * Sh::kGranules;
-            store(buf);
-            if (kSplit) {
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-            } else {
-                __syncthreads();  // the other stage is free: every wave has passed its step
+        auto load_v = [&](uint32_t j0, uint32_t stage) {
+            load(vb, a.kv.vp, a.kv.ve, true, j0, lds0 + 16 * ((kSplit ? wave : stage) * 2 * Sh::kGranules + Sh::kGranules + part0));
+        };
+        if (first < stop) {
+            pages(first);
+            load_k(first, 0);
+            load_v(first, 0);
+        }
+        if (kSplit) {
+#pragma unroll 1
+            for (uint32_t j0 = first; j0 < stop; j0 += Sh::kUnit) {
+                const bool more = j0 + Sh::kUnit < stop, masked = j0 + Sh::kKeys > lim_lo;
+                wait_loads<Sh::kLoads>();  // K
+                x.scores(mine);
+                if (more) {
+                    pages(j0 + Sh::kUnit);
+                    wait_reads();
+                    load_k(j0 + Sh::kUnit, 0);
+                }
+                x.softmax(j0, masked, a.sl2);
+                if (more) wait_loads<Sh::kLoads>();
+                else wait_loads<0>();
+                if (masked && __any(clean<T>(mine + Sh::kGranules, lane, 64, Sh::kGranules))) cleaned[turn] = 1;
+                x.values(mine + Sh::kGranules);
+                wait_reads();
+                if (more) load_v(j0 + Sh::kUnit, 0);
             }
-            load(j0 + Sh::kUnit);
-            pages(j0 + 2 * Sh::kUnit);
-            if (!idle && j0 < lim_hi)
-                x.template step<Sh::kBlocks>(buf, buf + Sh::kGranules, j0, j0 + Sh::kKeys > lim_lo, a.sl2);
-            if (kSplit) {
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
+        } else {
+            uint32_t stage = 0;
+#pragma unroll 1
+            for (uint32_t j0 = first; j0 < stop; j0 += Sh::kUnit) {
+                wait_loads<0>();
+                __syncthreads();  // this tile is there, and every wave has passed the other one
+                if (j0 + Sh::kUnit < stop) {
+                    pages(j0 + Sh::kUnit);
+                    load_k(j0 + Sh::kUnit, stage ^ 1);
+                    load_v(j0 + Sh::kUnit, stage ^ 1);
+                }
+                u32x4* buf = mine + stage * 2 * Sh::kGranules;
+                if (j0 + Sh::kKeys > lim_0) {  // for all waves alike
+                    if (clean<T>(buf + Sh::kGranules, tid, 256, Sh::kGranules)) cleaned[turn] = 1;
+                    __syncthreads();
+                }
+                if (!idle && j0 < lim_hi) {
+                    x.scores(buf);
+                    x.softmax(j0, j0 + Sh::kKeys > lim_lo, a.sl2);
+                    x.values(buf + Sh::kGranules);
+                }
+                stage ^= 1;
             }
-            stage ^= 1;
         }
 
-        // the rows' results
-        const bool whole = u0 == 0 && u1 == units;
-        float* const part = a.part + (size_t)(2 * w + (u0 == 0 ? 1 : 0)) * Sh::kPart;
-        float l = sum_halves(x.l);
-        if (kSplit) {
-            // join the waves: the common maximum, then sums of the rescaled rows
-            if (lane < 32) red[wave][lane][0] = x.m, red[wave][lane][1] = l;
-            __syncthreads();
-            float m = red[0][col][0];
+        // The results of the waves in LDS: wave, row, dim, four dims a granule,
+        // permuted like the keys.
+        __syncthreads();
+        float* const all = (float*)lds;
+        const float l = sum_halves(x.l);
+        if (tid == 0) cleaned[turn ^ 1] = 0;
+        if (half == 0) red[wave][col][0] = x.m, red[wave][col][1] = l;
 #pragma unroll
-            for (uint32_t i = 1; i < 4; ++i) m = fmaxf(m, red[i][col][0]);
-            const float base = m == -INFINITY ? 0.f : m * a.sl2;
-            const float f = __builtin_amdgcn_exp2f(x.m * a.sl2 - base);
-            float* const all = (float*)lds;  // wave, row, dim (rows kDim + 4 apart would cost LDS that is not there)
-            float* const own = all + (size_t)wave * 32 * kDim + col * kDim;
-            const uint32_t n32 = min(rows - row0, 32u);
-            if (col < n32) {
+        for (uint32_t d = 0; d < kDim / 32; ++d)
 #pragma unroll
-                for (uint32_t d = 0; d < kDim / 32; ++d)
-#pragma unroll
-                    for (uint32_t i = 0; i < 4; ++i) {
-                        const uint32_t e = 32 * d + 8 * i + 4 * half;
-                        f32x4 y;
-#pragma unroll
-                        for (uint32_t k = 0; k < 4; ++k) y[k] = x.o[d][4 * i + k] * f;
-                        *(f32x4*)(own + ((e / 4) ^ (col & 7)) * 4) = y;
-                    }
+            for (uint32_t i = 0; i < 4; ++i) {
+                const uint32_t g = 8 * d + 2 * i + half;
+                *(f32x4*)(all + (wave * 32 + col) * kDim + (g ^ (col & 7)) * 4) =
+                    f32x4{x.o[d][4 * i], x.o[d][4 * i + 1], x.o[d][4 * i + 2], x.o[d][4 * i + 3]};
             }
-            __syncthreads();
-            for (uint32_t i = tid; i < n32 * (kDim / 4); i += 256) {
-                const uint32_t r = i / (kDim / 4), g = i % (kDim / 4);
-                if (4 * g >= dim) continue;
-                f32x4 y = {0.f, 0.f, 0.f, 0.f};
-                float ls = 0.f, mr = red[0][r][0];
-#pragma unroll
-                for (uint32_t v = 1; v < 4; ++v) mr = fmaxf(mr, red[v][r][0]);
-                const float b2 = mr == -INFINITY ? 0.f : mr * a.sl2;
+        __syncthreads();
+        const bool whole = u0 == 0 && u1 == units;
+        const uint32_t count = min(rows - tile0, Sh::kRows);
+        float* const part = a.part + (size_t)(2 * w + (u0 == 0 ? 1 : 0)) * Sh::kPart;
+#pragma unroll 1
+        for (uint32_t i = tid; i < count * (kDim / 4); i += 256) {
+            const uint32_t r = i / (kDim / 4), g = i % (kDim / 4);
+            if (4 * g >= dim) continue;
+            f32x4 y;
+            float m, ls;
+            if (kSplit) {
+                m = fmaxf(fmaxf(red[0][r][0], red[1][r][0]), fmaxf(red[2][r][0], red[3][r][0]));
+                const float base = m == -INFINITY ? 0.f : m * a.sl2;
+                ls = 0.f;
+                y = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (uint32_t v = 0; v < 4; ++v) {
-                    y += *(const f32x4*)(all + (size_t)v * 32 * kDim + r * kDim + (g ^ (r & 7)) * 4);
-                    ls += red[v][r][1] * __builtin_amdgcn_exp2f(red[v][r][0] * a.sl2 - b2);
+                    const float f = __builtin_amdgcn_exp2f(red[v][r][0] * a.sl2 - base);
+                    ls += red[v][r][1] * f;
+                    y += *(const f32x4*)(all + (v * 32 + r) * kDim + (g ^ (r & 7)) * 4) * f;
                 }
-                if (whole) {
-                    const uint32_t rr = row0 + r, t2 = sp.q0 + rr / a.grp, h2 = st.kh * a.grp + rr % a.grp;
-                    const float inv = ls > 0.f ? 1.f / ls : ls == 0.f ? 0.f : ls;
-                    put4(a, (size_t)t2 * a.out.token + (size_t)h2 * a.out.head + 4 * g, y * inv);
-                    if (a.lse && g == 0)
-                        a.lse[(size_t)t2 * a.heads + h2] =
-                            ls > 0.f ? (mr * a.sl2 + log2f(ls)) * kLn2 : ls == 0.f ? -INFINITY : ls;
-                } else {
-                    *(f32x4*)(part + r * kDim + 4 * g) = y;
-                    if (g == 0) part[Sh::kRows * kDim + 2 * r] = mr, part[Sh::kRows * kDim + 2 * r + 1] = ls;
+            } else {
+                m = red[r / 32][r % 32][0];
+                ls = red[r / 32][r % 32][1];
+                y = *(const f32x4*)(all + r * kDim + (g ^ (r & 7)) * 4);
+            }
+            if (cleaned[turn]) {
+                // infinities and not-a-numbers that the row sees in the tiles that lost theirs
+                const int64_t see = (int64_t)sp.n - sp.c + (tile0 + r) / a.grp + 1;
+                for (int64_t j = max((int64_t)(lim_0 / Sh::kKeys * Sh::kKeys), (int64_t)u0 * Sh::kUnit); j < see && j < stop; ++j) {
+                    const T* v = (const T*)vb + seq_page(a.sq, a.kv, st.s, (uint32_t)j) * a.kv.vp + ((uint32_t)j & mask) * a.kv.ve + 4 * g;
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) {
+                        const float f = (float)v[k];
+                        if (f - f != 0.f) y[k] += f;
+                    }
                 }
             }
-        } else if (valid) {
-            const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-            const size_t at = (size_t)tok * a.out.token + (size_t)head * a.out.head;
-            const uint32_t r = 32 * wave + col;
-#pragma unroll
-            for (uint32_t d = 0; d < kDim / 32; ++d)
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    const uint32_t e = 32 * d + 8 * i + 4 * half;
-                    if (e >= dim) continue;
-                    f32x4 y;
-#pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k) y[k] = x.o[d][4 * i + k];
-                    if (whole) put4(a, at + e, y * inv);
-                    else *(f32x4*)(part + (size_t)r * kDim + e) = y;
-                }
-            if (half == 0) {
-                if (!whole) part[Sh::kRows * kDim + 2 * r] = x.m, part[Sh::kRows * kDim + 2 * r + 1] = l;
-                else if (a.lse)
-                    a.lse[(size_t)tok * a.heads + head] =
-                        l > 0.f ? (x.m * a.sl2 + log2f(l)) * kLn2 : l == 0.f ? -INFINITY : l;
+            if (whole) {
+                put_row(a, sp, st.kh, tile0 + r, g, y, m, ls);
+            } else {
+                put_part(part + r * kDim + 4 * g, y[0], y[1]);
+                put_part(part + r * kDim + 4 * g + 2, y[2], y[3]);
+                if (g == 0) put_part(part + Sh::kRows * kDim + 2 * r, m, ls);
             }
         }
-        if (tid == 0 && u0 == 0 && !whole) {
-            // the tile goes on in the next ranges
-            const uint32_t at = range_at(w, st.total, groups) + done;
-            a.split[w] = uint4{st.s, st.kh, st.tile, range_of(at + units - 1, st.total, groups) - w};
+        if (!whole) {
+            // the tile's ranges w0 .. w1, counted on the first one's word
+            const uint32_t at = range_at(w, st.total, groups) + done - u0;
+            const uint32_t w0 = range_of(at, st.total, groups), w1 = range_of(at + units - 1, st.total, groups);
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+            if (tid == 0) {
+                uint32_t* c = a.counters + w0 * kCounterStride;
+                const bool is_last = atomicAdd(c, 1u) == w1 - w0;
+                if (is_last) atomicExch(c, 0u);
+                last_one = is_last;
+            }
+            __syncthreads();
+            if (uniform(last_one)) {
+#pragma unroll 1
+                for (uint32_t i = tid; i < count * (kDim / 4); i += 256) {
+                    const uint32_t r = i / (kDim / 4), g = i % (kDim / 4);
+                    if (4 * g >= dim) continue;
+                    float m = -INFINITY, ls = 0.f;
+                    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+                    constexpr uint32_t kAhead = 4;  // parts whose loads are in flight together
+#pragma unroll 1
+                    for (uint32_t v = w0; v <= w1; v += kAhead) {
+                        float2 ml[kAhead], ya[kAhead], yb[kAhead];
+#pragma unroll
+                        for (uint32_t u = 0; u < kAhead; ++u) {
+                            const uint32_t vu = min(v + u, w1);
+                            const float* p = a.part + (size_t)(2 * vu + (vu == w0 ? 1 : 0)) * Sh::kPart;
+                            ml[u] = get_part(p + Sh::kRows * kDim + 2 * r);
+                            ya[u] = get_part(p + r * kDim + 4 * g);
+                            yb[u] = get_part(p + r * kDim + 4 * g + 2);
+                        }
+#pragma unroll
+                        for (uint32_t u = 0; u < kAhead; ++u)
+                            if (v + u <= w1) {
+                                const float top = fmaxf(m, ml[u].x), base = top == -INFINITY ? 0.f : top * a.sl2;
+                                const float fa = __builtin_amdgcn_exp2f(m * a.sl2 - base);
+                                const float fb = __builtin_amdgcn_exp2f(ml[u].x * a.sl2 - base);
+                                m = top;
+                                ls = ls * fa + ml[u].y * fb;
+                                y = y * fa + f32x4{ya[u].x, ya[u].y, yb[u].x, yb[u].y} * fb;
+                            }
+                    }
+                    put_row(a, sp, st.kh, tile0 + r, g, y, m, ls);
+                }
+            }
         }
         __syncthreads();  // LDS is free again
+        turn ^= 1;
 
         done += u1 - u0;
         st.unit = 0;
@@ -569,43 +700,9 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
                 st.kh = 0;
                 if (done < st.left)
                     do ++st.s;
-                    while (st.s + 1 < a.sq.count && seq_span(a.sq, a.kv.shift, st.s, a.tokens).c == 0);
+                    while (st.s + 1 < a.sq.count && uniform(seq_span(a.sq, a.kv.shift, st.s, a.tokens).c) == 0);
             }
         }
-    }
-}
-
-// Adds the parts of the tiles that a cut divides, in order: workgroup (w, y)
-// has rows y kJoinRows .. of the tile whose first part is the last of range w.
-constexpr uint32_t kJoinRows = 8;
-template <typename T, uint32_t kDim, bool kSplit>
-__global__ __launch_bounds__(256) void attend_join(TileArgs a) {
-    typedef Shape<T, kDim, kSplit> Sh;
-    const uint32_t w = blockIdx.x;
-    const uint4 d = a.split[w];
-    if (d.w == 0) return;
-    const SeqSpan sp = seq_span(a.sq, a.kv.shift, d.x, a.tokens);
-    const uint32_t rows = sp.c * a.grp, row0 = d.z * Sh::kRows;
-    for (uint32_t i = threadIdx.x; i < kJoinRows * (kDim / 4); i += 256) {
-        const uint32_t r = blockIdx.y * kJoinRows + i / (kDim / 4), g = i % (kDim / 4), row = row0 + r;
-        if (row >= rows || 4 * g >= a.kv.dim) continue;
-        float m = -INFINITY, l = 0.f;
-        f32x4 y = {0.f, 0.f, 0.f, 0.f};
-        for (uint32_t k = 0; k <= d.w; ++k) {
-            const float* p = a.part + (size_t)(2 * (w + k) + (k == 0 ? 1 : 0)) * Sh::kPart;
-            const float mk = p[Sh::kRows * kDim + 2 * r], lk = p[Sh::kRows * kDim + 2 * r + 1];
-            const f32x4 yk = *(const f32x4*)(p + (size_t)r * kDim + 4 * g);
-            const float top = fmaxf(m, mk), base = top == -INFINITY ? 0.f : top * a.sl2;
-            const float fa = __builtin_amdgcn_exp2f(m * a.sl2 - base), fb = __builtin_amdgcn_exp2f(mk * a.sl2 - base);
-            m = top;
-            l = l * fa + lk * fb;
-            y = y * fa + yk * fb;
-        }
-        const uint32_t t = sp.q0 + row / a.grp, h = d.y * a.grp + row % a.grp;
-        const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-        put4(a, (size_t)t * a.out.token + (size_t)h * a.out.head + 4 * g, y * inv);
-        if (a.lse && g == 0)
-            a.lse[(size_t)t * a.heads + h] = l > 0.f ? (m * a.sl2 + log2f(l)) * kLn2 : l == 0.f ? -INFINITY : l;
     }
 }
 
@@ -696,33 +793,24 @@ __global__ __launch_bounds__(256) void weights_tile(TileArgs a, const float* __r
 constexpr uint32_t kGroups = 512;  // two workgroups a compute unit
 
 template <typename T, uint32_t kDim, bool kSplit>
-size_t part_floats() {
-    return (size_t)2 * kGroups * Shape<T, kDim, kSplit>::kPart;
-}
-
-template <typename T, uint32_t kDim, bool kSplit>
-hipError_t launch_shape(TileArgs a, void* ws, hipStream_t s) {
-    a.split = (uint4*)ws;
-    a.part = (float*)((char*)ws + kGroups * sizeof(uint4));
+hipError_t launch_shape(TileArgs a, hipStream_t s) {
+    a.whole_page = (1u << a.kv.shift) >= Shape<T, kDim, kSplit>::kKeys && a.kv.dim == kDim &&
+                   a.kv.ke < (1u << 20) && a.kv.ve < (1u << 20);
     hipLaunchKernelGGL((attend_tile<T, kDim, kSplit>), dim3(kGroups), dim3(256), 0, s, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((attend_join<T, kDim, kSplit>), dim3(kGroups, Shape<T, kDim, kSplit>::kRows / kJoinRows),
-                       dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
 template <typename T>
-hipError_t launch_type(const TileArgs& a, bool split, void* ws, hipStream_t s) {
+hipError_t launch_type(const TileArgs& a, bool split, hipStream_t s) {
     const uint32_t d = a.kv.dim;
     if (split) {
-        if (d <= 64) return launch_shape<T, 64, true>(a, ws, s);
-        if (d <= 128) return launch_shape<T, 128, true>(a, ws, s);
-        return launch_shape<T, 256, true>(a, ws, s);
+        if (d <= 64) return launch_shape<T, 64, true>(a, s);
+        if (d <= 128) return launch_shape<T, 128, true>(a, s);
+        return launch_shape<T, 256, true>(a, s);
     }
-    if (d <= 64) return launch_shape<T, 64, false>(a, ws, s);
-    if (d <= 128) return launch_shape<T, 128, false>(a, ws, s);
-    return launch_shape<T, 256, false>(a, ws, s);
+    if (d <= 64) return launch_shape<T, 64, false>(a, s);
+    if (d <= 128) return launch_shape<T, 128, false>(a, s);
+    return launch_shape<T, 256, false>(a, s);
 }
 
 inline bool in16(const void* p, size_t a, size_t b, size_t c) { return (uintptr_t)p % 16 == 0 && (a | b | c) % 8 == 0; }
@@ -733,16 +821,18 @@ bool attend_tile_fits(const Rows& q, uint32_t tokens, uint32_t heads, const KvVi
     if ((q.type != MVK_TYPE_BF16 && q.type != MVK_TYPE_F16) || kv.dim % 8 || kv.dim > 256 || tokens == 0) return false;
     if (!in16(q.p, q.token, q.head, 0) || !in16(kv.K, kv.kp, kv.kh, kv.ke) || !in16(kv.V, kv.vp, kv.vh, kv.ve))
         return false;
-    // units are counted in 32 bits (64 keys a unit at least, 32 rows a tile)
-    const uint64_t grp = heads / kv.heads, tiles = (tokens * grp) / 32 + sq.count;
-    const uint64_t units = (((uint64_t)sq.width << kv.shift) + tokens) / 64 + 1;
-    return tiles < (1ull << 31) / units / kv.heads;
+    // units (64 keys at least) of tiles (32 rows at least) are counted in 32 bits
+    const uint64_t grp = heads / kv.heads, rows = tokens * grp, seen = ((uint64_t)sq.width << kv.shift) + tokens + 256;
+    if (seen * grp + rows + 256 >= (1ull << 32)) return false;
+    return rows / 32 + sq.count < (1ull << 31) / (seen / 64 + 1) / kv.heads;
 }
 
 size_t attend_tile_bytes(const KvView& kv, bool split) {
     const uint32_t dim = kv.dim <= 64 ? 64 : kv.dim <= 128 ? 128 : 256, rows = split ? 32 : 128;
-    return kGroups * sizeof(uint4) + (size_t)2 * kGroups * (rows * dim + 2 * rows) * sizeof(float);
+    return (size_t)2 * kGroups * (rows * dim + 2 * rows) * sizeof(float);
 }
+
+size_t attend_tile_ctrl_bytes() { return (size_t)kGroups * kCounterStride * sizeof(uint32_t); }
 
 bool attend_tile_split(uint32_t max_new, uint32_t heads, const KvView& kv) {
     return (uint64_t)max_new * (heads / kv.heads) <= 32;
@@ -780,13 +870,13 @@ hipError_t launch_weights_tile(const Rows& q, uint32_t tokens, uint32_t heads, c
 
 hipError_t launch_attend_tile(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
                               float scale, const Rows& out, float inv_scale, float* lse, bool split, void* ws,
-                              hipStream_t s) {
+                              uint32_t* counters, hipStream_t s) {
     TileArgs a = tile_args(q, tokens, heads, kv, sq, scale);
     a.out = out;
-    a.inv_scale = inv_scale, a.lse = lse;
+    a.inv_scale = inv_scale, a.lse = lse, a.part = (float*)ws, a.counters = counters;
     a.wide_out = (out.type == MVK_TYPE_BF16 || out.type == MVK_TYPE_F16) && (uintptr_t)out.p % 8 == 0 &&
                  (out.token | out.head) % 4 == 0;
-    return q.type == MVK_TYPE_BF16 ? launch_type<__bf16>(a, split, ws, s) : launch_type<_Float16>(a, split, ws, s);
+    return q.type == MVK_TYPE_BF16 ? launch_type<__bf16>(a, split, s) : launch_type<_Float16>(a, split, s);
 }
 
 }  // namespace mvk

@@ -291,13 +291,15 @@ hipError_t launch_weights_any(const Rows& q, uint32_t tokens, uint32_t heads, co
                               size_t w_head, hipStream_t s);
 // attention_tile.hip: on the matrix cores where the problem fits.  split: the
 // form for few rows a sequence and kv head (max_new says how many; either form
-// is right for every problem).  ws: attend_tile_bytes, 16-byte aligned.
+// is right for every problem).  ws: attend_tile_bytes, 16-byte aligned;
+// counters: attend_tile_ctrl_bytes, zero before the launch and left at zero.
 bool attend_tile_fits(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq);
 bool attend_tile_split(uint32_t max_new, uint32_t heads, const KvView& kv);
 size_t attend_tile_bytes(const KvView& kv, bool split);
+size_t attend_tile_ctrl_bytes();
 hipError_t launch_attend_tile(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
                               float scale, const Rows& out, float inv_scale, float* lse, bool split, void* ws,
-                              hipStream_t s);
+                              uint32_t* counters, hipStream_t s);
 hipError_t launch_weights_tile(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
                                float scale, const float* lse, const float* w_in, float* w_out, size_t w_seq,
                                size_t w_head, hipStream_t s);
