@@ -273,19 +273,31 @@ struct WaveRows {
 
     __device__ __forceinline__ void scores(const u32x4* lk) {
         const uint32_t lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+        constexpr uint32_t kT = kDim / 16;
+        V8 k[kT];
+#pragma unroll
+        for (uint32_t t = 0; t < kT; ++t) k[t] = __builtin_bit_cast(V8, lk[k_at<kDim>(col, 2 * t + half)]);
 #pragma unroll
         for (uint32_t b = 0; b < kBlocks; ++b) {
             s[b] = f32x16{};
 #pragma unroll
-            for (uint32_t t = 0; t < kDim / 16; ++t) {
-                const V8 k = __builtin_bit_cast(V8, lk[k_at<kDim>(32 * b + col, 2 * t + half)]);
-                s[b] = Mma<T>::mul(k, q[t], s[b]);
+            for (uint32_t t = 0; t < kT; ++t) {
+                s[b] = Mma<T>::mul(k[t], q[t], s[b]);
+                if (b + 1 < kBlocks) k[t] = __builtin_bit_cast(V8, lk[k_at<kDim>(32 * (b + 1) + col, 2 * t + half)]);
             }
+        }
+        // reads ahead of their products
+        __builtin_amdgcn_sched_group_barrier(kDsRead, kT, 0);
+#pragma unroll
+        for (uint32_t i = 0; i < kT * kBlocks; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
         }
     }
 
-    // Scores of keys from entry j0 on into weights; the sums rescaled to the new maximum.
-    __device__ __forceinline__ void softmax(uint32_t j0, bool masked, float sl2) {
+    // Scores of keys from entry j0 on: those that the row does not see go, and the
+    // sums are scaled to a new reference where the maximum asks for it.
+    __device__ __forceinline__ void rescale(uint32_t j0, bool masked, float sl2) {
         const uint32_t half = (threadIdx.x & 63) >> 5;
         if (masked) {
 #pragma unroll
@@ -300,50 +312,79 @@ struct WaveRows {
 #pragma unroll
             for (uint32_t i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
         top = max_halves(top);
-        // nothing but -inf so far: sums stay zero instead of inf - inf
-        const float base = top == -INFINITY ? 0.f : top * sl2;
-        if (__any(top != m)) {
-            const float a = __builtin_amdgcn_exp2f(m * sl2 - base);
+        // The reference is an earlier maximum until one exceeds it by 2^8: sums and
+        // weights stay far from the types' ends, and most steps scale nothing.
+        if (__any((top - m) * sl2 > 8.f)) {
+            // nothing but -inf so far: sums stay zero instead of inf - inf
+            const float a = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * sl2);
             l *= a;
 #pragma unroll
             for (uint32_t d = 0; d < kDim / 32; ++d)
 #pragma unroll
                 for (uint32_t i = 0; i < 16; ++i) o[d][i] *= a;
+            m = top;
         }
-        m = top;
-#pragma unroll
-        for (uint32_t b = 0; b < kBlocks; ++b)
-#pragma unroll
-            for (uint32_t i = 0; i < 16; ++i) {
-                s[b][i] = __builtin_amdgcn_exp2f(s[b][i] * sl2 - base);
-                l += s[b][i];
-            }
     }
 
-    __device__ __forceinline__ void values(const u32x4* lv) {
+    // Scores into weights, and the rows' sums with V.
+    __device__ __forceinline__ void values(const u32x4* lv, float sl2) {
         const uint32_t lane = threadIdx.x & 63, half = lane >> 5;
+        const float base = m == -INFINITY ? 0.f : m * sl2;
+        // keys 16 t + 4 half + 0..3 and 16 t + 8 + 4 half + 0..3, as P has them
+        auto read = [&](uint32_t t, uint32_t d) {
+            const uint32_t r = 16 * t + 4 * half + (lane & 15) / 4;
+            const uint32_t g = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+            s16x4 v[2];
 #pragma unroll
-        for (uint32_t t = 0; t < 2 * kBlocks; ++t) {
+            for (uint32_t w = 0; w < 2; ++w) {
+                const u32x4* at = lv + v_at<kDim>(r + 8 * w, g);
+                v[w] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) s16x4*)((const s16x4*)at + (lane & 1)));
+            }
+            return __builtin_bit_cast(V8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        auto weights = [&](uint32_t t) {
             V8 p;
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) p[i] = (T)s[t / 2][8 * (t % 2) + i];
-            // keys 16 t + 4 half + 0..3 and 16 t + 8 + 4 half + 0..3, as p has them
-            const uint32_t r = 16 * t + 4 * half + (lane & 15) / 4;
-#pragma unroll
-            for (uint32_t d = 0; d < kDim / 32; ++d) {
-                const uint32_t g = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-                s16x4 v[2];
-#pragma unroll
-                for (uint32_t w = 0; w < 2; ++w) {
-                    const u32x4* at = lv + v_at<kDim>(r + 8 * w, g);
-                    v[w] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (__attribute__((address_space(3))) s16x4*)((const s16x4*)at + (lane & 1)));
-                }
-                o[d] = Mma<T>::mul(__builtin_bit_cast(V8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7)), p,
-                                   o[d]);
+            for (uint32_t i = 0; i < 8; ++i) {
+                const float x = __builtin_amdgcn_exp2f(s[t / 2][8 * (t % 2) + i] * sl2 - base);
+                l += x;
+                p[i] = (T)x;
             }
+            return p;
+        };
+        // The reads of the next 16 keys are issued before this one's products and its
+        // weights between them (the barriers keep the compiler from pulling each read
+        // down to its product, which then waits for it).
+        constexpr uint32_t kD = kDim / 32, kT = 2 * kBlocks;
+        V8 v[2][kD], p;
+#pragma unroll
+        for (uint32_t d = 0; d < kD; ++d) v[0][d] = read(0, d);
+        __builtin_amdgcn_sched_barrier(0);
+        p = weights(0);
+#pragma unroll
+        for (uint32_t t = 0; t < kT; ++t) {
+            if (t + 1 < kT) {
+#pragma unroll
+                for (uint32_t d = 0; d < kD; ++d) v[(t + 1) & 1][d] = read(t + 1, d);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            V8 pn = p;
+            if (t + 1 < kT) pn = weights(t + 1);
+#pragma unroll
+            for (uint32_t d = 0; d < kD; ++d) o[d] = Mma<T>::mul(v[t & 1][d], p, o[d]);
+            p = pn;
+            if (t + 1 < kT) {
+#pragma unroll
+                for (uint32_t d = 0; d < kD; ++d) {
+                    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(kValu, 28 / kD, 0);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
+    static constexpr int kValu = 0x2, kMfma = 0x8, kDsRead = 0x100;  // of sched_group_barrier
 };
 
 template <typename T, uint32_t kDim, bool kSplit>
@@ -548,11 +589,11 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
                     wait_reads();
                     load_k(j0 + Sh::kUnit, 0);
                 }
-                x.softmax(j0, masked, a.sl2);
+                x.rescale(j0, masked, a.sl2);
                 if (more) wait_loads<Sh::kLoads>();
                 else wait_loads<0>();
                 if (masked && __any(clean<T>(mine + Sh::kGranules, lane, 64, Sh::kGranules))) cleaned[turn] = 1;
-                x.values(mine + Sh::kGranules);
+                x.values(mine + Sh::kGranules, a.sl2);
                 wait_reads();
                 if (more) load_v(j0 + Sh::kUnit, 0);
             }
@@ -574,8 +615,8 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
                 }
                 if (!idle && j0 < lim_hi) {
                     x.scores(buf);
-                    x.softmax(j0, j0 + Sh::kKeys > lim_lo, a.sl2);
-                    x.values(buf + Sh::kGranules);
+                    x.rescale(j0, j0 + Sh::kKeys > lim_lo, a.sl2);
+                    x.values(buf + Sh::kGranules, a.sl2);
                 }
                 stage ^= 1;
             }
@@ -662,7 +703,7 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
                     if (4 * g >= dim) continue;
                     float m = -INFINITY, ls = 0.f;
                     f32x4 y = {0.f, 0.f, 0.f, 0.f};
-                    constexpr uint32_t kAhead = 4;  // parts whose loads are in flight together
+                    constexpr uint32_t kAhead = 8;  // parts whose loads are in flight together
 #pragma unroll 1
                     for (uint32_t v = w0; v <= w1; v += kAhead) {
                         float2 ml[kAhead], ya[kAhead], yb[kAhead];
