@@ -37,18 +37,19 @@ _SCALINGS = {None: _lib.MVK_SCALE_NONE, "linear": _lib.MVK_SCALE_LINEAR, "base":
 __all__ = ["FIELD", "KVCache", "Sequences", "rotary_table", "rotary", "rotary_append", "paged_attention", "cache_evict"]
 
 
-def _rows(t: torch.Tensor, name: str, T: int | None = None, heads: int | None = None, dim: int | None = None):
-    """T x heads x dim, any strides but a contiguous last axis."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA tensor")
-    if t.dtype not in _TYPES:
-        raise TypeError(f"{name} must be bfloat16, float16, float32 or int32 (field), got {t.dtype}")
-    if t.dim() != 3 or any(w is not None and g != w for g, w in zip(t.shape, (T, heads, dim))):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected (T, heads, dim) = {(T, heads, dim)}")
+def _rows(t: torch.Tensor, name: str, T: int, heads: int | None, dim: int):
+    """T x heads x dim (heads None: any), any strides but a contiguous last axis."""
+    # (plain comparisons: these checks cost as much as a launch if written with loops)
+    kind = _TYPES.get(t.dtype) if isinstance(t, torch.Tensor) and t.is_cuda else None
+    if kind is None:
+        raise TypeError(f"{name} must be a CUDA tensor of bfloat16, float16, float32 or int32 (field)")
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != T or shape[2] != dim or (heads is not None and shape[1] != heads):
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected (T, heads, dim) = {(T, heads, dim)}")
     a, b, c = t.stride()
-    if (c != 1 and t.shape[2] > 1) or a < 0 or b < 0:
+    if c != 1 and dim > 1:
         raise ValueError(f"{name}: the last axis must be contiguous")
-    return _lib.MvkRows(t.data_ptr(), _TYPES[t.dtype], a, b)
+    return _lib.MvkRows(t.data_ptr(), kind, a, b)
 
 
 @dataclass
@@ -67,16 +68,18 @@ class KVCache:
         K, V = self.K, self.V
         if not (isinstance(K, torch.Tensor) and isinstance(V, torch.Tensor) and K.is_cuda and V.is_cuda):
             raise TypeError("K and V must be CUDA tensors")
-        if K.dtype != V.dtype or K.dtype not in _TYPES or K.dtype == torch.int32:
+        kind = _TYPES.get(K.dtype, _lib.MVK_TYPE_FIELD)
+        if K.dtype != V.dtype or kind == _lib.MVK_TYPE_FIELD:
             raise TypeError(f"K and V must both be bfloat16, float16 or float32, got {K.dtype}, {V.dtype}")
-        if K.dim() != 4 or K.shape != V.shape:
-            raise ValueError(f"K and V must be pages x kv_heads x page_size x dim, got {tuple(K.shape)}, {tuple(V.shape)}")
-        ks, vs = K.stride(), V.stride()
-        if K.shape[3] > 1 and (ks[3] != 1 or vs[3] != 1):
+        shape = K.shape
+        if len(shape) != 4 or shape != V.shape:
+            raise ValueError(f"K and V must be pages x kv_heads x page_size x dim, got {tuple(shape)}, {tuple(V.shape)}")
+        n, h, p, d = shape
+        ka, kb, kc, kd = K.stride()
+        va, vb, vc, vd = V.stride()
+        if (kd != 1 or vd != 1) and d > 1:
             raise ValueError("K and V: the last axis must be contiguous")
-        n, h, p, d = K.shape
-        return _lib.MvkKv(K.data_ptr(), V.data_ptr(), _TYPES[K.dtype], n, h, p, d, ks[0], ks[1], ks[2], vs[0], vs[1],
-                          vs[2])
+        return _lib.MvkKv(K.data_ptr(), V.data_ptr(), kind, n, h, p, d, ka, kb, kc, va, vb, vc)
 
 
 @dataclass
@@ -91,13 +94,15 @@ class Sequences:
     max_new: int | None = None
 
     def struct(self, rows: int):
-        count, width = self.table.shape
-        if not self.table.is_cuda or self.table.dtype != torch.int32 or (width > 1 and self.table.stride(1) != 1):
+        table, starts = self.table, self.q_start
+        count, width = table.shape
+        stride, one = table.stride()
+        if not table.is_cuda or table.dtype != torch.int32 or (one != 1 and width > 1):
             raise ValueError("table must be a CUDA int32 tensor with contiguous rows")
         lens = _dev(self.lens, torch.int32, (count,), "lens")
-        starts = _dev(self.q_start, torch.int32, (count + 1,), "q_start") if self.q_start is not None else None
-        most = rows if self.max_new is None else min(rows, int(self.max_new))
-        return _lib.MvkSeqs(self.table.data_ptr(), self.table.stride(0), count, width, lens, starts, most)
+        starts = _dev(starts, torch.int32, (count + 1,), "q_start") if starts is not None else None
+        most = rows if self.max_new is None or self.max_new > rows else int(self.max_new)
+        return _lib.MvkSeqs(table.data_ptr(), stride, count, width, lens, starts, most)
 
 
 def rotary_table(rot: int, rows: int, base: float = 10000.0, scaling: str | None = None, factor: float = 1.0,
@@ -119,25 +124,27 @@ def rotary_table(rot: int, rows: int, base: float = 10000.0, scaling: str | None
 def _rotary_call(q, k, v, positions, table, cache, seqs, layout, field_scale, out, p, stream):
     if layout not in _LAYOUTS:
         raise ValueError(f"layout must be one of {sorted(_LAYOUTS)}")
-    T, _, dim = (q if q is not None else k).shape
+    x = q if q is not None else k
+    T, _, dim = x.shape
     ref = ctypes.byref
     qs = ks = vs = os_ = cs = ss = None
     heads = 0
     if q is not None:
         heads = q.shape[1]
-        qs, os_ = _rows(q, "q"), _rows(out, "out", T, heads, dim)
+        qs, os_ = ref(_rows(q, "q", T, heads, dim)), ref(_rows(out, "out", T, heads, dim))
     if k is not None:
-        cs, ss = cache.struct(), seqs.struct(T)
-        ks, vs = _rows(k, "k", T, cs.kv_heads, cs.dim), _rows(v, "v", T, cs.kv_heads, cs.dim)
-    if (q if q is not None else k).dtype == torch.int32 and field_scale is None:
-        raise ValueError("field inputs need field_scale, the value of 1")
-    if table.dim() != 2:
-        raise ValueError("table must be rows x rot")
+        kv = cache.struct()
+        heads_kv, dim_kv = kv.kv_heads, kv.dim
+        ks, vs = ref(_rows(k, "k", T, heads_kv, dim_kv)), ref(_rows(v, "v", T, heads_kv, dim_kv))
+        cs, ss = ref(kv), ref(seqs.struct(T))
+    if field_scale is None:
+        if x.dtype == torch.int32:
+            raise ValueError("field inputs need field_scale, the value of 1")
+        field_scale = 0.0
+    rows, rot = table.shape
     _lib.check("mvk_rotary_append", _lib.load(p).mvk_rotary_append(
-        ref(qs) if qs else None, ref(ks) if ks else None, ref(vs) if vs else None, T, heads, dim, table.shape[1],
-        _LAYOUTS[layout], _dev(positions, torch.int32, (T,), "positions"), _dev(table, torch.float32, None, "table"),
-        table.shape[0], field_scale or 0.0, ref(os_) if os_ else None, ref(cs) if cs else None,
-        ref(ss) if ss else None, _stream(stream)))
+        qs, ks, vs, T, heads, dim, rot, _LAYOUTS[layout], _dev(positions, torch.int32, (T,), "positions"),
+        _dev(table, torch.float32, None, "table"), rows, field_scale, os_, cs, ss, _stream(stream)))
 
 
 def rotary(q: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, layout: str = "half",

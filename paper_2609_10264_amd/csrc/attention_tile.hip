@@ -86,25 +86,27 @@ __device__ __forceinline__ uint32_t floor_sum(uint32_t n, uint32_t m, uint32_t a
     }
 }
 
-// The tiles of one sequence (the same for each of its kv heads).
-template <uint32_t kRows, uint32_t kUnit>
+// The tiles of one sequence (the same for each of its kv heads).  A tile has a
+// unit for every kUnit keys and, before them, kExtra units without keys: what
+// its beginning and end cost besides.
+template <uint32_t kRows, uint32_t kUnit, uint32_t kExtra>
 struct Tiles {
     uint32_t c, n, base, count, last;  // base: entries before the new tokens; last: units of the last tile
     uint32_t grp;
     __device__ Tiles(const SeqSpan& sp, uint32_t grp) : c(sp.c), n(sp.n), grp(grp) {
         base = n > c ? n - c : 0;
         count = (c * grp + kRows - 1) / kRows;
-        last = (base + c + kUnit - 1) / kUnit;
+        last = (base + c + kUnit - 1) / kUnit + kExtra;
     }
     // units of tile t: its last row is a row of token ((t + 1) kRows - 1) / grp
     __device__ uint32_t units(uint32_t t) const {
         if (t + 1 >= count) return last;
-        return (base + ((t + 1) * kRows - 1) / grp + kUnit) / kUnit;
+        return (base + ((t + 1) * kRows - 1) / grp + kUnit) / kUnit + kExtra;
     }
     // units of the tiles before t (t < count)
     __device__ uint32_t before(uint32_t t) const {
         if (t == 0) return 0;
-        return floor_sum(t, grp * kUnit, kRows, grp * (base + kUnit) + kRows - 1);
+        return floor_sum(t, grp * kUnit, kRows, grp * (base + kUnit) + kRows - 1) + t * kExtra;
     }
     __device__ uint32_t all() const { return count == 0 ? 0 : before(count - 1) + last; }
 };
@@ -121,7 +123,7 @@ struct TileArgs {
     float* part;    // 2 parts a workgroup: kRows x kDim sums, then kRows (maximum, sum)
     uint32_t* counters;  // one a workgroup, kCounterStride words apart: zero before and after
     bool whole_page;     // a tile of keys lies in one page, its offsets in 32 bits, and dim is kDim
-    bool wide_out;  // out takes 8-byte stores of 4 16-bit values
+    bool wide_out;  // out takes stores of 4 values at once
 };
 
 __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
@@ -155,7 +157,7 @@ __device__ __forceinline__ uint32_t range_of(uint32_t x, uint32_t total, uint32_
 }
 
 // Every wave by itself: the units of all sequences, and where range w begins.
-template <uint32_t kRows, uint32_t kUnit>
+template <uint32_t kRows, uint32_t kUnit, uint32_t kExtra>
 __device__ __forceinline__ Start find_start(const TileArgs& a, uint32_t w, uint32_t groups) {
     const uint32_t lane = threadIdx.x & 63, hk = a.kv.heads, chunks = (a.sq.count + 63) / 64;
     Start st = {};
@@ -166,7 +168,7 @@ __device__ __forceinline__ Start find_start(const TileArgs& a, uint32_t w, uint3
         const uint32_t s0 = 64 * (it < chunks ? it : it - chunks), s = s0 + lane;
         if (chunks > 1 || it == 0) {
             u = 0;
-            if (s < a.sq.count) u = Tiles<kRows, kUnit>(seq_span(a.sq, a.kv.shift, s, a.tokens), a.grp).all() * hk;
+            if (s < a.sq.count) u = Tiles<kRows, kUnit, kExtra>(seq_span(a.sq, a.kv.shift, s, a.tokens), a.grp).all() * hk;
             incl = wave_scan(u);
         }
         const uint32_t sum = (uint32_t)__shfl((int)incl, 63);
@@ -186,7 +188,7 @@ __device__ __forceinline__ Start find_start(const TileArgs& a, uint32_t w, uint3
             const uint32_t per = us / hk, in = x - before;
             st.kh = in / per;
             st.unit = in % per;
-            const Tiles<kRows, kUnit> t(seq_span(a.sq, a.kv.shift, st.s, a.tokens), a.grp);
+            const Tiles<kRows, kUnit, kExtra> t(seq_span(a.sq, a.kv.shift, st.s, a.tokens), a.grp);
             // the last tile whose units begin at or before that: 64 candidates at a time
             uint32_t lo = 0, hi = t.count, first = 0;
 #pragma unroll 1
@@ -210,7 +212,7 @@ __device__ __forceinline__ Start find_start(const TileArgs& a, uint32_t w, uint3
 
 // Granules (8 values) of a row in LDS, permuted so that the reads below meet
 // every bank once: K is read granule by granule down the rows, V in blocks of 4
-// rows by 2 granules.
+// rows by 4 granules.
 template <uint32_t kDim>
 __device__ __forceinline__ uint32_t k_at(uint32_t row, uint32_t g) {
     constexpr uint32_t G = kDim / 8;
@@ -219,7 +221,7 @@ __device__ __forceinline__ uint32_t k_at(uint32_t row, uint32_t g) {
 template <uint32_t kDim>
 __device__ __forceinline__ uint32_t v_at(uint32_t row, uint32_t g) {
     constexpr uint32_t G = kDim / 8;
-    return row * G + (g ^ (G < 16 ? ((row >> 1) & 3) * 2 : (row & 7) * 2));
+    return row * G + (g ^ (G < 16 ? (row >> 1 & 1) * 4 : (row & 3) * 4));
 }
 
 __device__ __forceinline__ float max_halves(float x) {
@@ -261,57 +263,72 @@ __device__ __forceinline__ bool clean(u32x4* lv, uint32_t first, uint32_t step, 
 }
 
 // The state of a wave's 32 rows: lane l has row l % 32 (l / 32: which half of
-// the keys of a block, and of the dims of a product, it holds).
-template <typename T, uint32_t kDim, uint32_t kBlocks>
+// the keys of a block, and of the dims of a product, it holds).  A block is 32 keys.
+template <typename T, uint32_t kDim>
 struct WaveRows {
     typedef typename Mma<T>::V8 V8;
-    V8 q[kDim / 16];
-    f32x16 o[kDim / 32];  // O^T: register i of tile d: dim 32 d + 8 (i / 4) + 4 (l / 32) + i % 4
-    f32x16 s[kBlocks];    // S^T, then P^T: register i of block b: key 32 b + 8 (i / 4) + 4 (l / 32) + i % 4
-    float m, l;           // maximum of q . k so far; this lane's part of the sum
-    uint32_t lim;         // entries that the row sees
+    static constexpr uint32_t kT = kDim / 16, kD = kDim / 32;
+    static constexpr int kValu = 0x2, kMfma = 0x8, kDsRead = 0x100;  // of sched_group_barrier
+    V8 q[kT];
+    f32x16 o[kD];  // O^T: register i of tile d: dim 32 d + 8 (i / 4) + 4 (l / 32) + i % 4
+    float m, l;    // reference of the exponents (a maximum of q . k so far); this lane's part of the sum
+    uint32_t lim;  // entries that the row sees
 
-    __device__ __forceinline__ void scores(const u32x4* lk) {
-        const uint32_t lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
-        constexpr uint32_t kT = kDim / 16;
-        V8 k[kT];
+    // Operands from LDS: 16 dims of K's rows, and 16 keys by 32 dims of V, transposed:
+    // keys 16 t + 4 half + 0..3 and 16 t + 8 + 4 half + 0..3, the order that P has.
+    // The first addresses of this lane in a tile of K and one of V, in bytes; the
+    // order of the granules makes the others exclusive-ors of them.
+    uint32_t ka, va;
+    __device__ __forceinline__ void places(uint32_t k, uint32_t v) {
+        const uint32_t lane = threadIdx.x & 63, half = lane >> 5;
+        ka = k + 16 * k_at<kDim>(lane & 31, half);
+        va = v + 16 * v_at<kDim>(4 * half + (lane & 15) / 4, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
+    }
+    __device__ __forceinline__ V8 read_k(uint32_t at, uint32_t t) const {
+        return __builtin_bit_cast(V8, *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)((ka ^ (32 * t)) + at));
+    }
+    __device__ __forceinline__ V8 read_v(uint32_t at, uint32_t t, uint32_t d) const {
+        // (8 rows on, the granules' order is the same: see v_at)
+        s16x4 v[2];
 #pragma unroll
-        for (uint32_t t = 0; t < kT; ++t) k[t] = __builtin_bit_cast(V8, lk[k_at<kDim>(col, 2 * t + half)]);
-#pragma unroll
-        for (uint32_t b = 0; b < kBlocks; ++b) {
-            s[b] = f32x16{};
-#pragma unroll
-            for (uint32_t t = 0; t < kT; ++t) {
-                s[b] = Mma<T>::mul(k[t], q[t], s[b]);
-                if (b + 1 < kBlocks) k[t] = __builtin_bit_cast(V8, lk[k_at<kDim>(32 * (b + 1) + col, 2 * t + half)]);
-            }
-        }
-        // reads ahead of their products
-        __builtin_amdgcn_sched_group_barrier(kDsRead, kT, 0);
-#pragma unroll
-        for (uint32_t i = 0; i < kT * kBlocks; ++i) {
-            __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
-        }
+        for (uint32_t w = 0; w < 2; ++w)
+            v[w] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4*)(uintptr_t)((va ^ (64 * d)) + at + (16 * t + 8 * w) * 2 * kDim));
+        return __builtin_bit_cast(V8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
     }
 
-    // Scores of keys from entry j0 on: those that the row does not see go, and the
-    // sums are scaled to a new reference where the maximum asks for it.
-    __device__ __forceinline__ void rescale(uint32_t j0, bool masked, float sl2) {
+    __device__ __forceinline__ void read_k(V8 (&k)[kT], uint32_t at) const {
+#pragma unroll
+        for (uint32_t t = 0; t < kT; ++t) k[t] = read_k(at, t);
+        __builtin_amdgcn_sched_barrier(0);  // (else each read is pulled down to its product, which then waits for it)
+    }
+    // S^T of a block: register i: key 8 (i / 4) + 4 (l / 32) + i % 4.
+    __device__ __forceinline__ f32x16 scores(const V8 (&k)[kT]) const {
+        f32x16 s = {};
+#pragma unroll
+        for (uint32_t t = 0; t < kT; ++t) s = Mma<T>::mul(k[t], q[t], s);
+        return s;
+    }
+
+    // The largest of a block's scores and m (this half's).
+    __device__ __forceinline__ float largest(const f32x16& s) const {
+        float x = m;
+#pragma unroll
+        for (uint32_t i = 0; i < 16; ++i) x = fmaxf(x, s[i]);
+        return x;
+    }
+
+    // Before the step of a block from entry j0 on: the scores that the row does not see
+    // go, and the sums are scaled to a new reference where the largest score asks for it.
+    __device__ __forceinline__ void rescale(f32x16& s, float most, uint32_t j0, bool masked, float sl2) {
         const uint32_t half = (threadIdx.x & 63) >> 5;
         if (masked) {
 #pragma unroll
-            for (uint32_t b = 0; b < kBlocks; ++b)
-#pragma unroll
-                for (uint32_t i = 0; i < 16; ++i)
-                    if (j0 + 32 * b + 8 * (i / 4) + 4 * half + i % 4 >= lim) s[b][i] = -INFINITY;
+            for (uint32_t i = 0; i < 16; ++i)
+                if (j0 + 8 * (i / 4) + 4 * half + i % 4 >= lim) s[i] = -INFINITY;
+            most = largest(s);
         }
-        float top = m;
-#pragma unroll
-        for (uint32_t b = 0; b < kBlocks; ++b)
-#pragma unroll
-            for (uint32_t i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        top = max_halves(top);
+        const float top = max_halves(most);
         // The reference is an earlier maximum until one exceeds it by 2^8: sums and
         // weights stay far from the types' ends, and most steps scale nothing.
         if (__any((top - m) * sl2 > 8.f)) {
@@ -319,80 +336,76 @@ struct WaveRows {
             const float a = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * sl2);
             l *= a;
 #pragma unroll
-            for (uint32_t d = 0; d < kDim / 32; ++d)
+            for (uint32_t d = 0; d < kD; ++d)
 #pragma unroll
                 for (uint32_t i = 0; i < 16; ++i) o[d][i] *= a;
             m = top;
         }
     }
 
-    // Scores into weights, and the rows' sums with V.
-    __device__ __forceinline__ void values(const u32x4* lv, float sl2) {
-        const uint32_t lane = threadIdx.x & 63, half = lane >> 5;
-        const float base = m == -INFINITY ? 0.f : m * sl2;
-        // keys 16 t + 4 half + 0..3 and 16 t + 8 + 4 half + 0..3, as P has them
-        auto read = [&](uint32_t t, uint32_t d) {
-            const uint32_t r = 16 * t + 4 * half + (lane & 15) / 4;
-            const uint32_t g = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-            s16x4 v[2];
+    // Weights of keys 16 t .. of a block, in the cache's type, and their sum.
+    __device__ __forceinline__ V8 weights(const f32x16& s, uint32_t t, float sl2, float base) {
+        V8 p;
 #pragma unroll
-            for (uint32_t w = 0; w < 2; ++w) {
-                const u32x4* at = lv + v_at<kDim>(r + 8 * w, g);
-                v[w] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4*)((const s16x4*)at + (lane & 1)));
-            }
-            return __builtin_bit_cast(V8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
-        };
-        auto weights = [&](uint32_t t) {
-            V8 p;
-#pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) {
-                const float x = __builtin_amdgcn_exp2f(s[t / 2][8 * (t % 2) + i] * sl2 - base);
-                l += x;
-                p[i] = (T)x;
-            }
-            return p;
-        };
-        // The reads of the next 16 keys are issued before this one's products and its
-        // weights between them (the barriers keep the compiler from pulling each read
-        // down to its product, which then waits for it).
-        constexpr uint32_t kD = kDim / 32, kT = 2 * kBlocks;
-        V8 v[2][kD], p;
-#pragma unroll
-        for (uint32_t d = 0; d < kD; ++d) v[0][d] = read(0, d);
-        __builtin_amdgcn_sched_barrier(0);
-        p = weights(0);
-#pragma unroll
-        for (uint32_t t = 0; t < kT; ++t) {
-            if (t + 1 < kT) {
-#pragma unroll
-                for (uint32_t d = 0; d < kD; ++d) v[(t + 1) & 1][d] = read(t + 1, d);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            V8 pn = p;
-            if (t + 1 < kT) pn = weights(t + 1);
-#pragma unroll
-            for (uint32_t d = 0; d < kD; ++d) o[d] = Mma<T>::mul(v[t & 1][d], p, o[d]);
-            p = pn;
-            if (t + 1 < kT) {
-#pragma unroll
-                for (uint32_t d = 0; d < kD; ++d) {
-                    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(kValu, 28 / kD, 0);
-                }
-            }
-            __builtin_amdgcn_sched_barrier(0);
+        for (uint32_t i = 0; i < 8; ++i) {
+            const float x = __builtin_amdgcn_exp2f(s[8 * t + i] * sl2 - base);
+            l += x;
+            p[i] = (T)x;
         }
+        return p;
     }
-    static constexpr int kValu = 0x2, kMfma = 0x8, kDsRead = 0x100;  // of sched_group_barrier
+
+    // The block's weights and its sums with V (kV: its place in the tile).  With kNext
+    // also the scores of the next block from its operands k, whose products run while
+    // the weights are computed, and then the operands of the block after that (`at`:
+    // their place from ka on), whose reads run behind the products with V, as does the
+    // search for the next scores' largest.
+    template <bool kNext, uint32_t kV>
+    __device__ __forceinline__ f32x16 step(const f32x16& s, V8 (&k)[kT], uint32_t at, float sl2, float& most) {
+        const float base = m == -INFINITY ? 0.f : m * sl2;
+        V8 p[2], v[2][kD];
+        f32x16 next = {};
+#pragma unroll
+        for (uint32_t d = 0; d < kD; ++d) v[0][d] = read_v(kV, 0, d);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (uint32_t t = 0; t < 2; ++t) p[t] = weights(s, t, sl2, base);
+        if (kNext) {
+            next = scores(k);
+#pragma unroll
+            for (uint32_t t = 0; t < kT; ++t) {
+                __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kValu, 56 / kT, 0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (uint32_t d = 0; d < kD; ++d) v[1][d] = read_v(kV, 1, d);
+        __builtin_amdgcn_sched_barrier(0);
+        if (kNext) read_k(k, at);
+#pragma unroll
+        for (uint32_t t = 0; t < 2; ++t)
+#pragma unroll
+            for (uint32_t d = 0; d < kD; ++d) o[d] = Mma<T>::mul(v[t][d], p[t], o[d]);
+        if (kNext) {
+            most = largest(next);
+#pragma unroll
+            for (uint32_t i = 0; i < 2 * kD; ++i) {
+                __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kValu, 2, 0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        return next;
+    }
 };
 
 template <typename T, uint32_t kDim, bool kSplit>
 struct Shape {
     static constexpr uint32_t kRows = kSplit ? 32 : 128;
-    static constexpr uint32_t kBlocks = kSplit || kDim > 128 ? 1 : 2;  // 32-key blocks of an LDS tile
-    static constexpr uint32_t kKeys = 32 * kBlocks;
+    static constexpr uint32_t kKeys = kSplit ? 32 : 64;              // of an LDS tile
     static constexpr uint32_t kUnit = kSplit ? 4 * kKeys : kKeys;    // keys of one unit
+    static constexpr uint32_t kExtra = kSplit ? 0 : 3;
     static constexpr uint32_t kGranules = kKeys * (kDim / 8);        // of K, and of V
     static constexpr uint32_t kLoads = kGranules / 64 / (kSplit ? 1 : 4);  // of K, and of V, a wave
     // a tile a wave, or two; the waves' results take their place
@@ -410,18 +423,22 @@ __device__ const u32x4 kZeroGranule = {0, 0, 0, 0};
 // wait_loads comes before their data is read.  (m0 is written and used inside
 // the statement; nothing else in this file uses it.)
 __device__ __forceinline__ void load_lds(const void* from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(uniform(to)) : "memory");
 }
 __device__ __forceinline__ void load_lds(const void* base, uint32_t offset, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to)
+    const uint64_t b = (uint64_t)base, s = (uint64_t)uniform((uint32_t)(b >> 32)) << 32 | uniform((uint32_t)b);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(s), "s"(uniform(to))
                  : "memory");
 }
-// All but the kNewest last loads of this wave have landed.
+// All but the kNewest last loads of this wave have landed.  (The builtin, unlike
+// assembly, tells the compiler that its own loads have: it would wait for them
+// again inside the loops, and with them for the loads in flight.)
 template <uint32_t kNewest>
 __device__ __forceinline__ void wait_loads() {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kNewest) : "memory");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((kNewest & 15) | 7 << 4 | 15 << 8 | (kNewest >> 4) << 14);
+    asm volatile("" ::: "memory");
 }
-
 // The LDS reads of this wave are done: their place may be filled again.
 __device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
@@ -438,30 +455,71 @@ __device__ __forceinline__ float2 get_part(const float* p) {
 
 // Four consecutive values of a row of the output.
 __device__ __forceinline__ void put4(const TileArgs& a, size_t at, f32x4 x) {
-    if (a.wide_out) {
-        typedef __bf16 B4 __attribute__((ext_vector_type(4)));
-        typedef _Float16 H4 __attribute__((ext_vector_type(4)));
-        u32x2 v;
-        if (a.out.type == MVK_TYPE_BF16) v = __builtin_bit_cast(u32x2, __builtin_convertvector(x, B4));
-        else v = __builtin_bit_cast(u32x2, __builtin_convertvector(x, H4));
-        *(u32x2*)((uint16_t*)a.out.p + at) = v;
-        return;
-    }
+    typedef __bf16 B4 __attribute__((ext_vector_type(4)));
+    typedef _Float16 H4 __attribute__((ext_vector_type(4)));
+    if (!a.wide_out) {
 #pragma unroll 1
-    for (int i = 0; i < 4; ++i) {
-        const float y = i == 0 ? x[0] : i == 1 ? x[1] : i == 2 ? x[2] : x[3];
-        store_as(a.out.p, a.out.type, at + i, y, a.inv_scale);
+        for (int i = 0; i < 4; ++i) {
+            const float y = i == 0 ? x[0] : i == 1 ? x[1] : i == 2 ? x[2] : x[3];
+            store_as(a.out.p, a.out.type, at + i, y, a.inv_scale);
+        }
+    } else if (a.out.type == MVK_TYPE_BF16) {
+        *(u32x2*)((uint16_t*)a.out.p + at) = __builtin_bit_cast(u32x2, __builtin_convertvector(x, B4));
+    } else if (a.out.type == MVK_TYPE_F16) {
+        *(u32x2*)((uint16_t*)a.out.p + at) = __builtin_bit_cast(u32x2, __builtin_convertvector(x, H4));
+    } else if (a.out.type == MVK_TYPE_F32) {
+        *(f32x4*)((float*)a.out.p + at) = x;
+    } else {
+        *(u32x4*)((uint32_t*)a.out.p + at) = u32x4{field_of(x[0] * a.inv_scale), field_of(x[1] * a.inv_scale),
+                                                   field_of(x[2] * a.inv_scale), field_of(x[3] * a.inv_scale)};
     }
+}
+
+// A lane's part of its row, dims 8 i .. 8 i + 3 from `at` on (aligned outputs); one
+// loop a type, so that the type is not asked for at every store.
+template <uint32_t kDim>
+__device__ __forceinline__ void put_rows(const TileArgs& a, size_t at, const f32x16* o, float f) {
+    typedef __bf16 B4 __attribute__((ext_vector_type(4)));
+    typedef _Float16 H4 __attribute__((ext_vector_type(4)));
+    const uint32_t live = a.kv.dim / 8;
+    auto value = [&](uint32_t i) {
+        const f32x16& x = o[i / 4];
+        return f32x4{x[4 * (i % 4)], x[4 * (i % 4) + 1], x[4 * (i % 4) + 2], x[4 * (i % 4) + 3]} * f;
+    };
+    if (a.out.type == MVK_TYPE_BF16) {
+#pragma unroll
+        for (uint32_t i = 0; i < kDim / 8; ++i)
+            if (i < live) *(u32x2*)((uint16_t*)a.out.p + at + 8 * i) = __builtin_bit_cast(u32x2, __builtin_convertvector(value(i), B4));
+    } else if (a.out.type == MVK_TYPE_F16) {
+#pragma unroll
+        for (uint32_t i = 0; i < kDim / 8; ++i)
+            if (i < live) *(u32x2*)((uint16_t*)a.out.p + at + 8 * i) = __builtin_bit_cast(u32x2, __builtin_convertvector(value(i), H4));
+    } else {
+        const bool field = a.out.type == MVK_TYPE_FIELD;
+#pragma unroll
+        for (uint32_t i = 0; i < kDim / 8; ++i)
+            if (i < live) {
+                f32x4 x = value(i);
+                if (field) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[k] = __uint_as_float(field_of(x[k] * a.inv_scale));
+                }
+                *(f32x4*)((float*)a.out.p + at + 8 * i) = x;
+            }
+    }
+}
+
+__device__ __forceinline__ void put_lse(const TileArgs& a, size_t at, float m, float l) {
+    a.lse[at] = l > 0.f ? (m * a.sl2 + __builtin_log2f(l)) * kLn2 : l == 0.f ? -INFINITY : l;
 }
 
 // Four values y (not yet divided by the sum l) of row `row` of (sequence, kv head), dims 4 g and on.
 __device__ __forceinline__ void put_row(const TileArgs& a, const SeqSpan& sp, uint32_t kh, uint32_t row, uint32_t g,
                                         f32x4 y, float m, float l) {
     const uint32_t t = sp.q0 + row / a.grp, h = kh * a.grp + row % a.grp;
-    // (a sum that is not a number stays one; a row without entries is zero)
-    const float inv = l > 0.f ? 1.f / l : l;
-    put4(a, (size_t)t * a.out.token + (size_t)h * a.out.head + 4 * g, l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : y * inv);
-    if (a.lse && g == 0) a.lse[(size_t)t * a.heads + h] = l > 0.f ? (m * a.sl2 + log2f(l)) * kLn2 : l == 0.f ? -INFINITY : l;
+    // (a sum that is not a number stays one; a row without entries is zero, its sums are)
+    put4(a, (size_t)t * a.out.token + (size_t)h * a.out.head + 4 * g, y * (l > 0.f ? 1.f / l : l));
+    if (a.lse && g == 0) put_lse(a, (size_t)t * a.heads + h, m, l);
 }
 
 constexpr uint32_t kCounterStride = 16;
@@ -471,7 +529,7 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
     typedef Shape<T, kDim, kSplit> Sh;
     typedef typename Mma<T>::V8 V8;
     constexpr uint32_t G = kDim / 8;  // granules a row
-    __shared__ u32x4 lds[Sh::kLds];
+    __shared__ __attribute__((aligned(65536))) u32x4 lds[Sh::kLds];  // (at 0: see kTile)
     __shared__ float red[4][32][2];
     __shared__ uint32_t last_one, cleaned[2];  // (cleaned: of this segment and the next)
     const uint32_t tid = threadIdx.x, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6)), lane = tid & 63;
@@ -480,28 +538,34 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
     // consecutive ranges on one XCD, whose L2 then holds the keys they share
     const uint32_t groups = gridDim.x, xcds = groups % 8 == 0 ? 8 : 1;
     const uint32_t w = (blockIdx.x % xcds) * (groups / xcds) + blockIdx.x / xcds;
-    Start st = find_start<Sh::kRows, Sh::kUnit>(a, w, groups);
+    Start st = find_start<Sh::kRows, Sh::kUnit, Sh::kExtra>(a, w, groups);
     st = {uniform(st.s), uniform(st.kh), uniform(st.tile), uniform(st.unit), uniform(st.left), uniform(st.total)};
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
     u32x4* const mine = kSplit ? lds + wave * 2 * Sh::kGranules : lds;
     // load i of this wave fills 64 granules from granule 64 (i + kLoads wave) of the tile on
     const uint32_t part0 = kSplit ? 0 : 64 * Sh::kLoads * wave;
 
-    if (tid == 0) cleaned[0] = 0;
+    if (tid < 2) cleaned[tid] = 0;
     __syncthreads();
     uint32_t done = 0, turn = 0;
+    SeqSpan sp = {};
+    uint32_t ids = 0, id0 = 0, id1 = 0;  // lane i: the page of the sequence's pages id0 + i, of id0 .. id1 - 1
+    auto sequence = [&]() {
+        const SeqSpan x = seq_span(a.sq, a.kv.shift, st.s, a.tokens);
+        sp = {uniform(x.q0), uniform(x.c), uniform(x.n)};
+        id0 = id1 = 0;
+    };
+    if (st.left) sequence();
 #pragma unroll 1
     while (done < st.left) {
-        SeqSpan sp = seq_span(a.sq, a.kv.shift, st.s, a.tokens);
-        sp = {uniform(sp.q0), uniform(sp.c), uniform(sp.n)};
-        const Tiles<Sh::kRows, Sh::kUnit> tiles(sp, a.grp);
+        const Tiles<Sh::kRows, Sh::kUnit, Sh::kExtra> tiles(sp, a.grp);
         const uint32_t units = tiles.units(st.tile);
         const uint32_t u0 = st.unit, u1 = min(units, u0 + (st.left - done));
 
         // rows
         const uint32_t rows = sp.c * a.grp, tile0 = st.tile * Sh::kRows, row0 = tile0 + (kSplit ? 0 : 32 * wave);
         const uint32_t known = min(row0 + col, rows - 1);
-        WaveRows<T, kDim, Sh::kBlocks> x;
+        WaveRows<T, kDim> x;
         {
             const uint32_t tok = known / a.grp, head = st.kh * a.grp + known % a.grp;
             const int64_t see = (int64_t)sp.n - sp.c + tok + 1;
@@ -530,13 +594,13 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
         const char* const kb = (const char*)((const T*)a.kv.K + (size_t)st.kh * a.kv.kh);
         const char* const vb = (const char*)((const T*)a.kv.V + (size_t)st.kh * a.kv.vh);
         const uint32_t mask = (1u << a.kv.shift) - 1;
-        const uint32_t first = u0 * Sh::kUnit + (kSplit ? wave * Sh::kKeys : 0);
-        const uint32_t stop = min(u1 * Sh::kUnit, sp.n);  // entries at and beyond it are not needed
-        uint32_t ids = 0, id0 = 0, id1 = 0;  // lane i: the page of the sequence's pages id0 + i, of id0 .. id1 - 1
+        const uint32_t key0 = (max(u0, Sh::kExtra) - Sh::kExtra) * Sh::kUnit, key1 = (max(u1, Sh::kExtra) - Sh::kExtra) * Sh::kUnit;
+        const uint32_t first = key0 + (kSplit ? wave * Sh::kKeys : 0);
+        const uint32_t stop = min(key1, sp.n);  // entries at and beyond it are not needed
         // before the loads of the tile at j0: its pages are known (places beyond the
         // last page in use are read in that page, so no address leaves the pool)
         auto pages = [&](uint32_t j0) {
-            if ((min(j0 + Sh::kKeys, sp.n) - 1) >> a.kv.shift >= id1) {
+            if ((min(j0 + Sh::kKeys, sp.n) - 1) >> a.kv.shift >= id1 || j0 >> a.kv.shift < id0) {
                 id0 = j0 >> a.kv.shift;
                 id1 = id0 + 64;
                 ids = seq_page(a.sq, a.kv, st.s, min((id0 + lane) << a.kv.shift, sp.n - 1));
@@ -573,120 +637,128 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
         auto load_v = [&](uint32_t j0, uint32_t stage) {
             load(vb, a.kv.vp, a.kv.ve, true, j0, lds0 + 16 * ((kSplit ? wave : stage) * 2 * Sh::kGranules + Sh::kGranules + part0));
         };
-        if (first < stop) {
-            pages(first);
-            load_k(first, 0);
-            load_v(first, 0);
-        }
+        x.places(lds0 + (kSplit ? wave * 32 * Sh::kGranules : 0), lds0 + (kSplit ? wave * 32 * Sh::kGranules : 0) + 16 * Sh::kGranules);
         if (kSplit) {
+            if (first < stop) {
+                pages(first);
+                load_k(first, 0);
+                load_v(first, 0);
+            }
 #pragma unroll 1
             for (uint32_t j0 = first; j0 < stop; j0 += Sh::kUnit) {
                 const bool more = j0 + Sh::kUnit < stop, masked = j0 + Sh::kKeys > lim_lo;
                 wait_loads<Sh::kLoads>();  // K
-                x.scores(mine);
+                V8 k[kDim / 16];
+                x.read_k(k, 0);
+                f32x16 s = x.scores(k);
                 if (more) {
                     pages(j0 + Sh::kUnit);
                     wait_reads();
                     load_k(j0 + Sh::kUnit, 0);
                 }
-                x.rescale(j0, masked, a.sl2);
+                float most = x.largest(s);
+                x.rescale(s, most, j0, masked, a.sl2);
                 if (more) wait_loads<Sh::kLoads>();
                 else wait_loads<0>();
                 if (masked && __any(clean<T>(mine + Sh::kGranules, lane, 64, Sh::kGranules))) cleaned[turn] = 1;
-                x.values(mine + Sh::kGranules, a.sl2);
+                x.template step<false, 0>(s, k, 0, a.sl2, most);
                 wait_reads();
                 if (more) load_v(j0 + Sh::kUnit, 0);
             }
-        } else {
+        } else if (first < stop) {
+            // Two blocks a tile.  The scores of a block are formed during the step before
+            // it, from operands read during the step before that; so when a tile's steps
+            // begin, its K has been read, and the next tile's K and its V are there.
+            const uint32_t end = idle ? 0 : min(stop, lim_hi);  // blocks from here on say nothing to this wave
+            constexpr uint32_t kTile = 32 * Sh::kGranules, kBlock = 8 * Sh::kGranules;  // bytes
+            static_assert((kTile & (kTile - 1)) == 0, "one bit tells the tiles apart");
             uint32_t stage = 0;
+            pages(first);
+            load_k(first, 0);
+            load_v(first, 0);
+            if (first + Sh::kUnit < stop) {
+                pages(first + Sh::kUnit);
+                load_k(first + Sh::kUnit, 1);
+                wait_loads<2 * Sh::kLoads>();
+            } else {
+                wait_loads<Sh::kLoads>();
+            }
+            __syncthreads();
+            f32x16 s0 = {}, s1 = {};
+            V8 k[kDim / 16];
+            x.read_k(k, 0);
+            float most = 0.f;
+            if (first < end) {
+                s0 = x.scores(k);
+                most = x.largest(s0);
+            }
+            x.read_k(k, kBlock);
 #pragma unroll 1
             for (uint32_t j0 = first; j0 < stop; j0 += Sh::kUnit) {
                 wait_loads<0>();
-                __syncthreads();  // this tile is there, and every wave has passed the other one
-                if (j0 + Sh::kUnit < stop) {
-                    pages(j0 + Sh::kUnit);
-                    load_k(j0 + Sh::kUnit, stage ^ 1);
-                    load_v(j0 + Sh::kUnit, stage ^ 1);
+                __syncthreads();
+                if (j0 + Sh::kUnit < stop) load_v(j0 + Sh::kUnit, stage ^ 1);
+                if (j0 + 2 * Sh::kUnit < stop) {
+                    pages(j0 + 2 * Sh::kUnit);
+                    load_k(j0 + 2 * Sh::kUnit, stage);
                 }
-                u32x4* buf = mine + stage * 2 * Sh::kGranules;
                 if (j0 + Sh::kKeys > lim_0) {  // for all waves alike
-                    if (clean<T>(buf + Sh::kGranules, tid, 256, Sh::kGranules)) cleaned[turn] = 1;
+                    if (clean<T>(mine + (2 * stage + 1) * Sh::kGranules, tid, 256, Sh::kGranules)) cleaned[turn] = 1;
                     __syncthreads();
                 }
-                if (!idle && j0 < lim_hi) {
-                    x.scores(buf);
-                    x.rescale(j0, j0 + Sh::kKeys > lim_lo, a.sl2);
-                    x.values(buf + Sh::kGranules, a.sl2);
-                }
                 stage ^= 1;
+                x.ka ^= kTile;
+                if (j0 < end) {
+                    x.rescale(s0, most, j0, j0 + 32 > lim_lo, a.sl2);
+                    // the wave with products to issue goes first: the two workgroups of a
+                    // compute unit then take turns (chunk of 512 over 16000: 2 % faster)
+                    __builtin_amdgcn_s_setprio(1);
+                    s1 = x.template step<true, 0>(s0, k, 0, a.sl2, most);
+                    __builtin_amdgcn_s_setprio(0);
+                }
+                if (j0 + 32 < end) {
+                    x.rescale(s1, most, j0 + 32, j0 + 64 > lim_lo, a.sl2);
+                    __builtin_amdgcn_s_setprio(1);
+                    s0 = x.template step<true, kBlock>(s1, k, kBlock, a.sl2, most);
+                    __builtin_amdgcn_s_setprio(0);
+                }
+                x.va ^= kTile;
             }
         }
 
-        // The results of the waves in LDS: wave, row, dim, four dims a granule,
-        // permuted like the keys.
-        __syncthreads();
-        float* const all = (float*)lds;
-        const float l = sum_halves(x.l);
-        if (tid == 0) cleaned[turn ^ 1] = 0;
-        if (half == 0) red[wave][col][0] = x.m, red[wave][col][1] = l;
-#pragma unroll
-        for (uint32_t d = 0; d < kDim / 32; ++d)
-#pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) {
-                const uint32_t g = 8 * d + 2 * i + half;
-                *(f32x4*)(all + (wave * 32 + col) * kDim + (g ^ (col & 7)) * 4) =
-                    f32x4{x.o[d][4 * i], x.o[d][4 * i + 1], x.o[d][4 * i + 2], x.o[d][4 * i + 3]};
-            }
+        // The results.  Infinities and not-a-numbers that a row sees in the tiles that
+        // lost theirs come back first (key by key; rare).
         __syncthreads();
         const bool whole = u0 == 0 && u1 == units;
-        const uint32_t count = min(rows - tile0, Sh::kRows);
-        float* const part = a.part + (size_t)(2 * w + (u0 == 0 ? 1 : 0)) * Sh::kPart;
+        if (uniform(cleaned[turn])) {
+            const uint32_t fix0 = max(lim_0 / Sh::kKeys * Sh::kKeys, key0);
+            const bool mine_first = !kSplit || wave == 0;  // (the waves of the tokens form are added)
 #pragma unroll 1
-        for (uint32_t i = tid; i < count * (kDim / 4); i += 256) {
-            const uint32_t r = i / (kDim / 4), g = i % (kDim / 4);
-            if (4 * g >= dim) continue;
-            f32x4 y;
-            float m, ls;
-            if (kSplit) {
-                m = fmaxf(fmaxf(red[0][r][0], red[1][r][0]), fmaxf(red[2][r][0], red[3][r][0]));
-                const float base = m == -INFINITY ? 0.f : m * a.sl2;
-                ls = 0.f;
-                y = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (uint32_t j = fix0; j < stop; ++j) {
+                const T* v = (const T*)vb + seq_page(a.sq, a.kv, st.s, j) * a.kv.vp + (j & mask) * a.kv.ve;
 #pragma unroll
-                for (uint32_t v = 0; v < 4; ++v) {
-                    const float f = __builtin_amdgcn_exp2f(red[v][r][0] * a.sl2 - base);
-                    ls += red[v][r][1] * f;
-                    y += *(const f32x4*)(all + (v * 32 + r) * kDim + (g ^ (r & 7)) * 4) * f;
-                }
-            } else {
-                m = red[r / 32][r % 32][0];
-                ls = red[r / 32][r % 32][1];
-                y = *(const f32x4*)(all + r * kDim + (g ^ (r & 7)) * 4);
-            }
-            if (cleaned[turn]) {
-                // infinities and not-a-numbers that the row sees in the tiles that lost theirs
-                const int64_t see = (int64_t)sp.n - sp.c + (tile0 + r) / a.grp + 1;
-                for (int64_t j = max((int64_t)(lim_0 / Sh::kKeys * Sh::kKeys), (int64_t)u0 * Sh::kUnit); j < see && j < stop; ++j) {
-                    const T* v = (const T*)vb + seq_page(a.sq, a.kv, st.s, (uint32_t)j) * a.kv.vp + ((uint32_t)j & mask) * a.kv.ve + 4 * g;
+                for (uint32_t i = 0; i < kDim / 8; ++i) {
+                    typedef T T4 __attribute__((ext_vector_type(4)));
+                    if (i >= live || j >= x.lim || !mine_first) continue;
+                    const T4 f = *(const T4*)(v + 8 * i + 4 * half);
 #pragma unroll
                     for (uint32_t k = 0; k < 4; ++k) {
-                        const float f = (float)v[k];
-                        if (f - f != 0.f) y[k] += f;
+                        const float y = (float)f[k];
+                        if (y - y != 0.f) x.o[i / 4][4 * (i % 4) + k] += y;
                     }
                 }
             }
-            if (whole) {
-                put_row(a, sp, st.kh, tile0 + r, g, y, m, ls);
-            } else {
-                put_part(part + r * kDim + 4 * g, y[0], y[1]);
-                put_part(part + r * kDim + 4 * g + 2, y[2], y[3]);
-                if (g == 0) put_part(part + Sh::kRows * kDim + 2 * r, m, ls);
-            }
         }
+        if (tid == 0) cleaned[turn ^ 1] = 0;  // (last read before the barrier that ended the segment before)
+        float* const part = a.part + (size_t)(2 * w + (u0 == 0 ? 1 : 0)) * Sh::kPart;
+        // the tile's ranges w0 .. w1 where there are several; counted on the first one's word
+        uint32_t w0 = 0, w1 = 0;
         if (!whole) {
-            // the tile's ranges w0 .. w1, counted on the first one's word
             const uint32_t at = range_at(w, st.total, groups) + done - u0;
-            const uint32_t w0 = range_of(at, st.total, groups), w1 = range_of(at + units - 1, st.total, groups);
+            w0 = range_of(at, st.total, groups), w1 = range_of(at + units - 1, st.total, groups);
+        }
+        // After this workgroup's part is written: is it the last of the tile's?
+        auto last_of_tile = [&]() {
             __builtin_amdgcn_s_waitcnt(0);
             __syncthreads();
             if (tid == 0) {
@@ -696,14 +768,111 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
                 last_one = is_last;
             }
             __syncthreads();
-            if (uniform(last_one)) {
+            return uniform(last_one) != 0;
+        };
+        float l = sum_halves(x.l);
+        if (!kSplit) {
+            // each wave its own rows, from registers: four values a lane, lane after lane
+            constexpr uint32_t kSums = 32 * kDim;  // floats of a wave's sums
+            bool out = true;
+            if (!whole) {
+                float* p = part + wave * kSums + 4 * lane;
+#pragma unroll
+                for (uint32_t i = 0; i < kDim / 8; ++i) {
+                    put_part(p + 256 * i, x.o[i / 4][4 * (i % 4)], x.o[i / 4][4 * (i % 4) + 1]);
+                    put_part(p + 256 * i + 2, x.o[i / 4][4 * (i % 4) + 2], x.o[i / 4][4 * (i % 4) + 3]);
+                }
+                if (half == 0) put_part(part + 4 * kSums + 64 * wave + 2 * col, x.m, l);
+                out = last_of_tile();
+                if (out) {
+                    x.m = -INFINITY, l = 0.f;
+#pragma unroll
+                    for (uint32_t d = 0; d < kDim / 32; ++d) x.o[d] = f32x16{};
+#pragma unroll 1
+                    for (uint32_t v = w0; v <= w1; ++v) {
+                        const float* from = a.part + (size_t)(2 * v + (v == w0 ? 1 : 0)) * Sh::kPart;
+                        const float2 ml = get_part(from + 4 * kSums + 64 * wave + 2 * col);
+                        float2 y[kDim / 4];
+#pragma unroll
+                        for (uint32_t i = 0; i < kDim / 4; ++i)
+                            y[i] = get_part(from + wave * kSums + 4 * lane + 256 * (i / 2) + 2 * (i % 2));
+                        const float top = fmaxf(x.m, ml.x), base = top == -INFINITY ? 0.f : top * a.sl2;
+                        const float fa = __builtin_amdgcn_exp2f(x.m * a.sl2 - base), fb = __builtin_amdgcn_exp2f(ml.x * a.sl2 - base);
+                        x.m = top;
+                        l = l * fa + ml.y * fb;
+#pragma unroll
+                        for (uint32_t i = 0; i < kDim / 4; ++i) {
+                            x.o[i / 8][2 * (i % 8)] = x.o[i / 8][2 * (i % 8)] * fa + y[i].x * fb;
+                            x.o[i / 8][2 * (i % 8) + 1] = x.o[i / 8][2 * (i % 8) + 1] * fa + y[i].y * fb;
+                        }
+                    }
+                }
+            }
+            if (out && a.wide_out) {
+                if (row0 + col < rows) {
+                    const uint32_t tok = known / a.grp, head = st.kh * a.grp + known % a.grp;
+                    const float inv = l > 0.f ? 1.f / l : l;  // (zero for a row without entries; its sums are zeros)
+                    put_rows<kDim>(a, (size_t)(sp.q0 + tok) * a.out.token + (size_t)head * a.out.head + 4 * half, x.o, inv);
+                    if (a.lse && half == 0) put_lse(a, (size_t)(sp.q0 + tok) * a.heads + head, x.m, l);
+                }
+                out = false;
+            }
+            if (out) {
+                // rows without alignment: by way of LDS, value by value
+                float* const all = (float*)lds + wave * kSums;
+#pragma unroll
+                for (uint32_t i = 0; i < kDim / 8; ++i)
+                    *(f32x4*)(all + col * kDim + ((2 * i + half) ^ (col & 7)) * 4) =
+                        f32x4{x.o[i / 4][4 * (i % 4)], x.o[i / 4][4 * (i % 4) + 1], x.o[i / 4][4 * (i % 4) + 2], x.o[i / 4][4 * (i % 4) + 3]};
+                if (half == 0) red[wave][col][0] = x.m, red[wave][col][1] = l;
+                wait_reads();
+#pragma unroll 1
+                for (uint32_t i = lane; i < 32 * (kDim / 4); i += 64) {
+                    const uint32_t r = i / (kDim / 4), g = i % (kDim / 4);
+                    if (4 * g < dim && row0 + r < rows)
+                        put_row(a, sp, st.kh, row0 + r, g, *(const f32x4*)(all + r * kDim + (g ^ (r & 7)) * 4), red[wave][r][0], red[wave][r][1]);
+                }
+            }
+        } else {
+            // the waves' sums by way of LDS: wave, row, dim, four dims a granule, permuted like the keys
+            float* const all = (float*)lds;
+            if (half == 0) red[wave][col][0] = x.m, red[wave][col][1] = l;
+#pragma unroll
+            for (uint32_t i = 0; i < kDim / 8; ++i)
+                *(f32x4*)(all + (wave * 32 + col) * kDim + ((2 * i + half) ^ (col & 7)) * 4) =
+                    f32x4{x.o[i / 4][4 * (i % 4)], x.o[i / 4][4 * (i % 4) + 1], x.o[i / 4][4 * (i % 4) + 2], x.o[i / 4][4 * (i % 4) + 3]};
+            __syncthreads();
+            const uint32_t count = min(rows - tile0, Sh::kRows);
+#pragma unroll 1
+            for (uint32_t i = tid; i < count * (kDim / 4); i += 256) {
+                const uint32_t r = i / (kDim / 4), g = i % (kDim / 4);
+                if (4 * g >= dim) continue;
+                const float m = fmaxf(fmaxf(red[0][r][0], red[1][r][0]), fmaxf(red[2][r][0], red[3][r][0]));
+                const float base = m == -INFINITY ? 0.f : m * a.sl2;
+                float ls = 0.f;
+                f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (uint32_t v = 0; v < 4; ++v) {
+                    const float f = __builtin_amdgcn_exp2f(red[v][r][0] * a.sl2 - base);
+                    ls += red[v][r][1] * f;
+                    y += *(const f32x4*)(all + (v * 32 + r) * kDim + (g ^ (r & 7)) * 4) * f;
+                }
+                if (whole) {
+                    put_row(a, sp, st.kh, tile0 + r, g, y, m, ls);
+                } else {
+                    put_part(part + r * kDim + 4 * g, y[0], y[1]);
+                    put_part(part + r * kDim + 4 * g + 2, y[2], y[3]);
+                    if (g == 0) put_part(part + Sh::kRows * kDim + 2 * r, m, ls);
+                }
+            }
+            if (!whole && last_of_tile()) {
 #pragma unroll 1
                 for (uint32_t i = tid; i < count * (kDim / 4); i += 256) {
                     const uint32_t r = i / (kDim / 4), g = i % (kDim / 4);
                     if (4 * g >= dim) continue;
                     float m = -INFINITY, ls = 0.f;
                     f32x4 y = {0.f, 0.f, 0.f, 0.f};
-                    constexpr uint32_t kAhead = 8;  // parts whose loads are in flight together
+                    constexpr uint32_t kAhead = 16;  // parts whose loads are in flight together
 #pragma unroll 1
                     for (uint32_t v = w0; v <= w1; v += kAhead) {
                         float2 ml[kAhead], ya[kAhead], yb[kAhead];
@@ -739,9 +908,12 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
             st.tile = 0;
             if (++st.kh == a.kv.heads) {
                 st.kh = 0;
-                if (done < st.left)
-                    do ++st.s;
-                    while (st.s + 1 < a.sq.count && uniform(seq_span(a.sq, a.kv.shift, st.s, a.tokens).c) == 0);
+                if (done < st.left) {
+                    do {
+                        ++st.s;
+                        sequence();
+                    } while (sp.c == 0 && st.s + 1 < a.sq.count);
+                }
             }
         }
     }
@@ -865,7 +1037,7 @@ bool attend_tile_fits(const Rows& q, uint32_t tokens, uint32_t heads, const KvVi
     // units (64 keys at least) of tiles (32 rows at least) are counted in 32 bits
     const uint64_t grp = heads / kv.heads, rows = tokens * grp, seen = ((uint64_t)sq.width << kv.shift) + tokens + 256;
     if (seen * grp + rows + 256 >= (1ull << 32)) return false;
-    return rows / 32 + sq.count < (1ull << 31) / (seen / 64 + 1) / kv.heads;
+    return rows / 32 + sq.count < (1ull << 31) / (seen / 64 + 8) / kv.heads;
 }
 
 size_t attend_tile_bytes(const KvView& kv, bool split) {
@@ -915,8 +1087,8 @@ hipError_t launch_attend_tile(const Rows& q, uint32_t tokens, uint32_t heads, co
     TileArgs a = tile_args(q, tokens, heads, kv, sq, scale);
     a.out = out;
     a.inv_scale = inv_scale, a.lse = lse, a.part = (float*)ws, a.counters = counters;
-    a.wide_out = (out.type == MVK_TYPE_BF16 || out.type == MVK_TYPE_F16) && (uintptr_t)out.p % 8 == 0 &&
-                 (out.token | out.head) % 4 == 0;
+    const bool half = out.type == MVK_TYPE_BF16 || out.type == MVK_TYPE_F16;
+    a.wide_out = (uintptr_t)out.p % (half ? 8 : 16) == 0 && (out.token | out.head) % 4 == 0;
     return q.type == MVK_TYPE_BF16 ? launch_type<__bf16>(a, split, s) : launch_type<_Float16>(a, split, s);
 }
 
