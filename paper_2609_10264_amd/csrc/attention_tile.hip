@@ -279,8 +279,8 @@ struct WaveRows {
     // The first addresses of this lane in a tile of K and one of V, in bytes; the
     // order of the granules makes the others exclusive-ors of them.
     uint32_t ka, va;
-    __device__ __forceinline__ void places(uint32_t k, uint32_t v) {
-        const uint32_t lane = threadIdx.x & 63, half = lane >> 5;
+    __device__ __forceinline__ void places(uint32_t lane, uint32_t k, uint32_t v) {
+        const uint32_t half = lane >> 5;
         ka = k + 16 * k_at<kDim>(lane & 31, half);
         va = v + 16 * v_at<kDim>(4 * half + (lane & 15) / 4, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
     }
@@ -532,8 +532,7 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
     __shared__ __attribute__((aligned(65536))) u32x4 lds[Sh::kLds];  // (at 0: see kTile)
     __shared__ float red[4][32][2];
     __shared__ uint32_t last_one, cleaned[2];  // (cleaned: of this segment and the next)
-    const uint32_t tid = threadIdx.x, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6)), lane = tid & 63;
-    const uint32_t col = lane & 31, half = lane >> 5;
+    const uint32_t tid = threadIdx.x, wave = uniform(tid >> 6);
     const uint32_t dim = a.kv.dim, live = dim / 8;  // granules of a row that hold data
     // consecutive ranges on one XCD, whose L2 then holds the keys they share
     const uint32_t groups = gridDim.x, xcds = groups % 8 == 0 ? 8 : 1;
@@ -558,6 +557,11 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
     if (st.left) sequence();
 #pragma unroll 1
     while (done < st.left) {
+        // (unknown to the compiler, which would otherwise keep every address of the
+        // beginnings and ends of tiles in registers that the loops need)
+        uint32_t lane = tid & 63;
+        asm volatile("" : "+v"(lane));
+        const uint32_t col = lane & 31, half = lane >> 5;
         const Tiles<Sh::kRows, Sh::kUnit, Sh::kExtra> tiles(sp, a.grp);
         const uint32_t units = tiles.units(st.tile);
         const uint32_t u0 = st.unit, u1 = min(units, u0 + (st.left - done));
@@ -565,31 +569,6 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
         // rows
         const uint32_t rows = sp.c * a.grp, tile0 = st.tile * Sh::kRows, row0 = tile0 + (kSplit ? 0 : 32 * wave);
         const uint32_t known = min(row0 + col, rows - 1);
-        WaveRows<T, kDim> x;
-        {
-            const uint32_t tok = known / a.grp, head = st.kh * a.grp + known % a.grp;
-            const int64_t see = (int64_t)sp.n - sp.c + tok + 1;
-            x.lim = see > 0 ? (uint32_t)see : 0u;
-            const T* qr = (const T*)a.q.p + (size_t)(sp.q0 + tok) * a.q.token + (size_t)head * a.q.head;
-            u32x4 v[kDim / 16];  // (rows and granules that are not there: zeros, so that all loads are in flight at once)
-#pragma unroll
-            for (uint32_t t = 0; t < kDim / 16; ++t) {
-                const uint32_t g = 2 * t + half;
-                v[t] = *(row0 + col < rows && g < live ? (const u32x4*)(qr + 8 * g) : &kZeroGranule);
-            }
-#pragma unroll
-            for (uint32_t t = 0; t < kDim / 16; ++t) x.q[t] = __builtin_bit_cast(V8, v[t] ^ a.flip);
-#pragma unroll
-            for (uint32_t d = 0; d < kDim / 32; ++d) x.o[d] = f32x16{};
-            x.m = -INFINITY;
-            x.l = 0.f;
-        }
-        // limits of the wave's rows: rows are in order, so lane 0 sees least
-        const uint32_t lim_lo = uniform(x.lim);
-        const uint32_t lim_hi = (uint32_t)__builtin_amdgcn_readlane((int)x.lim, 31);
-        const uint32_t lim_0 = (uint32_t)max((int64_t)sp.n - sp.c + tile0 / a.grp + 1, (int64_t)0);  // of the tile's rows
-        const bool idle = !kSplit && row0 >= rows;  // a wave without rows
-
         // keys
         const char* const kb = (const char*)((const T*)a.kv.K + (size_t)st.kh * a.kv.kh);
         const char* const vb = (const char*)((const T*)a.kv.V + (size_t)st.kh * a.kv.vh);
@@ -637,13 +616,44 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
         auto load_v = [&](uint32_t j0, uint32_t stage) {
             load(vb, a.kv.vp, a.kv.ve, true, j0, lds0 + 16 * ((kSplit ? wave : stage) * 2 * Sh::kGranules + Sh::kGranules + part0));
         };
-        x.places(lds0 + (kSplit ? wave * 32 * Sh::kGranules : 0), lds0 + (kSplit ? wave * 32 * Sh::kGranules : 0) + 16 * Sh::kGranules);
-        if (kSplit) {
-            if (first < stop) {
-                pages(first);
-                load_k(first, 0);
-                load_v(first, 0);
+        // the first loads of keys, then the rows, which arrive behind them
+        if (first < stop) {
+            pages(first);
+            load_k(first, 0);
+            load_v(first, 0);
+            if (!kSplit && first + Sh::kUnit < stop) {
+                pages(first + Sh::kUnit);
+                load_k(first + Sh::kUnit, 1);
             }
+        }
+
+        WaveRows<T, kDim> x;
+        {
+            const uint32_t tok = known / a.grp, head = st.kh * a.grp + known % a.grp;
+            const int64_t see = (int64_t)sp.n - sp.c + tok + 1;
+            x.lim = see > 0 ? (uint32_t)see : 0u;
+            const T* qr = (const T*)a.q.p + (size_t)(sp.q0 + tok) * a.q.token + (size_t)head * a.q.head;
+            u32x4 v[kDim / 16];  // (rows and granules that are not there: zeros, so that all loads are in flight at once)
+#pragma unroll
+            for (uint32_t t = 0; t < kDim / 16; ++t) {
+                const uint32_t g = 2 * t + half;
+                v[t] = *(row0 + col < rows && g < live ? (const u32x4*)(qr + 8 * g) : &kZeroGranule);
+            }
+#pragma unroll
+            for (uint32_t t = 0; t < kDim / 16; ++t) x.q[t] = __builtin_bit_cast(V8, v[t] ^ a.flip);
+#pragma unroll
+            for (uint32_t d = 0; d < kDim / 32; ++d) x.o[d] = f32x16{};
+            x.m = -INFINITY;
+            x.l = 0.f;
+        }
+        // limits of the wave's rows: rows are in order, so lane 0 sees least
+        const uint32_t lim_lo = uniform(x.lim);
+        const uint32_t lim_hi = (uint32_t)__builtin_amdgcn_readlane((int)x.lim, 31);
+        const uint32_t lim_0 = (uint32_t)max((int64_t)sp.n - sp.c + tile0 / a.grp + 1, (int64_t)0);  // of the tile's rows
+        const bool idle = !kSplit && row0 >= rows;  // a wave without rows
+
+        x.places(lane, lds0 + (kSplit ? wave * 32 * Sh::kGranules : 0), lds0 + (kSplit ? wave * 32 * Sh::kGranules : 0) + 16 * Sh::kGranules);
+        if (kSplit) {
 #pragma unroll 1
             for (uint32_t j0 = first; j0 < stop; j0 += Sh::kUnit) {
                 const bool more = j0 + Sh::kUnit < stop, masked = j0 + Sh::kKeys > lim_lo;
@@ -673,16 +683,7 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
             constexpr uint32_t kTile = 32 * Sh::kGranules, kBlock = 8 * Sh::kGranules;  // bytes
             static_assert((kTile & (kTile - 1)) == 0, "one bit tells the tiles apart");
             uint32_t stage = 0;
-            pages(first);
-            load_k(first, 0);
-            load_v(first, 0);
-            if (first + Sh::kUnit < stop) {
-                pages(first + Sh::kUnit);
-                load_k(first + Sh::kUnit, 1);
-                wait_loads<2 * Sh::kLoads>();
-            } else {
-                wait_loads<Sh::kLoads>();
-            }
+            wait_loads<0>();
             __syncthreads();
             f32x16 s0 = {}, s1 = {};
             V8 k[kDim / 16];
@@ -788,22 +789,31 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
                     x.m = -INFINITY, l = 0.f;
 #pragma unroll
                     for (uint32_t d = 0; d < kDim / 32; ++d) x.o[d] = f32x16{};
+                    // two parts' loads in flight
 #pragma unroll 1
-                    for (uint32_t v = w0; v <= w1; ++v) {
-                        const float* from = a.part + (size_t)(2 * v + (v == w0 ? 1 : 0)) * Sh::kPart;
-                        const float2 ml = get_part(from + 4 * kSums + 64 * wave + 2 * col);
-                        float2 y[kDim / 4];
+                    for (uint32_t v = w0; v <= w1; v += 2) {
+                        float2 ml[2], y[2][kDim / 4];
 #pragma unroll
-                        for (uint32_t i = 0; i < kDim / 4; ++i)
-                            y[i] = get_part(from + wave * kSums + 4 * lane + 256 * (i / 2) + 2 * (i % 2));
-                        const float top = fmaxf(x.m, ml.x), base = top == -INFINITY ? 0.f : top * a.sl2;
-                        const float fa = __builtin_amdgcn_exp2f(x.m * a.sl2 - base), fb = __builtin_amdgcn_exp2f(ml.x * a.sl2 - base);
-                        x.m = top;
-                        l = l * fa + ml.y * fb;
+                        for (uint32_t u = 0; u < 2; ++u) {
+                            const uint32_t vu = min(v + u, w1);
+                            const float* from = a.part + (size_t)(2 * vu + (vu == w0 ? 1 : 0)) * Sh::kPart;
+                            ml[u] = get_part(from + 4 * kSums + 64 * wave + 2 * col);
 #pragma unroll
-                        for (uint32_t i = 0; i < kDim / 4; ++i) {
-                            x.o[i / 8][2 * (i % 8)] = x.o[i / 8][2 * (i % 8)] * fa + y[i].x * fb;
-                            x.o[i / 8][2 * (i % 8) + 1] = x.o[i / 8][2 * (i % 8) + 1] * fa + y[i].y * fb;
+                            for (uint32_t i = 0; i < kDim / 4; ++i)
+                                y[u][i] = get_part(from + wave * kSums + 4 * lane + 256 * (i / 2) + 2 * (i % 2));
+                        }
+#pragma unroll
+                        for (uint32_t u = 0; u < 2; ++u) {
+                            if (v + u > w1) break;
+                            const float top = fmaxf(x.m, ml[u].x), base = top == -INFINITY ? 0.f : top * a.sl2;
+                            const float fa = __builtin_amdgcn_exp2f(x.m * a.sl2 - base), fb = __builtin_amdgcn_exp2f(ml[u].x * a.sl2 - base);
+                            x.m = top;
+                            l = l * fa + ml[u].y * fb;
+#pragma unroll
+                            for (uint32_t i = 0; i < kDim / 4; ++i) {
+                                x.o[i / 8][2 * (i % 8)] = x.o[i / 8][2 * (i % 8)] * fa + y[u][i].x * fb;
+                                x.o[i / 8][2 * (i % 8) + 1] = x.o[i / 8][2 * (i % 8) + 1] * fa + y[u][i].y * fb;
+                            }
                         }
                     }
                 }
@@ -922,81 +932,107 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
 // Collected weights: a workgroup owns kWeightKeys entries of one (sequence, kv
 // head), 32 a wave, and adds the probabilities of all rows that see them, in
 // order: S = Q K^T (rows down, keys across, so that a lane sums its own key),
-// p = exp(scale S - lse).  K is read once; each wave reads the rows for itself.
+// p = exp(scale S - lse).  K is read once and stays in registers; the rows pass
+// through LDS 32 at a time, one tile in flight, for the four waves together.
 constexpr uint32_t kWeightKeys = 128;
 template <typename T, uint32_t kDim>
 __global__ __launch_bounds__(256) void weights_tile(TileArgs a, const float* __restrict__ lse, const float* w_in,
                                                     float* w_out, size_t w_seq, size_t w_head) {
     typedef typename Mma<T>::V8 V8;
-    __shared__ float row_lse[4][32];
-    __shared__ uint32_t row_lim[4][32];
-    const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    constexpr uint32_t G = kDim / 8, kT = kDim / 16, kGranules = 32 * G;  // of 32 keys or rows
+    constexpr uint32_t kLoadsK = kGranules / 64, kLoadsQ = kGranules / 256, kStep = 64 / G;
+    __shared__ __attribute__((aligned(65536))) u32x4 lds[6 * kGranules];  // K of the waves, two tiles of rows
+    __shared__ float row_lse[2][32];
+    __shared__ uint32_t row_lim[2][32];
+    const uint32_t tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
     const uint32_t kh = blockIdx.y, s = blockIdx.z, live = a.kv.dim / 8;
-    const SeqSpan sp = seq_span(a.sq, a.kv.shift, s, a.tokens);
-    const uint32_t j0 = blockIdx.x * kWeightKeys + 32 * wave;
-    if (j0 >= sp.n) return;  // no barrier below spans waves
+    SeqSpan sp = seq_span(a.sq, a.kv.shift, s, a.tokens);
+    sp = {uniform(sp.q0), uniform(sp.c), uniform(sp.n)};
+    const uint32_t first = blockIdx.x * kWeightKeys, j0 = first + 32 * wave, j = j0 + col;
+    if (first >= sp.n) return;
     const int64_t base = (int64_t)sp.n - sp.c;
-    const uint32_t j = j0 + col, jc = min(j, sp.n - 1);
-    V8 k[kDim / 16];
+    const uint32_t rows = sp.c * a.grp;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
+    const u32x4* const zero = &kZeroGranule;
     {
-        const size_t page = seq_page(a.sq, a.kv, s, jc), at = jc & ((1u << a.kv.shift) - 1);
-        const T* kr = (const T*)a.kv.K + page * a.kv.kp + kh * a.kv.kh + at * a.kv.ke;
+        const T* const kb = (const T*)a.kv.K + (size_t)kh * a.kv.kh;
+        size_t page[kLoadsK];  // (all looked up before the first load waits for its own)
 #pragma unroll
-        for (uint32_t t = 0; t < kDim / 16; ++t) {
-            u32x4 v = {0, 0, 0, 0};
-            const uint32_t g = 2 * t + half;
-            if (g < live) v = *(const u32x4*)(kr + 8 * g);
-            k[t] = __builtin_bit_cast(V8, v);
+        for (uint32_t i = 0; i < kLoadsK; ++i) page[i] = seq_page(a.sq, a.kv, s, min(j0 + kStep * i + lane / G, sp.n - 1));
+#pragma unroll
+        for (uint32_t i = 0; i < kLoadsK; ++i) {
+            const uint32_t r = kStep * i + lane / G, g = k_at<kDim>(r, lane % G) % G;
+            const uint32_t at = min(j0 + r, sp.n - 1) & ((1u << a.kv.shift) - 1);
+            load_lds(g < live ? (const void*)(kb + page[i] * a.kv.kp + at * a.kv.ke + 8 * g) : zero, lds0 + 16 * (wave * kGranules + 64 * i));
         }
     }
-    const uint32_t rows = sp.c * a.grp;
-    // rows of the first token that sees entry j0, from a whole 32 on
-    uint32_t r0 = j0 > base ? (uint32_t)((int64_t)j0 - base) * a.grp / 32 * 32 : 0u;
-    float sum = 0.f;
-    u32x4 q[kDim / 16];
-    float z = 0.f;
+    // rows of the first token that sees entry `first`, from a whole 32 on
+    uint32_t r0 = first > base ? (uint32_t)((int64_t)first - base) * a.grp / 32 * 32 : 0u, stage = 0;
+    auto load = [&](uint32_t r, uint32_t to) {
+#pragma unroll
+        for (uint32_t i = 0; i < kLoadsQ; ++i) {
+            const uint32_t at = kStep * (kLoadsQ * wave + i) + lane / G, g = k_at<kDim>(at, lane % G) % G, row = r + at;
+            const uint32_t tok = row / a.grp, head = kh * a.grp + row % a.grp;
+            const T* qr = (const T*)a.q.p + (size_t)(sp.q0 + tok) * a.q.token + (size_t)head * a.q.head;
+            load_lds(g < live && row < rows ? (const void*)(qr + 8 * g) : zero,
+                     lds0 + 16 * ((4 + to) * kGranules + 64 * (kLoadsQ * wave + i)));
+        }
+    };
+    // of row r + tid (32 threads): what is taken from its scores, and the entries that it sees
+    float z = INFINITY;
     uint32_t lim = 0;
-    auto load = [&](uint32_t r) {
-        const uint32_t row = r + col;
-        const uint32_t tok = row / a.grp, head = kh * a.grp + row % a.grp;
+    auto about = [&](uint32_t r) {
+        const uint32_t row = r + tid, tok = row / a.grp, head = kh * a.grp + row % a.grp;
         z = INFINITY;
         lim = 0;
-#pragma unroll
-        for (uint32_t t = 0; t < kDim / 16; ++t) q[t] = u32x4{0, 0, 0, 0};
-        if (row < rows) {
+        if (tid < 32 && row < rows) {
             const int64_t see = base + tok + 1;
             lim = see > 0 ? (uint32_t)see : 0u;
             z = lse[(size_t)(sp.q0 + tok) * a.heads + head] * kLog2e;
             if (z == -INFINITY) z = INFINITY;  // a row without a sum gives nothing
-            const T* qr = (const T*)a.q.p + (size_t)(sp.q0 + tok) * a.q.token + (size_t)head * a.q.head;
-#pragma unroll
-            for (uint32_t t = 0; t < kDim / 16; ++t) {
-                const uint32_t g = 2 * t + half;
-                if (g < live) q[t] = *(const u32x4*)(qr + 8 * g) ^ a.flip;
-            }
         }
     };
-    if (r0 < rows) load(r0);
-    for (; r0 < rows; r0 += 32) {
-        if (half == 0) row_lse[wave][col] = z, row_lim[wave][col] = lim;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        f32x16 x = {};
-#pragma unroll
-        for (uint32_t t = 0; t < kDim / 16; ++t) x = Mma<T>::mul(__builtin_bit_cast(V8, q[t]), k[t], x);
-        const bool masked = j0 + 32 > (uint32_t)__builtin_amdgcn_readfirstlane((int)lim) || r0 + 32 > rows;
-        if (r0 + 32 < rows) load(r0 + 32);
-#pragma unroll
-        for (uint32_t i = 0; i < 16; ++i) {
-            const uint32_t r = 8 * (i / 4) + 4 * half + i % 4;
-            float p = __builtin_amdgcn_exp2f(x[i] * a.sl2 - row_lse[wave][r]);
-            if (masked && j >= row_lim[wave][r]) p = 0.f;
-            sum += p;
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+    float sum = 0.f, sum2 = 0.f;
+    V8 k[kT];
+    if (r0 < rows) {
+        load(r0, 0);
+        about(r0);
     }
-    sum = sum_halves(sum);
+    wait_loads<0>();
+#pragma unroll
+    for (uint32_t t = 0; t < kT; ++t)  // (a negative scale: its sign goes to K here)
+        k[t] = __builtin_bit_cast(V8, lds[wave * kGranules + k_at<kDim>(col, 2 * t + half)] ^ a.flip);
+#pragma unroll 1
+    for (; r0 < rows; r0 += 32) {
+        if (tid < 32) row_lse[stage][tid] = z, row_lim[stage][tid] = lim;
+        wait_loads<0>();
+        __syncthreads();  // these rows are there, and every wave has passed the other tile
+        if (r0 + 32 < rows) {
+            load(r0 + 32, stage ^ 1);
+            about(r0 + 32);
+        }
+        f32x16 x = {};
+        V8 q[kT];
+#pragma unroll
+        for (uint32_t t = 0; t < kT; ++t)
+            q[t] = __builtin_bit_cast(V8, lds[(4 + stage) * kGranules + k_at<kDim>(col, 2 * t + half)]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (uint32_t t = 0; t < kT; ++t) x = Mma<T>::mul(q[t], k[t], x);
+        const bool masked = j0 + 32 > row_lim[stage][0] || r0 + 32 > rows;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const f32x4 zs = *(const f32x4*)&row_lse[stage][8 * i + 4 * half];
+#pragma unroll
+            for (uint32_t u = 0; u < 4; ++u) {
+                float p = __builtin_amdgcn_exp2f(x[4 * i + u] * a.sl2 - zs[u]);
+                if (masked && j >= row_lim[stage][8 * i + 4 * half + u]) p = 0.f;
+                (u & 1 ? sum2 : sum) += p;
+            }
+        }
+        stage ^= 1;
+    }
+    sum = sum_halves(sum + sum2);
     if (half == 0 && j < sp.n) {
         const size_t o = (size_t)s * w_seq + (size_t)kh * w_head + j;
         w_out[o] = ((int64_t)j < base && w_in ? w_in[o] : 0.f) + sum;
