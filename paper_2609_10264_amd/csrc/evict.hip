@@ -14,6 +14,7 @@ namespace mvk {
 namespace {
 
 constexpr uint32_t kSelThreads = 1024, kSelWaves = kSelThreads / 64;
+constexpr uint32_t kListKeys = 4096;  // keys of a list in LDS
 
 // Unsigned keys in the order of the floats: -0 and 0 alike, not-a-numbers below all.
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -32,31 +33,76 @@ struct EvictArgs {
     int32_t* lens_out;
 };
 
-// The largest key x such that at least `want` of the candidates' keys are >= x
-// (want >= 1, at most the candidates), one bit a step from the top.  count(x):
-// this wave's candidates with keys >= x.  Ends early where a count is exactly
-// `want`: then the kept are those >= x.
-template <typename Count>
-__device__ __forceinline__ uint32_t find_threshold(Count count, uint32_t want, uint32_t (*sm)[kSelWaves], bool& exact) {
-    const uint32_t wave = threadIdx.x >> 6;
-    uint32_t x = 0;
-    exact = false;
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t cand = x | (1u << bit);
-        const uint32_t mine = count(cand);
-        uint32_t* s = sm[bit & 1];  // two in turn: one barrier a step
-        if ((threadIdx.x & 63) == 0) s[wave] = mine;
-        __syncthreads();
+// Where a search stands: the want-th largest of the candidates' keys lies in
+// [x, x + 2^bit); lo keys are >= x, hi are >= x + 2^bit (hi < want <= lo).
+struct Search {
+    uint32_t x, bit, lo, hi, want;
+    __device__ __forceinline__ bool done() const { return bit == 0 || lo == want; }
+    __device__ __forceinline__ bool holds(uint32_t k) const { return k && k >= x && (bit == 32 || (k - x) >> bit == 0); }
+};
+
+// One step of kBits bits.  count(c): this wave's keys >= c.
+template <uint32_t kBits, typename Count>
+__device__ __forceinline__ void search_step(Search& s, Count count, uint32_t (*sm)[3][kSelWaves], uint32_t& turn) {
+    const uint32_t bits = min(kBits, s.bit), unit = 1u << (s.bit - bits), wave = threadIdx.x >> 6;
+    uint32_t(*c)[kSelWaves] = sm[turn];  // two in turn: one barrier a step
+    turn ^= 1;
+    constexpr uint32_t kCands = (1u << kBits) - 1;
+#pragma unroll
+    for (uint32_t i = 0; i < kCands; ++i) {
+        const uint32_t n = count(s.x + (i + 1) * unit);
+        if ((threadIdx.x & 63) == 0) c[i][wave] = n;
+    }
+    __syncthreads();
+    const uint32_t x0 = s.x;
+    s.bit -= bits;
+#pragma unroll
+    for (uint32_t i = 0; i < kCands; ++i) {
+        if (i + 1 >= 1u << bits) break;
         uint32_t sum = 0;
 #pragma unroll
-        for (uint32_t i = 0; i < kSelWaves; ++i) sum += s[i];
-        if (sum >= want) x = cand;
-        if (sum == want) {
-            exact = true;
-            break;
-        }
+        for (uint32_t w = 0; w < kSelWaves; ++w) sum += c[i][w];
+        if (sum >= s.want) s.x = x0 + (i + 1) * unit, s.lo = sum;
+        else if (sum > s.hi) s.hi = sum;
     }
-    return x;
+}
+
+// The rest of a search among the `n` keys of a list in LDS (those in its range), two
+// bits a step.
+template <uint32_t kMost>
+__device__ __forceinline__ void search_list(Search& s, const uint32_t* list, uint32_t n, uint32_t (*sm)[3][kSelWaves],
+                                            uint32_t& turn) {
+    constexpr uint32_t kEach = kMost / kSelThreads;
+    uint32_t k[kEach];
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+        const uint32_t e = i * kSelThreads + threadIdx.x;
+        k[i] = e < n ? list[e] : 0u;
+    }
+    const uint32_t above = s.hi;  // keys beyond the range are not in the list
+    s.want -= above, s.lo -= above, s.hi = 0;
+    while (!s.done())
+        search_step<2>(
+            s,
+            [&](uint32_t c) {
+                uint32_t m = 0;
+#pragma unroll
+                for (uint32_t i = 0; i < kEach; ++i) m += (uint32_t)__popcll(__ballot(k[i] >= c));
+                return m;
+            },
+            sm, turn);
+    s.want += above, s.lo += above, s.hi += above;
+}
+
+// Appends the keys that the search's range holds to the list (in any order: only their values count).
+__device__ __forceinline__ void append(uint32_t* list, uint32_t* size, bool f, uint32_t k) {
+    const uint64_t b = __ballot(f);
+    if (!b) return;
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t at = 0;
+    if (lane == 0) at = atomicAdd(size, (uint32_t)__popcll(b));
+    at = (uint32_t)__shfl((int)at, 0);
+    if (f) list[at + (uint32_t)__popcll(b & ((1ull << lane) - 1))] = k;
 }
 
 // Exclusive prefix sums of sm[0, kCount), in place, and the total (wave 0 scans).
@@ -97,32 +143,48 @@ __device__ __forceinline__ uint32_t scan_counts(uint32_t* sm, uint32_t* total) {
 // the count of a lane mask for each.
 template <uint32_t kEach>
 __device__ __forceinline__ void select_in_registers(const EvictArgs& a, const float* w, float* wo, int32_t* kept,
-                                                    uint32_t n, uint32_t want, uint32_t (*sm)[kSelWaves],
-                                                    uint32_t* counts, uint32_t* tied, uint32_t* total) {
+                                                    uint32_t n, uint32_t want, uint32_t (*sm)[3][kSelWaves],
+                                                    uint32_t* counts, uint32_t* tied, uint32_t* total, uint32_t* list) {
     const uint32_t tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c0 = a.sinks, c1 = n - a.recent;
     uint32_t k[kEach];
 #pragma unroll
     for (uint32_t i = 0; i < kEach; ++i) {
         const uint32_t e = i * kSelThreads + tid;
-        // 0 stands for what is no candidate, so the least candidate key is 1
         k[i] = __float_as_uint(e < n ? w[e] : 0.f);
     }
 #pragma unroll
     for (uint32_t i = 0; i < kEach; ++i) {
         const uint32_t e = i * kSelThreads + tid;
+        // 0 stands for what is no candidate, so the least candidate key is 1
         k[i] = e >= c0 && e < c1 ? max(weight_key(__uint_as_float(k[i])), 1u) : 0u;
     }
-    uint32_t thr = 0xffffffffu;
-    bool exact = true;
-    if (want)
-        thr = find_threshold(
-            [&](uint32_t c) {
-                uint32_t s = 0;
+    Search s = {0, 32, c1 - c0, 0, want};
+    uint32_t turn = 0;
+    auto count = [&](uint32_t c) {
+        uint32_t m = 0;
 #pragma unroll
-                for (uint32_t i = 0; i < kEach; ++i) s += (uint32_t)__popcll(__ballot(k[i] >= c));
-                return s;
-            },
-            want, sm, exact);
+        for (uint32_t i = 0; i < kEach; ++i) m += (uint32_t)__popcll(__ballot(k[i] >= c));
+        return m;
+    };
+    if (want) {
+        if (kEach * kSelThreads <= kListKeys) {
+            while (!s.done()) search_step<2>(s, count, sm, turn);
+        } else {
+            // until few keys are left in the range, then among those alone
+            while (!s.done() && s.lo - s.hi > kListKeys) search_step<1>(s, count, sm, turn);
+            if (!s.done()) {
+                if (tid == 0) *total = 0;
+                __syncthreads();
+#pragma unroll
+                for (uint32_t i = 0; i < kEach; ++i) append(list, total, s.holds(k[i]), k[i]);
+                __syncthreads();
+                search_list<kListKeys>(s, list, s.lo - s.hi, sm, turn);
+            }
+        }
+    }
+    const uint32_t thr = want ? s.x : 0xffffffffu;
+    const bool exact = !want || s.lo == want;
+    __syncthreads();
     const uint64_t below = (1ull << lane) - 1;
     uint32_t ties = 0xffffffffu;  // how many of the keys equal to thr are kept
     if (!exact) {
@@ -134,12 +196,11 @@ __device__ __forceinline__ void select_in_registers(const EvictArgs& a, const fl
             const uint32_t c = (uint32_t)__popcll(__ballot(k[i] == thr));
             if (lane == 0) tied[i * kSelWaves + wave] = c;
         }
-        __syncthreads();
-        if (lane == 0) sm[0][wave] = more;
+        if (lane == 0) sm[0][0][wave] = more;
         scan_counts<kEach * kSelWaves>(tied, total);
         uint32_t sum = 0;
 #pragma unroll
-        for (uint32_t i = 0; i < kSelWaves; ++i) sum += sm[0][i];
+        for (uint32_t i = 0; i < kSelWaves; ++i) sum += sm[0][0][i];
         ties = want - sum;
     }
     auto keep = [&](uint32_t i) {
@@ -171,7 +232,7 @@ __device__ __forceinline__ void select_in_registers(const EvictArgs& a, const fl
 }
 
 __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a, SeqView sq) {
-    __shared__ uint32_t sm[2][kSelWaves], counts[32 * kSelWaves], tied[32 * kSelWaves], total;
+    __shared__ uint32_t sm[2][3][kSelWaves], counts[32 * kSelWaves], tied[32 * kSelWaves], total, list[kListKeys];
     const uint32_t h = blockIdx.x, s = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const uint32_t n = seq_entries(sq, a.shift, s), m = min(n, a.budget);
     const float* w = a.w + (size_t)s * a.w_seq + (size_t)h * a.w_head;
@@ -188,8 +249,8 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a, SeqView
     }
     // here n > budget >= sinks + recent
     const uint32_t want = m - a.sinks - a.recent;
-    if (n <= 4 * kSelThreads) return select_in_registers<4>(a, w, wo, kept, n, want, sm, counts, tied, &total);
-    if (n <= 32 * kSelThreads) return select_in_registers<32>(a, w, wo, kept, n, want, sm, counts, tied, &total);
+    if (n <= kListKeys) return select_in_registers<kListKeys / kSelThreads>(a, w, wo, kept, n, want, sm, counts, tied, &total, list);
+    if (n <= 32 * kSelThreads) return select_in_registers<32>(a, w, wo, kept, n, want, sm, counts, tied, &total, list);
     // longer rows: each step reads the weights again (they stay in L2)
     const uint32_t c0 = a.sinks, c1 = n - a.recent;
     auto key = [&](uint32_t e) { return e >= c0 && e < c1 ? max(weight_key(w[e]), 1u) : 0u; };
@@ -201,16 +262,31 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a, SeqView
         }
         return c;
     };
-    uint32_t thr = 0xffffffffu, ties = 0xffffffffu;
-    bool exact = true;
-    if (want) thr = find_threshold([&](uint32_t c) { return count_if([c](uint32_t k) { return k >= c; }); }, want, sm, exact);
+    Search s_ = {0, 32, c1 - c0, 0, want};
+    uint32_t turn = 0, ties = 0xffffffffu;
+    if (want) {
+        while (!s_.done() && s_.lo - s_.hi > kListKeys)
+            search_step<1>(s_, [&](uint32_t c) { return count_if([c](uint32_t k) { return k >= c; }); }, sm, turn);
+        if (!s_.done()) {
+            if (tid == 0) total = 0;
+            __syncthreads();
+            for (uint32_t e0 = 0; e0 < n; e0 += kSelThreads) {
+                const uint32_t k = e0 + tid < n ? key(e0 + tid) : 0u;
+                append(list, &total, s_.holds(k), k);
+            }
+            __syncthreads();
+            search_list<kListKeys>(s_, list, s_.lo - s_.hi, sm, turn);
+        }
+    }
+    const uint32_t thr = want ? s_.x : 0xffffffffu;
+    const bool exact = !want || s_.lo == want;
     __syncthreads();
     if (!exact) {
         const uint32_t more = count_if([thr](uint32_t k) { return k > thr; });
-        if (lane == 0) sm[0][wave] = more;
+        if (lane == 0) sm[0][0][wave] = more;
         __syncthreads();
         uint32_t sum = 0;
-        for (uint32_t i = 0; i < kSelWaves; ++i) sum += sm[0][i];
+        for (uint32_t i = 0; i < kSelWaves; ++i) sum += sm[0][0][i];
         ties = want - sum;
         __syncthreads();
     }
