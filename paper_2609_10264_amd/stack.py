@@ -5,9 +5,10 @@ Every layer has seven projections of a 4096-wide decoder block:
 q, k, v, o (4096 x 4096), up, gate (11008 x 4096), down (4096 x 11008).
 Per layer and batch of B query columns the client encodes four inputs
 (q/k/v share one, up/gate share one), the server evaluates the seven products,
-and the client verifies and decrypts the seven responses.  The nonlinear
-operations between projections are outside this library: every input is a
-fresh synthetic query.
+and the client verifies and decrypts the seven responses.  In the schedules
+below every input is a fresh synthetic query; run_attention instead carries the
+values of an attention block through: the client's rotary positions, cache and
+attention (attention.py) between the projections q, k, v and o.
 
 Codes are shared per shape (one privacy code per input width n, one
 verification code per output height m); P^T and Q are per matrix.  This module
@@ -28,8 +29,9 @@ from dataclasses import dataclass, field
 
 import torch
 
-from . import (Code, Key, PackedW, Prepared, client_prepare_group, client_prepare_multi, decode_verify, decode_verify_masked_group, encode,
-               encode_masked, keygen, pack_weights, pack_weights_group, server_eval, server_eval_group)
+from . import (FIELD, Code, Key, KVCache, PackedW, Prepared, Sequences, client_prepare_group, client_prepare_multi,
+               decode_verify, decode_verify_masked_group, encode, encode_masked, keygen, pack_weights,
+               pack_weights_group, paged_attention, rotary_append, server_eval, server_eval_group)
 
 # (name, m, n, input group)
 PROJECTIONS = (
@@ -42,6 +44,7 @@ PROJECTIONS = (
     ("down", 4096, 11008, "mlp_out"),
 )
 INPUTS = ("attn_in", "attn_out", "mlp_in", "mlp_out")
+HEADS, HEAD_DIM = 32, 128  # of q, k and v
 
 
 @dataclass
@@ -130,6 +133,44 @@ def run_layer(layer: Layer, X: dict, ex: dict, ey: dict, tamper=None, stream=Non
                                      ey[name][0], ey[name][1], vL=vL, vR=vR, stream=stream)
         out[name] = (Y, acc, Xhat[group], Yhat, vL, vR)
     return out
+
+
+def run_attention(layer: Layer, X: torch.Tensor, ex: dict, ey: dict, cache: KVCache, seqs: Sequences,
+                  positions: torch.Tensor, rot: torch.Tensor, field_scale: float, out_scale: float,
+                  layout: str = "half", weights: torch.Tensor | None = None, tamper=None, stream=None):
+    """The attention block of one layer for the new tokens X (T x 4096 field
+    elements, one query column each, the sequences' tokens one after another):
+    q, k, v by delegation, rotary positions with the append of k and v to the
+    cache, attention over the sequences' entries, and o by delegation.
+
+    ex["attn_in"], ex["attn_out"]: noise (T x t_x); ey[name]: challenges.
+    cache, seqs: this layer's pools, and the sequences' tables, lengths (with the
+    new tokens) and starts; rot: rotary_table, read at `positions` (T).
+    field_scale: the value of 1 in the decrypted q, k, v (the weights' scale times
+    the queries'); out_scale: of 1 in the query of o.  weights: the entries'
+    collected attention weights (count x HEADS x width * page_size), updated.
+    Returns (Y_o, {name: (Y, accept, Xhat, Yhat)}): the values are only good if
+    every accept bit is set."""
+    T = X.shape[0]
+    res = {}
+
+    def delegate(group, x):
+        names = stage(group)
+        xh = encode(layer.keys[names[0]], x, ex[group][0], ex[group][1], stream=stream)
+        for name, yh in evaluate_stage(layer, group, xh, stream=stream).items():
+            if tamper is not None:
+                tamper(name, yh)
+            Y, acc, _, _ = decode_verify(layer.keys[name], xh, yh, ex[group][0], ex[group][1], ey[name][0],
+                                         ey[name][1], stream=stream)
+            res[name] = (Y, acc, xh, yh)
+
+    delegate("attn_in", X)
+    q, k, v = (res[name][0].view(T, HEADS, HEAD_DIM) for name in ("q", "k", "v"))
+    p = layer.keys["q"].p
+    q = rotary_append(q, k, v, positions, rot, cache, seqs, layout=layout, field_scale=field_scale, p=p, stream=stream)
+    x = paged_attention(q, cache, seqs, out_dtype=FIELD, field_scale=out_scale, weights=weights, p=p, stream=stream)
+    delegate("attn_out", x.view(T, HEADS * HEAD_DIM))
+    return res["o"][0], res
 
 
 def prepare_input(layer: Layer, group: str, ex: dict, ey: dict, preps: dict, flag: torch.Tensor | None = None,
@@ -328,5 +369,5 @@ def macs_per_layer(B: int) -> int:
 
 
 __all__ = ["PROJECTIONS", "INPUTS", "Layer", "LayerOutputs", "build_layer", "evaluate_stage", "check_stage",
-           "run_layer", "prepare_input", "prepare_layer", "run_layer_prepared", "run_pass_overlapped", "codes_for",
+           "run_layer", "run_attention", "HEADS", "HEAD_DIM", "prepare_input", "prepare_layer", "run_layer_prepared", "run_pass_overlapped", "codes_for",
            "input_width", "stage", "macs_per_layer", "Code"]
