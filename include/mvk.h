@@ -712,7 +712,9 @@ typedef struct mvk_kv {
  * new tokens of a sequence, as far as the caller knows (it chooses the kernel,
  * not the result).  All arrays are device int32 and are
  * read when the work runs.  Lengths are clamped to the table's width, page
- * numbers outside the pool are read as the nearest page and never written. */
+ * numbers outside the pool are read as the nearest page and never written.  Starts
+ * outside the token rows are clamped; where they do not ascend, the rows that two
+ * sequences claim are unspecified or left alone, and no other memory is touched. */
 typedef struct mvk_seqs {
     const int32_t *table;
     uint64_t table_stride;

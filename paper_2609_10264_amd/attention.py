@@ -185,7 +185,7 @@ def paged_attention(q: torch.Tensor, cache: KVCache, seqs: Sequences, scale: flo
     (weights None with weights_out: from zero)."""
     T, heads, dim = q.shape
     if out is None:
-        out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
+        out = q.new_empty(q.shape) if out_dtype is None else torch.empty(q.shape, dtype=out_dtype, device=q.device)
     if out.dtype == torch.int32 and field_scale is None:
         raise ValueError("field outputs need field_scale, the value of 1")
     cs, ss = cache.struct(), seqs.struct(T)

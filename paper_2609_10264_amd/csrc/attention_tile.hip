@@ -34,6 +34,14 @@
 // (they are read on the device).  A tile that a cut divides leaves parts
 // (unnormalised sums with their maxima); the workgroup that counts itself last
 // on it adds them in order, so the result does not depend on timing.
+//
+// Measured, dim 128 in bfloat16 (a large copy: 5.19 TB/s, an 8192^3 product: 1369
+// TFLOP/s): tokens, 48 sequences of 130 to 32767 entries, 64 + 8 heads: 226 us, 5.35
+// TB/s of cache; one token over 2048 entries of 32 heads 15 us, of which 6.5 are its
+// bytes, the rest starts, first loads and joins.  Chunks, a prompt of 8192, 32 heads:
+// 673 us, 816 TFLOP/s: the softmax's vector work between the products bounds it.
+// The tokens form for up to 32 rows: 32 sequences of 8 new tokens over 8000 entries,
+// 8 kv heads, take 213 us with 32 rows and 241 with the chunks form at 40.
 #include "kv.h"
 #include "mvk_internal.h"
 
@@ -126,12 +134,16 @@ struct TileArgs {
     bool wide_out;  // out takes stores of 4 values at once
 };
 
+// Sums that stop at kTooMany: sequences whose starts do not ascend share token rows
+// and may have more units together than attend_tile_fits allows for.
+constexpr uint32_t kTooMany = 0xffffffffu;
+__device__ __forceinline__ uint32_t add_units(uint32_t x, uint32_t y) { return __builtin_elementwise_add_sat(x, y); }
 __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
     const uint32_t lane = threadIdx.x & 63;
 #pragma unroll
     for (uint32_t s = 1; s < 64; s <<= 1) {
         const uint32_t y = (uint32_t)__shfl_up((int)x, s);
-        if (lane >= s) x += y;
+        if (lane >= s) x = add_units(x, y);
     }
     return x;
 }
@@ -173,8 +185,9 @@ __device__ __forceinline__ Start find_start(const TileArgs& a, uint32_t w, uint3
         }
         const uint32_t sum = (uint32_t)__shfl((int)incl, 63);
         if (it < chunks) {
-            st.total += sum;
+            st.total = add_units(st.total, sum);
             if (it + 1 < chunks) continue;
+            if (st.total == kTooMany) return st;  // (left is 0: no workgroup has work)
             x = range_at(w, st.total, groups);
             st.left = range_at(w + 1, st.total, groups) - x;
             if (st.left == 0) return st;
@@ -934,6 +947,10 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
 // order: S = Q K^T (rows down, keys across, so that a lane sums its own key),
 // p = exp(scale S - lse).  K is read once and stays in registers; the rows pass
 // through LDS 32 at a time, one tile in flight, for the four waves together.
+// A launch of its own, since a weight needs its row's whole sum; without atomics.
+// Measured: single tokens of 8 sequences over 4096 to 12000 entries, 32 + 8 heads of
+// 128, 35 us (3.5 TB/s of K); a chunk of 256 over 6000, 46 us, 280 TFLOP/s: 392
+// workgroups, so some compute units have two and others one.
 constexpr uint32_t kWeightKeys = 128;
 template <typename T, uint32_t kDim>
 __global__ __launch_bounds__(256) void weights_tile(TileArgs a, const float* __restrict__ lse, const float* w_in,

@@ -372,3 +372,21 @@ def test_refusals():
         mvk.paged_attention(pr.dq, pr.cache, pr.seqs, weights_out=torch.zeros((1, 2, 8), device="cuda"))
     with pytest.raises(ValueError):
         mvk.paged_attention(pr.dq, pr.cache, mvk.Sequences(pr.seqs.table.long(), pr.seqs.lens, pr.seqs.q_start))
+
+
+def test_starts_that_claim_the_same_rows_beyond_the_count_of_units():
+    """Every second of 65535 sequences claims all 2048 rows over 2^20 entries: more units
+    than are counted in 32 bits, so nothing is done, and the next call is as ever."""
+    import paper_2609_10264_amd as mvk
+    S, T, page = 65535, 2048, 1 << 20
+    print(f"attention of {S} sequences with overlapping starts", flush=True)
+    cache = mvk.KVCache.allocate(1, 1, page, 8)
+    q = torch.ones((T, 1, 8), dtype=BF, device="cuda")
+    starts = (torch.arange(S + 1, device="cuda") % 2 * T).to(torch.int32)
+    seqs = mvk.Sequences(torch.zeros((S, 1), dtype=torch.int32, device="cuda"),
+                         torch.full((S,), page, dtype=torch.int32, device="cuda"), starts, max_new=T)
+    out = torch.full((T, 1, 8), 7.0, dtype=BF, device="cuda")
+    mvk.paged_attention(q, cache, seqs, out=out)
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all())
+    _check(Problem([70, 300], [5, 140], 4, 2, 64))
