@@ -807,7 +807,7 @@ mvk_status mvk_paged_attention(const mvk_rows *q, uint32_t T, uint32_t heads, co
  *   w          : count x kv_heads x (a row of at least width * page_size) floats, strides w_seq, w_head
  *   w_out      : NULL, or the kept entries' weights (rows of at least budget, strides o_seq, o_head)
  *   kept       : count x kv_heads x budget int32, the kept entries' indices, -1 beyond m
- *   lens_out   : count int32, m of each sequence
+ *   lens_out   : count int32, m of each sequence; may be seqs->lens
  * dst has src's type, kv_heads, dim and any page size; dst_width * page_size of
  * dst is at least min(budget, width * page_size of src).  seqs->q_start is not used.
  * Errors: MVK_EINVAL (sinks + recent > budget, budget 0, mismatched caches),

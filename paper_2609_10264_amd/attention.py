@@ -228,7 +228,7 @@ def cache_evict(cache: KVCache, seqs: Sequences, weights: torch.Tensor, dst: KVC
     kv_heads x width * page_size), copied in order into dst_table's pages of dst,
     their weights into weights_out.  Returns (kept, lens): the kept entries'
     indices (count x kv_heads x budget, -1 beyond) and how many each sequence
-    has now."""
+    has now (lens_out, which may be seqs.lens)."""
     cs, ds, ss = cache.struct(), dst.struct(), seqs.struct(0)
     dev = weights.device
     if kept is None:

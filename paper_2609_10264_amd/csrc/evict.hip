@@ -34,7 +34,6 @@ struct EvictArgs {
     size_t o_seq, o_head;
     uint32_t budget, recent, sinks, shift;  // shift: of src
     int32_t* kept;
-    int32_t* lens_out;
 };
 
 // Where a search stands: the want-th largest of the candidates' keys lies in
@@ -242,7 +241,6 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a, SeqView
     const float* w = a.w + (size_t)s * a.w_seq + (size_t)h * a.w_head;
     float* wo = a.wo ? a.wo + (size_t)s * a.o_seq + (size_t)h * a.o_head : nullptr;
     int32_t* kept = a.kept + ((size_t)s * gridDim.x + h) * a.budget;
-    if (h == 0 && tid == 0) a.lens_out[s] = (int32_t)m;
     for (uint32_t i = m + tid; i < a.budget; i += kSelThreads) kept[i] = -1;
     if (n <= a.budget) {
         for (uint32_t i = tid; i < n; i += kSelThreads) {
@@ -330,29 +328,48 @@ struct CopyArgs {
     SeqView sq;             // of src
     const int32_t* dtable;
     size_t dts;
-    uint32_t dwidth, budget;
+    uint32_t dwidth, budget, most;  // most: rows that a sequence may keep
     const int32_t* kept;
+    int32_t* lens_out;
 };
 
 // kRowsEach rows a group of threads that holds one, T (an element or a 16-byte
 // granule) a thread; their loads are in flight together.  dims: T's a row.
+// How many rows there are is read from `kept` (-1 beyond them), not from the
+// lengths: lens_out, written here, may be their place.
 constexpr uint32_t kRowsEach = 4;
 template <typename T>
 __global__ __launch_bounds__(256) void evict_copy(CopyArgs a, uint32_t dims, uint32_t per) {
     const uint32_t h = blockIdx.y, s = blockIdx.z;
-    const uint32_t m = min(seq_entries(a.sq, a.src.shift, s), a.budget);
     const uint32_t group = threadIdx.x / per, rows = 256 / per;  // rows at once: per threads each
     const uint32_t r0 = blockIdx.x * rows * kRowsEach + group;
-    if (group >= rows || r0 >= m) return;
+    if (group >= rows || r0 >= a.most) return;
     const int32_t* kept = a.kept + ((size_t)s * gridDim.y + h) * a.budget;
+    int32_t at[kRowsEach];
+#pragma unroll
+    for (uint32_t u = 0; u < kRowsEach; ++u) {
+        const uint32_t r = r0 + u * rows;
+        at[u] = r < a.most ? kept[r] : -1;
+    }
+    if (h == 0 && threadIdx.x % per == 0) {
+        // of each sequence one thread finds the last row, or that there is none
+#pragma unroll
+        for (uint32_t u = 0; u < kRowsEach; ++u) {
+            const uint32_t r = r0 + u * rows;
+            if (at[u] >= 0 && (r + 1 == a.most || kept[r + 1] < 0)) a.lens_out[s] = (int32_t)(r + 1);
+            if (at[u] < 0 && r == 0) a.lens_out[s] = 0;
+        }
+    }
+    if (at[0] < 0) return;
     size_t ks[kRowsEach], vs[kRowsEach], kd[kRowsEach], vd[kRowsEach];
     bool on[kRowsEach];
 #pragma unroll
     for (uint32_t u = 0; u < kRowsEach; ++u) {
-        const uint32_t r = r0 + u * rows, e = (uint32_t)kept[min(r, m - 1)], slot = min(r, m - 1) >> a.dst.shift;
+        const uint32_t r = at[u] < 0 ? r0 : r0 + u * rows, e = (uint32_t)(at[u] < 0 ? at[0] : at[u]);
+        const uint32_t slot = r >> a.dst.shift;
         const uint32_t sp = seq_page(a.sq, a.src, s, e), se = e & ((1u << a.src.shift) - 1);
         const int32_t dp = slot < a.dwidth ? a.dtable[(size_t)s * a.dts + slot] : -1;
-        on[u] = r < m && dp >= 0 && (uint32_t)dp < a.dst.pages;
+        on[u] = at[u] >= 0 && dp >= 0 && (uint32_t)dp < a.dst.pages;
         const uint32_t de = r & ((1u << a.dst.shift) - 1);
         ks[u] = sp * a.src.kp + h * a.src.kh + se * a.src.ke;
         vs[u] = sp * a.src.vp + h * a.src.vh + se * a.src.ve;
@@ -389,13 +406,13 @@ hipError_t launch_evict(const KvView& src, const SeqView& sq, size_t elem, const
                         uint32_t budget, uint32_t recent, uint32_t sinks, const KvView& dst, const int32_t* dtable,
                         size_t dts, uint32_t dwidth, float* wo, size_t o_seq, size_t o_head, int32_t* kept,
                         int32_t* lens_out, hipStream_t s) {
-    const EvictArgs e = {w, w_seq, w_head, wo, o_seq, o_head, budget, recent, sinks, src.shift, kept, lens_out};
+    const EvictArgs e = {w, w_seq, w_head, wo, o_seq, o_head, budget, recent, sinks, src.shift, kept};
     hipLaunchKernelGGL(evict_select, dim3(src.heads, sq.count), dim3(kSelThreads), 0, s, e, sq);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
     const uint64_t cap = (uint64_t)sq.width << src.shift;
     const uint32_t most = (uint32_t)(cap < budget ? cap : budget);
-    CopyArgs c = {src, dst, sq, dtable, dts, dwidth, budget, kept};
+    CopyArgs c = {src, dst, sq, dtable, dts, dwidth, budget, most, kept, lens_out};
     auto go = [&](auto kernel, uint32_t dims) {
         uint32_t per = 1;
         while (per < dims && per < 256) per *= 2;

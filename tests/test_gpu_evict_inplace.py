@@ -1,0 +1,55 @@
+"""Eviction whose outputs take the place of its inputs (mvk_cache_evict)."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+BF, I32 = torch.bfloat16, torch.int32
+
+
+class Case:
+    """Two long rows and two that keep all, of more heads than run at once."""
+    lens, hk, dim, page, budget = [2000, 1500, 70, 0], 700, 8, 16, 100
+
+    def __init__(self):
+        import paper_2609_10264_amd as mvk
+        g = torch.Generator(device="cuda").manual_seed(4)
+        S, width = len(self.lens), 125
+        self.table = torch.randperm(S * width, generator=g, device="cuda").to(I32).view(S, width)
+        self.cache = mvk.KVCache(*(torch.randn((S * width, self.hk, self.page, self.dim), generator=g, device="cuda").to(BF)
+                                   for _ in range(2)))
+        self.w = torch.rand((S, self.hk, width * self.page), generator=g, device="cuda")
+        self.dtable = torch.arange(S * 7, dtype=I32, device="cuda").view(S, 7)
+
+    def seqs(self):
+        import paper_2609_10264_amd as mvk
+        return mvk.Sequences(self.table, torch.tensor(self.lens, dtype=I32, device="cuda"))
+
+    def dst(self):
+        import paper_2609_10264_amd as mvk
+        return mvk.KVCache.allocate(28, self.hk, self.page, self.dim)
+
+
+def test_lengths_in_place():
+    """Every head chooses by the lengths before the call, whichever head is first."""
+    import paper_2609_10264_amd as mvk
+    c = Case()
+    want_dst, dst, seqs = c.dst(), c.dst(), c.seqs()
+    want, want_lens = mvk.cache_evict(c.cache, c.seqs(), c.w, want_dst, c.dtable, c.budget, recent=9, sinks=2)
+    kept, lens = mvk.cache_evict(c.cache, seqs, c.w, dst, c.dtable, c.budget, recent=9, sinks=2, lens_out=seqs.lens)
+    torch.cuda.synchronize()
+    assert lens is seqs.lens and lens.tolist() == want_lens.tolist() == [100, 100, 70, 0]
+    assert torch.equal(kept, want)
+    assert torch.equal(dst.K, want_dst.K) and torch.equal(dst.V, want_dst.V)
+    # the choice itself, of a late head: the heaviest but for the protected
+    for h in (0, 699):
+        others = c.w[0, h, 2:1991].cpu()
+        top = (others.topk(100 - 11).indices + 2).sort().values.tolist()
+        assert kept[0, h].tolist() == [0, 1] + top + list(range(1991, 2000))
