@@ -805,12 +805,14 @@ mvk_status mvk_paged_attention(const mvk_rows *q, uint32_t T, uint32_t heads, co
  * (dst_table: count x dst_width), which share no memory with the pages read:
  * pages of a common prefix may belong to several sequences, so none is altered.
  *   w          : count x kv_heads x (a row of at least width * page_size) floats, strides w_seq, w_head
- *   w_out      : NULL, or the kept entries' weights (rows of at least budget, strides o_seq, o_head)
+ *   w_out      : NULL, or the kept entries' weights (rows of at least budget, strides o_seq,
+ *                o_head); shares no memory with w
  *   kept       : count x kv_heads x budget int32, the kept entries' indices, -1 beyond m
  *   lens_out   : count int32, m of each sequence; may be seqs->lens
  * dst has src's type, kv_heads, dim and any page size; dst_width * page_size of
  * dst is at least min(budget, width * page_size of src).  seqs->q_start is not used.
- * Errors: MVK_EINVAL (sinks + recent > budget, budget 0, mismatched caches),
+ * Errors: MVK_EINVAL (sinks + recent > budget, budget 0, mismatched caches, w_out in w's
+ * memory: rows that meet where both have the same strides, else extents that do),
  * MVK_ERANGE (dim > MVK_MAX_HEAD_DIM, count or kv_heads > 65535, buffers above 2^62 bytes).
  */
 mvk_status mvk_cache_evict(const mvk_kv *src, const mvk_seqs *seqs, const float *w, uint64_t w_seq, uint64_t w_head,

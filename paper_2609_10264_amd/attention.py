@@ -226,9 +226,9 @@ def cache_evict(cache: KVCache, seqs: Sequences, weights: torch.Tensor, dst: KVC
     """Keep at most `budget` entries of every sequence and kv head: the first
     `sinks`, the last `recent` and the heaviest others by `weights` (count x
     kv_heads x width * page_size), copied in order into dst_table's pages of dst,
-    their weights into weights_out.  Returns (kept, lens): the kept entries'
-    indices (count x kv_heads x budget, -1 beyond) and how many each sequence
-    has now (lens_out, which may be seqs.lens)."""
+    their weights into weights_out (in no memory of weights).  Returns (kept,
+    lens): the kept entries' indices (count x kv_heads x budget, -1 beyond) and
+    how many each sequence has now (lens_out, which may be seqs.lens)."""
     cs, ds, ss = cache.struct(), dst.struct(), seqs.struct(0)
     dev = weights.device
     if kept is None:

@@ -1235,6 +1235,31 @@ inline bool span_too_big(uint64_t a, uint64_t sa, uint64_t b, uint64_t sb, uint6
     return a * sa + b * sb > (1ull << 62) / elem;
 }
 
+// Rows of `len` bytes at p + i*s0 + j*s1 (bytes), i < n0, j < n1, below 2^62 bytes in all.
+struct RowSet {
+    const void* p;
+    uint64_t n0, s0, n1, s1, len;
+    uint64_t begin() const { return (uint64_t)(uintptr_t)p; }
+    uint64_t end() const { return begin() + (n0 - 1) * s0 + (n1 - 1) * s1 + len; }
+};
+
+// Do rows of a and b share memory?  Exact where the strides are the same, as those
+// of interleaved views of one buffer are; with others, where their extents meet.
+bool share_memory(const RowSet& a, const RowSet& b) {
+    if (!a.n0 || !a.n1 || !b.n0 || !b.n1) return false;
+    if (a.end() <= b.begin() || b.end() <= a.begin()) return false;
+    if (a.s0 != b.s0 || a.s1 != b.s1 || (a.n1 | b.n1) > 65536u) return true;
+    const int64_t d = (int64_t)(b.begin() - a.begin()), s0 = (int64_t)a.s0, s1 = (int64_t)a.s1;
+    // rows (i, j) of b and (k, l) of a meet if d + (i - k) s0 + (j - l) s1 lies in (-b.len, a.len)
+    for (int64_t dj = 1 - (int64_t)a.n1; dj < (int64_t)b.n1; ++dj) {
+        const int64_t x = d + dj * s1, low = -(int64_t)b.len - x;  // di s0 has to exceed low
+        int64_t di = 1 - (int64_t)a.n0;
+        if (s0) di = std::max(di, (low >= 0 ? low / s0 : -((-low + s0 - 1) / s0)) + 1);
+        if (di < (int64_t)b.n0 && di * s0 > low && x + di * s0 < (int64_t)a.len) return true;
+    }
+    return false;
+}
+
 mvk_status check_rows(const mvk_rows* r, uint64_t T, uint64_t heads) {
     if (!r || (!r->data && T) || r->type < MVK_TYPE_BF16 || r->type > MVK_TYPE_FIELD) return MVK_EINVAL;
     if ((uintptr_t)r->data % type_size(r->type) != 0) return MVK_EINVAL;
@@ -1402,6 +1427,10 @@ mvk_status mvk_cache_evict(const mvk_kv* src, const mvk_seqs* seqs, const float*
         span_too_big(seqs->count, o_seq, src->kv_heads, o_head, 4) || too_big(seqs->count, dst_table_stride, 4) ||
         too_big((uint64_t)seqs->count * src->kv_heads, budget, 4))
         return MVK_ERANGE;
+    // kept weights are read again while others are written
+    if (w_out && share_memory({w, seqs->count, 4 * w_seq, src->kv_heads, 4 * w_head, 4 * cap},
+                              {w_out, seqs->count, 4 * o_seq, src->kv_heads, 4 * o_head, 4 * most}))
+        return MVK_EINVAL;
     return hip_status(launch_evict(view_of(src), view_of(seqs), type_size(src->type), w, w_seq, w_head, budget, recent,
                                    sinks, view_of(dst), dst_table, dst_table_stride, dst_width, w_out, o_seq, o_head,
                                    kept, lens_out, (hipStream_t)stream));

@@ -1,0 +1,39 @@
+"""Outputs in an input's memory that a call cannot write without changing its own
+results are refused, and views of one buffer that do not meet are taken (the
+library's host side; nothing is computed)."""
+from tests.test_host_dispatch import host  # noqa: F401
+
+STRUCTS = """
+def rows(data, type_=0, token=1024, head=128): return L.MvkRows(data, type_, token, head)
+def kv(heads=4, dim=128):
+    K, V = ptr(), ptr()
+    return L.MvkKv(K, V, 0, 8, heads, 16, dim, heads * 16 * dim, 16 * dim, dim, heads * 16 * dim, 16 * dim, dim)
+def seqs(count=2): return L.MvkSeqs(ptr(), 4, count, 4, ptr(), ptr(), 1)
+"""
+
+
+def test_eviction_weights(host):  # noqa: F811
+    out = host(STRUCTS + """
+w = ptr()
+def call(wo, o_seq=256, o_head=64, w_seq=256, w_head=64):
+    src, dst, sq = kv(), kv(), seqs()
+    rec.rec_reset()
+    st = lib.mvk_cache_evict(ref(src), ref(sq), w, w_seq, w_head, 20, 4, 4, ref(dst), ptr(), 2, 2, wo, o_seq, o_head,
+                             ptr(), ptr(), None)
+    return [st, rec.rec_count()]
+result["itself"] = call(w)
+result["a row on"] = call(w + 4 * 64)
+result["one float before its end"] = call(w + 4 * (2 * 256 - 1))
+result["behind it"] = call(w + 4 * 2 * 256)
+result["the last float of w_out"] = call(w - 4 * (256 + 3 * 64 + 19))
+result["before it"] = call(w - 4 * (256 + 3 * 64 + 20))
+# views of one buffer, count x 2 x heads x 64 and count x heads x 2 x 64
+result["seqs interleaved"] = call(w + 4 * 256, o_seq=512, w_seq=512)
+result["heads interleaved"] = call(w + 4 * 64, o_seq=512, o_head=128, w_seq=512, w_head=128)
+result["heads interleaved, a float short"] = call(w + 4 * 63, o_seq=512, o_head=128, w_seq=512, w_head=128)
+result["other strides"] = call(w + 4 * 64, o_seq=1024, o_head=128, w_seq=512, w_head=128)
+""")
+    refused, done = [-1, 0], [0, 2]  # (MVK_EINVAL)
+    assert out == {"itself": refused, "a row on": refused, "one float before its end": refused, "behind it": done,
+                   "the last float of w_out": refused, "before it": done, "seqs interleaved": done,
+                   "heads interleaved": done, "heads interleaved, a float short": refused, "other strides": refused}

@@ -53,3 +53,19 @@ def test_lengths_in_place():
         others = c.w[0, h, 2:1991].cpu()
         top = (others.topk(100 - 11).indices + 2).sort().values.tolist()
         assert kept[0, h].tolist() == [0, 1] + top + list(range(1991, 2000))
+
+
+def test_weights_in_place_are_refused():
+    import paper_2609_10264_amd as mvk
+    c = Case()
+    before = c.w.clone()
+    with pytest.raises(mvk.MvkError):
+        mvk.cache_evict(c.cache, c.seqs(), c.w, c.dst(), c.dtable, c.budget, weights_out=c.w)
+    assert torch.equal(c.w, before)
+    # another part of the same buffer is no overlap
+    both = torch.zeros((4, 2, c.hk, 2000), device="cuda")
+    both[:, 0] = c.w
+    kept, _ = mvk.cache_evict(c.cache, c.seqs(), both[:, 0], c.dst(), c.dtable, c.budget, weights_out=both[:, 1])
+    for s, m in enumerate((100, 100, 70, 0)):
+        assert torch.equal(both[s, 1, :, :m], c.w[s].gather(1, kept[s, :, :m].long()))
+    assert torch.equal(both[:, 0], c.w)
