@@ -782,15 +782,18 @@ mvk_status mvk_rotary_append(const mvk_rows *q, const mvk_rows *k, const mvk_row
  *   out        : T x heads x dim: BF16, F16, F32, or FIELD: o / field_scale
  *                rounded to the nearest integer and embedded in F_p (a
  *                magnitude above (p-1)/2 is clamped to it).  Rows that belong
- *                to no sequence are left alone.
+ *                to no sequence are left alone.  out may be q itself (same type and
+ *                strides) where w_out is NULL, and else shares no memory with it.
  *   lse        : NULL, or T x heads floats: ln sum_j exp(scale q . k_j), -inf for a row without entries
  *   w_out      : NULL, or the entries' collected weights, count x kv_heads x (a row
  *                of at least width * page_size): entry j of the sequence gets
  *                (j < n - c ? w_in : 0) + the sum of p_j over the sequence's new
  *                tokens and the kv head's query heads; places j >= n are left alone.
- *                w_in: same strides, NULL for zeros, may be w_out.
+ *                w_in: same strides, NULL for zeros, may be w_out (and else
+ *                shares no memory with it).
  * Sums have a fixed order: the same inputs give the same bits.
- * Errors: MVK_EINVAL, MVK_ERANGE (dim > MVK_MAX_HEAD_DIM, buffers above 2^62
+ * Errors: MVK_EINVAL (also out in q's memory and w_out in w_in's, but for the cases above:
+ * rows that meet where both have the same strides, else extents that do), MVK_ERANGE (dim > MVK_MAX_HEAD_DIM, buffers above 2^62
  * bytes, T * heads above 2^31 - 1), MVK_ENOMEM, MVK_ECAPTURE (workspace).
  */
 mvk_status mvk_paged_attention(const mvk_rows *q, uint32_t T, uint32_t heads, const mvk_kv *cache,

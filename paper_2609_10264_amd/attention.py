@@ -179,7 +179,7 @@ def paged_attention(q: torch.Tensor, cache: KVCache, seqs: Sequences, scale: flo
     """Attention of the new tokens q (T x heads x dim, already in the cache as
     keys and values) over their sequences' entries.  scale: dim ** -0.5 by
     default.  out_dtype: q's by default, float32, or FIELD: out / field_scale
-    rounded into the field.  lse: T x heads float32, written.  weights,
+    rounded into the field; out may be q where no weights are collected.  lse: T x heads float32, written.  weights,
     weights_out (count x kv_heads x width * page_size float32; may be one
     tensor): the attention weight every entry has collected, before and after
     (weights None with weights_out: from zero)."""

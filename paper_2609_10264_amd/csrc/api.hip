@@ -1260,6 +1260,11 @@ bool share_memory(const RowSet& a, const RowSet& b) {
     return false;
 }
 
+RowSet row_set(const mvk_rows* r, uint64_t T, uint64_t heads, uint64_t dim) {
+    const uint64_t e = type_size(r->type);
+    return {r->data, T, e * r->token, heads, e * r->head, e * dim};
+}
+
 mvk_status check_rows(const mvk_rows* r, uint64_t T, uint64_t heads) {
     if (!r || (!r->data && T) || r->type < MVK_TYPE_BF16 || r->type > MVK_TYPE_FIELD) return MVK_EINVAL;
     if ((uintptr_t)r->data % type_size(r->type) != 0) return MVK_EINVAL;
@@ -1380,6 +1385,15 @@ mvk_status mvk_paged_attention(const mvk_rows* q, uint32_t T, uint32_t heads, co
     if (w_in && !w_out) return MVK_EINVAL;
     if (w_out && ((cache->kv_heads > 1 && w_head < cap) || (seqs->count > 1 && w_seq < cap))) return MVK_EINVAL;
     if (w_out && span_too_big(seqs->count, w_seq, cache->kv_heads, w_head, 4)) return MVK_ERANGE;
+    // in place only element for element (a row's queries are read before its result is
+    // written), and not with weights, for which the queries are read again
+    if ((w_out || q->data != out->data || q->type != out->type || q->token != out->token || q->head != out->head) &&
+        share_memory(row_set(q, T, heads, cache->dim), row_set(out, T, heads, cache->dim)))
+        return MVK_EINVAL;
+    if (w_in && w_in != w_out &&
+        share_memory({w_in, seqs->count, 4 * w_seq, cache->kv_heads, 4 * w_head, 4 * cap},
+                     {w_out, seqs->count, 4 * w_seq, cache->kv_heads, 4 * w_head, 4 * cap}))
+        return MVK_EINVAL;
     if (T == 0 && !w_out) return MVK_OK;
     hipStream_t s = (hipStream_t)stream;
     const Rows rq = view_of(q), ro = view_of(out);

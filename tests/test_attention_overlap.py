@@ -37,3 +37,36 @@ result["other strides"] = call(w + 4 * 64, o_seq=1024, o_head=128, w_seq=512, w_
     assert out == {"itself": refused, "a row on": refused, "one float before its end": refused, "behind it": done,
                    "the last float of w_out": refused, "before it": done, "seqs interleaved": done,
                    "heads interleaved": done, "heads interleaved, a float short": refused, "other strides": refused}
+
+
+def test_attention_in_the_memory_of_its_queries(host):  # noqa: F811
+    out = host(STRUCTS + """
+q = ptr()
+def call(o, type_=0, token=1024, head=128, wo=None, wi=None, q_token=1024, q_head=128, dim=128, heads=8):
+    cache, sq = kv(dim=dim), seqs()
+    rec.rec_reset()
+    st = lib.mvk_paged_attention(ref(rows(q, 0, q_token, q_head)), 3, heads, ref(cache), ref(sq), 0.1,
+                                 ref(rows(o, type_, token, head)), 1.0, None, wi, wo, 256, 64, None)
+    return [st, rec.rec_count() > 0]
+call(ptr(), wo=ptr())  # (the workspace's own launches)
+w = ptr()
+for dim in (128, 100):  # both kernels
+    r = result[str(dim)] = {}
+    r["apart"] = call(ptr(), dim=dim), call(ptr(), dim=dim, wo=w)
+    r["itself"] = call(q, dim=dim), call(q, dim=dim, wo=w)
+    r["another type"] = call(q, type_=1, dim=dim), call(q, type_=2, dim=dim)
+    r["other strides"] = call(q, token=2048, dim=dim), call(q, head=256, token=2048, dim=dim)
+    r["a head on"] = call(q + 256, dim=dim), call(q + 256, dim=dim, wo=w)
+    r["a token before"] = call(q - 2048, dim=dim), call(q - 2048, dim=dim, wo=w)
+    # q and out as parts of one row of heads, and as halves of one head
+    r["beside"] = [call(q + 2048, token=2048, q_token=2048, dim=dim, wo=x) for x in (None, w)]
+    r["beside, a head short"] = [call(q + 2048 - 256, token=2048, q_token=2048, dim=dim, wo=x) for x in (None, w)]
+    r["halves"] = [call(q + 256, token=2048, head=256, q_token=2048, q_head=256, dim=dim, wo=x) for x in (None, w)]
+result["w"] = [call(ptr(), wo=w, wi=x) for x in (w, None, ptr(), w + 4, w + 4 * 64, w - 4 * 64, w + 4 * 512)]
+""")
+    no, yes = [-1, False], [0, True]
+    for dim in ("128", "100"):
+        assert out[dim] == {"apart": [yes, yes], "itself": [yes, no], "another type": [no, no],
+                            "other strides": [no, no], "a head on": [no, no], "a token before": [no, no],
+                            "beside": [yes, yes], "beside, a head short": [no, no], "halves": [yes, yes]}, dim
+    assert out["w"] == [yes, yes, yes, no, no, no, yes]
