@@ -25,6 +25,7 @@ streams, every data dependence of an inference pass kept as a stream edge).
 """
 from __future__ import annotations
 
+from contextlib import nullcontext
 from dataclasses import dataclass, field
 
 import torch
@@ -148,11 +149,16 @@ def run_attention(layer: Layer, X: torch.Tensor, ex: dict, ey: dict, cache: KVCa
     new tokens) and starts; rot: rotary_table, read at `positions` (T).
     field_scale: the value of 1 in the decrypted q, k, v (the weights' scale times
     the queries'); out_scale: of 1 in the query of o.  weights: the entries'
-    collected attention weights (count x HEADS x width * page_size), updated.
+    collected attention weights (count x HEADS x width * page_size).
     Returns (Y_o, {name: (Y, accept, Xhat, Yhat)}): the values are only good if
-    every accept bit is set."""
+    every accept bit is set.  Otherwise `weights` is as before the call (decided on
+    the device), the cache differs in the new tokens' entries alone, and the call
+    may be made again with the same arguments."""
     T = X.shape[0]
     res = {}
+
+    def on_stream():
+        return torch.cuda.stream(stream) if stream is not None else nullcontext()
 
     def delegate(group, x):
         names = stage(group)
@@ -168,8 +174,22 @@ def run_attention(layer: Layer, X: torch.Tensor, ex: dict, ey: dict, cache: KVCa
     q, k, v = (res[name][0].view(T, HEADS, HEAD_DIM) for name in ("q", "k", "v"))
     p = layer.keys["q"].p
     q = rotary_append(q, k, v, positions, rot, cache, seqs, layout=layout, field_scale=field_scale, p=p, stream=stream)
-    x = paged_attention(q, cache, seqs, out_dtype=FIELD, field_scale=out_scale, weights=weights, p=p, stream=stream)
+    collected = None
+    if weights is not None:
+        with on_stream():
+            collected = torch.empty_strided(weights.shape, weights.stride(), dtype=weights.dtype, device=weights.device)
+            collected.copy_(weights)
+    x = paged_attention(q, cache, seqs, out_dtype=FIELD, field_scale=out_scale, weights=weights, weights_out=collected,
+                        p=p, stream=stream)
     delegate("attn_out", x.view(T, HEADS * HEAD_DIM))
+    if weights is not None:
+        with on_stream():
+            # seen[1]: some bit is not set (a fill by index: library sums clear scratch
+            # memory in a way that a captured graph must not)
+            seen = torch.zeros(2, device=weights.device)
+            for _, accept, _, _ in res.values():
+                seen.index_fill_(0, (accept != 1).long(), 1.0)
+            weights.copy_(torch.where(seen[1] == 0, collected, weights))
     return res["o"][0], res
 
 
