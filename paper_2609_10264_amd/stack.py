@@ -173,14 +173,16 @@ def run_attention(layer: Layer, X: torch.Tensor, ex: dict, ey: dict, cache: KVCa
     delegate("attn_in", X)
     q, k, v = (res[name][0].view(T, HEADS, HEAD_DIM) for name in ("q", "k", "v"))
     p = layer.keys["q"].p
-    q = rotary_append(q, k, v, positions, rot, cache, seqs, layout=layout, field_scale=field_scale, p=p, stream=stream)
-    collected = None
-    if weights is not None:
-        with on_stream():
+    # (what does not outlive the call belongs to the stream that uses it)
+    with on_stream():
+        q = rotary_append(q, k, v, positions, rot, cache, seqs, layout=layout, field_scale=field_scale, p=p,
+                          stream=stream)
+        collected = None
+        if weights is not None:
             collected = torch.empty_strided(weights.shape, weights.stride(), dtype=weights.dtype, device=weights.device)
             collected.copy_(weights)
-    x = paged_attention(q, cache, seqs, out_dtype=FIELD, field_scale=out_scale, weights=weights, weights_out=collected,
-                        p=p, stream=stream)
+        x = paged_attention(q, cache, seqs, out_dtype=FIELD, field_scale=out_scale, weights=weights,
+                            weights_out=collected, p=p, stream=stream)
     delegate("attn_out", x.view(T, HEADS * HEAD_DIM))
     if weights is not None:
         with on_stream():
