@@ -10,6 +10,8 @@
 // The search is a chain of compares, counts and barriers on one compute unit a row:
 // 12.7 us for 32 rows of 4096, 43 for 96 rows of up to 32768.  The copy is bound by
 // memory: 138 us for 660 MB (8191 kept of each of those rows), 4.8 TB/s.
+#include <algorithm>
+
 #include "kv.h"
 #include "mvk_internal.h"
 
@@ -342,53 +344,54 @@ template <typename T>
 __global__ __launch_bounds__(256) void evict_copy(CopyArgs a, uint32_t dims, uint32_t per) {
     const uint32_t h = blockIdx.y, s = blockIdx.z;
     const uint32_t group = threadIdx.x / per, rows = 256 / per;  // rows at once: per threads each
-    const uint32_t r0 = blockIdx.x * rows * kRowsEach + group;
-    if (group >= rows || r0 >= a.most) return;
+    if (group >= rows) return;
     const int32_t* kept = a.kept + ((size_t)s * gridDim.y + h) * a.budget;
-    int32_t at[kRowsEach];
-#pragma unroll
-    for (uint32_t u = 0; u < kRowsEach; ++u) {
-        const uint32_t r = r0 + u * rows;
-        at[u] = r < a.most ? kept[r] : -1;
-    }
-    if (h == 0 && threadIdx.x % per == 0) {
-        // of each sequence one thread finds the last row, or that there is none
+    for (uint32_t r0 = blockIdx.x * rows * kRowsEach + group; r0 < a.most; r0 += gridDim.x * rows * kRowsEach) {
+        int32_t at[kRowsEach];
 #pragma unroll
         for (uint32_t u = 0; u < kRowsEach; ++u) {
             const uint32_t r = r0 + u * rows;
-            if (at[u] >= 0 && (r + 1 == a.most || kept[r + 1] < 0)) a.lens_out[s] = (int32_t)(r + 1);
-            if (at[u] < 0 && r == 0) a.lens_out[s] = 0;
+            at[u] = r < a.most ? kept[r] : -1;
         }
-    }
-    if (at[0] < 0) return;
-    size_t ks[kRowsEach], vs[kRowsEach], kd[kRowsEach], vd[kRowsEach];
-    bool on[kRowsEach];
+        if (h == 0 && threadIdx.x % per == 0) {
+            // of each sequence one thread finds the last row, or that there is none
 #pragma unroll
-    for (uint32_t u = 0; u < kRowsEach; ++u) {
-        const uint32_t r = at[u] < 0 ? r0 : r0 + u * rows, e = (uint32_t)(at[u] < 0 ? at[0] : at[u]);
-        const uint32_t slot = r >> a.dst.shift;
-        const uint32_t sp = seq_page(a.sq, a.src, s, e), se = e & ((1u << a.src.shift) - 1);
-        const int32_t dp = slot < a.dwidth ? a.dtable[(size_t)s * a.dts + slot] : -1;
-        on[u] = at[u] >= 0 && dp >= 0 && (uint32_t)dp < a.dst.pages;
-        const uint32_t de = r & ((1u << a.dst.shift) - 1);
-        ks[u] = sp * a.src.kp + h * a.src.kh + se * a.src.ke;
-        vs[u] = sp * a.src.vp + h * a.src.vh + se * a.src.ve;
-        kd[u] = dp * a.dst.kp + h * a.dst.kh + de * a.dst.ke;
-        vd[u] = dp * a.dst.vp + h * a.dst.vh + de * a.dst.ve;
-    }
-    for (uint32_t c = threadIdx.x % per; c < dims; c += per) {
-        T k[kRowsEach], v[kRowsEach];
+            for (uint32_t u = 0; u < kRowsEach; ++u) {
+                const uint32_t r = r0 + u * rows;
+                if (at[u] >= 0 && (r + 1 == a.most || kept[r + 1] < 0)) a.lens_out[s] = (int32_t)(r + 1);
+                if (at[u] < 0 && r == 0) a.lens_out[s] = 0;
+            }
+        }
+        if (at[0] < 0) return;  // (none of the later rows has one)
+        size_t ks[kRowsEach], vs[kRowsEach], kd[kRowsEach], vd[kRowsEach];
+        bool on[kRowsEach];
 #pragma unroll
         for (uint32_t u = 0; u < kRowsEach; ++u) {
-            k[u] = ((const T*)a.src.K)[ks[u] + c];
-            v[u] = ((const T*)a.src.V)[vs[u] + c];
+            const uint32_t r = at[u] < 0 ? r0 : r0 + u * rows, e = (uint32_t)(at[u] < 0 ? at[0] : at[u]);
+            const uint32_t slot = r >> a.dst.shift;
+            const uint32_t sp = seq_page(a.sq, a.src, s, e), se = e & ((1u << a.src.shift) - 1);
+            const int32_t dp = slot < a.dwidth ? a.dtable[(size_t)s * a.dts + slot] : -1;
+            on[u] = at[u] >= 0 && dp >= 0 && (uint32_t)dp < a.dst.pages;
+            const uint32_t de = r & ((1u << a.dst.shift) - 1);
+            ks[u] = sp * a.src.kp + h * a.src.kh + se * a.src.ke;
+            vs[u] = sp * a.src.vp + h * a.src.vh + se * a.src.ve;
+            kd[u] = dp * a.dst.kp + h * a.dst.kh + de * a.dst.ke;
+            vd[u] = dp * a.dst.vp + h * a.dst.vh + de * a.dst.ve;
         }
+        for (uint32_t c = threadIdx.x % per; c < dims; c += per) {
+            T k[kRowsEach], v[kRowsEach];
 #pragma unroll
-        for (uint32_t u = 0; u < kRowsEach; ++u)
-            if (on[u]) {
-                ((T*)a.dst.K)[kd[u] + c] = k[u];
-                ((T*)a.dst.V)[vd[u] + c] = v[u];
+            for (uint32_t u = 0; u < kRowsEach; ++u) {
+                k[u] = ((const T*)a.src.K)[ks[u] + c];
+                v[u] = ((const T*)a.src.V)[vs[u] + c];
             }
+#pragma unroll
+            for (uint32_t u = 0; u < kRowsEach; ++u)
+                if (on[u]) {
+                    ((T*)a.dst.K)[kd[u] + c] = k[u];
+                    ((T*)a.dst.V)[vd[u] + c] = v[u];
+                }
+        }
     }
 }
 
@@ -417,7 +420,9 @@ hipError_t launch_evict(const KvView& src, const SeqView& sq, size_t elem, const
         uint32_t per = 1;
         while (per < dims && per < 256) per *= 2;
         const uint32_t each = 256 / per * kRowsEach;
-        hipLaunchKernelGGL(kernel, dim3((most + each - 1) / each, src.heads, sq.count), dim3(256), 0, s, c, dims, per);
+        // (one launch takes fewer than 2^32 threads an axis)
+        const dim3 grid(std::min((most + each - 1) / each, 1u << 22), src.heads, sq.count);
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, c, dims, per);
         return hipGetLastError();
     };
     const uint32_t per = (uint32_t)(16 / elem);

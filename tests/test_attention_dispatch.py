@@ -35,3 +35,22 @@ for T, heads in ((3, 5), (2**20, 16), (2**20, 64), (2**25, 63), (2**31 - 1, 1)):
     for name, (st, launches) in out.items():
         assert st == 0 and [x[0] for x in launches] == ["attend_any"] and launches[0][2], (name, launches)
     assert out["3 x 5"][1][0][1] == 4
+
+
+def test_rows_of_the_eviction(host):  # noqa: F811
+    """Up to 2^31 - 1 kept entries in launches of fewer than 2^32 threads."""
+    out = host(STRUCTS + """
+def evict(n, dim, page):
+    K, V = ptr() + 2, ptr() + 2  # (no 16-byte rows)
+    width = -(-n // page)
+    src = L.MvkKv(K, V, 0, 8, 1, page, dim, *((page * dim, page * dim, dim) * 2))
+    sq = seqs(1, width, 0)
+    rec.rec_reset()
+    return [lib.mvk_cache_evict(ref(src), ref(sq), ptr(), n, n, n, 0, 0, ref(src), ptr(), width, width, None, 0, 0,
+                                ptr(), ptr(), None), grids()]
+for n, dim in ((100, 512), (2**25, 512), (2**26 + 1, 512), (2**30, 300), (2**31 - 2**20, 1)):
+    result[f"{n} of {dim}"] = evict(n, dim, 2**20 if n > 100 else 16)
+""")
+    for name, (st, launches) in out.items():
+        assert st == 0 and [x[0].split("(")[0] for x in launches] == ["evict_select", "evict_copy"], (name, launches)
+        assert all(x[2] for x in launches), (name, launches)
