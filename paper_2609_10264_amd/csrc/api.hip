@@ -1400,8 +1400,9 @@ mvk_status mvk_paged_attention(const mvk_rows* q, uint32_t T, uint32_t heads, co
     const KvView kv = view_of(cache);
     const SeqView sq = view_of(seqs);
     const float inv_scale = out->type == MVK_TYPE_FIELD ? 1.f / field_scale : 1.f;
-    const bool tile = attend_tile_fits(rq, T, heads, kv, sq);
-    const bool split = attend_tile_split(std::min(seqs->max_new, T), heads, kv);
+    const bool split = attend_tile_split(std::min(seqs->max_new, T), heads, kv) &&
+                       attend_tile_fits(rq, T, heads, kv, sq, true);
+    const bool tile = split || attend_tile_fits(rq, T, heads, kv, sq, false);
     const size_t lse_bytes = w_out && !lse ? align_up((size_t)T * heads * sizeof(float)) : 0;
     const size_t bytes = lse_bytes + (tile ? attend_tile_bytes(kv, split) : 0);
     void* ws = nullptr;

@@ -1,5 +1,6 @@
 // Attention over a paged cache on the matrix cores: 16-bit values, dims that
-// are multiples of 8 up to 256, 16-byte aligned rows.
+// are multiples of 8 up to 256, 16-byte aligned rows, units counted in 32 bits
+// (units_fit).
 //
 // New token i (of c) of a sequence of n entries sees entries j <= n - c + i:
 //   o = sum_j p_j v_j,   p_j = exp(x_j - max) / sum,   x_j = scale q . k_j.
@@ -44,6 +45,7 @@
 // 8 kv heads, take 213 us with 32 rows and 241 with the chunks form at 40.
 #include "kv.h"
 #include "mvk_internal.h"
+#include "units.h"
 
 namespace mvk {
 
@@ -74,51 +76,6 @@ struct Mma<_Float16> {
     static constexpr uint32_t kExp = 0x7c00u;
 };
 
-// sum_{i < n} floor((a i + b) / m), by the Euclidean descent; a n + b and the
-// sum are below 2^32 (attend_tile_fits).
-__device__ __forceinline__ uint32_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
-    uint32_t sum = 0;
-#pragma unroll 1
-    for (;;) {
-        const uint32_t qa = a / m, qb = b / m;
-        sum += (uint32_t)((uint64_t)n * (n - 1) / 2) * qa + n * qb;
-        a -= qa * m;
-        b -= qb * m;
-        const uint32_t y = a * n + b;
-        if (y < m) return sum;
-        n = y / m;
-        b = y - n * m;
-        const uint32_t t = m;
-        m = a;
-        a = t;
-    }
-}
-
-// The tiles of one sequence (the same for each of its kv heads).  A tile has a
-// unit for every kUnit keys and, before them, kExtra units without keys: what
-// its beginning and end cost besides.
-template <uint32_t kRows, uint32_t kUnit, uint32_t kExtra>
-struct Tiles {
-    uint32_t c, n, base, count, last;  // base: entries before the new tokens; last: units of the last tile
-    uint32_t grp;
-    __device__ Tiles(const SeqSpan& sp, uint32_t grp) : c(sp.c), n(sp.n), grp(grp) {
-        base = n > c ? n - c : 0;
-        count = (c * grp + kRows - 1) / kRows;
-        last = (base + c + kUnit - 1) / kUnit + kExtra;
-    }
-    // units of tile t: its last row is a row of token ((t + 1) kRows - 1) / grp
-    __device__ uint32_t units(uint32_t t) const {
-        if (t + 1 >= count) return last;
-        return (base + ((t + 1) * kRows - 1) / grp + kUnit) / kUnit + kExtra;
-    }
-    // units of the tiles before t (t < count)
-    __device__ uint32_t before(uint32_t t) const {
-        if (t == 0) return 0;
-        return floor_sum(t, grp * kUnit, kRows, grp * (base + kUnit) + kRows - 1) + t * kExtra;
-    }
-    __device__ uint32_t all() const { return count == 0 ? 0 : before(count - 1) + last; }
-};
-
 struct TileArgs {
     Rows q, out;
     KvView kv;
@@ -135,7 +92,7 @@ struct TileArgs {
 };
 
 // Sums that stop at kTooMany: sequences whose starts do not ascend share token rows
-// and may have more units together than attend_tile_fits allows for.
+// and may have more units together than units_fit allows for.
 constexpr uint32_t kTooMany = 0xffffffffu;
 __device__ __forceinline__ uint32_t add_units(uint32_t x, uint32_t y) { return __builtin_elementwise_add_sat(x, y); }
 __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
@@ -180,7 +137,10 @@ __device__ __forceinline__ Start find_start(const TileArgs& a, uint32_t w, uint3
         const uint32_t s0 = 64 * (it < chunks ? it : it - chunks), s = s0 + lane;
         if (chunks > 1 || it == 0) {
             u = 0;
-            if (s < a.sq.count) u = Tiles<kRows, kUnit, kExtra>(seq_span(a.sq, a.kv.shift, s, a.tokens), a.grp).all() * hk;
+            if (s < a.sq.count) {
+                const SeqSpan sp = seq_span(a.sq, a.kv.shift, s, a.tokens);
+                u = Tiles<kRows, kUnit, kExtra>(sp.c, sp.n, a.grp).all() * hk;
+            }
             incl = wave_scan(u);
         }
         const uint32_t sum = (uint32_t)__shfl((int)incl, 63);
@@ -201,7 +161,8 @@ __device__ __forceinline__ Start find_start(const TileArgs& a, uint32_t w, uint3
             const uint32_t per = us / hk, in = x - before;
             st.kh = in / per;
             st.unit = in % per;
-            const Tiles<kRows, kUnit, kExtra> t(seq_span(a.sq, a.kv.shift, st.s, a.tokens), a.grp);
+            const SeqSpan sp = seq_span(a.sq, a.kv.shift, st.s, a.tokens);
+            const Tiles<kRows, kUnit, kExtra> t(sp.c, sp.n, a.grp);
             // the last tile whose units begin at or before that: 64 candidates at a time
             uint32_t lo = 0, hi = t.count, first = 0;
 #pragma unroll 1
@@ -575,7 +536,7 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
         uint32_t lane = tid & 63;
         asm volatile("" : "+v"(lane));
         const uint32_t col = lane & 31, half = lane >> 5;
-        const Tiles<Sh::kRows, Sh::kUnit, Sh::kExtra> tiles(sp, a.grp);
+        const Tiles<Sh::kRows, Sh::kUnit, Sh::kExtra> tiles(sp.c, sp.n, a.grp);
         const uint32_t units = tiles.units(st.tile);
         const uint32_t u0 = st.unit, u1 = min(units, u0 + (st.left - done));
 
@@ -1083,14 +1044,16 @@ inline bool in16(const void* p, size_t a, size_t b, size_t c) { return (uintptr_
 
 }  // namespace
 
-bool attend_tile_fits(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq) {
+bool attend_tile_fits(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq, bool split) {
     if ((q.type != MVK_TYPE_BF16 && q.type != MVK_TYPE_F16) || kv.dim % 8 || kv.dim > 256 || tokens == 0) return false;
     if (!in16(q.p, q.token, q.head, 0) || !in16(kv.K, kv.kp, kv.kh, kv.ke) || !in16(kv.V, kv.vp, kv.vh, kv.ve))
         return false;
-    // units (64 keys at least) of tiles (32 rows at least) are counted in 32 bits
-    const uint64_t grp = heads / kv.heads, rows = tokens * grp, seen = ((uint64_t)sq.width << kv.shift) + tokens + 256;
-    if (seen * grp + rows + 256 >= (1ull << 32)) return false;
-    return rows / 32 + sq.count < (1ull << 31) / (seen / 64 + 8) / kv.heads;
+    const uint64_t cap = (uint64_t)sq.width << kv.shift;
+    if ((cap + kWeightKeys - 1) / kWeightKeys * 256 >= (1ull << 32)) return false;  // threads of the weights' launch
+    typedef Shape<__bf16, 128, true> Tokens;  // (rows and units are the same for every type and dim)
+    typedef Shape<__bf16, 128, false> Chunks;
+    return split ? units_fit<Tokens::kRows, Tokens::kUnit, Tokens::kExtra>(tokens, heads / kv.heads, kv.heads, sq.count, cap)
+                 : units_fit<Chunks::kRows, Chunks::kUnit, Chunks::kExtra>(tokens, heads / kv.heads, kv.heads, sq.count, cap);
 }
 
 size_t attend_tile_bytes(const KvView& kv, bool split) {

@@ -293,7 +293,7 @@ hipError_t launch_weights_any(const Rows& q, uint32_t tokens, uint32_t heads, co
 // form for few rows a sequence and kv head (max_new says how many; either form
 // is right for every problem).  ws: attend_tile_bytes, 16-byte aligned;
 // counters: attend_tile_ctrl_bytes, zero before the launch and left at zero.
-bool attend_tile_fits(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq);
+bool attend_tile_fits(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq, bool split);
 bool attend_tile_split(uint32_t max_new, uint32_t heads, const KvView& kv);
 size_t attend_tile_bytes(const KvView& kv, bool split);
 size_t attend_tile_ctrl_bytes();

@@ -11,8 +11,9 @@ def grids():
     g, out = (ctypes.c_uint32 * 3)(), []
     for i in range(rec.rec_count()):
         rec.rec_grid(i, g)
-        out.append([rec.rec_name(i).decode().replace("void ", "").replace("mvk::(anonymous namespace)::", "").split("<")[0],
-                    g[0], g[0] * g[2] < 2**32])
+        name = rec.rec_name(i).decode()  # (not every type's name is known to the demangler)
+        kernels = ("attend_any", "attend_tile", "weights_any", "weights_tile", "evict_select", "evict_copy")
+        out.append([next((k for k in kernels if k in name), name), g[0], g[0] * g[2] < 2**32])
     return out
 def attend(T, heads, kv_heads, dim, type_=0, count=1, width=4, page=16, max_new=None, w=None):
     cache, sq = kv(kv_heads, dim, type_, page), seqs(count, width, T if max_new is None else max_new)
@@ -52,5 +53,30 @@ for n, dim in ((100, 512), (2**25, 512), (2**26 + 1, 512), (2**30, 300), (2**31 
     result[f"{n} of {dim}"] = evict(n, dim, 2**20 if n > 100 else 16)
 """)
     for name, (st, launches) in out.items():
-        assert st == 0 and [x[0].split("(")[0] for x in launches] == ["evict_select", "evict_copy"], (name, launches)
+        assert st == 0 and [x[0] for x in launches] == ["evict_select", "evict_copy"], (name, launches)
+        assert all(x[2] for x in launches), (name, launches)
+
+
+def test_large_batches_run_on_the_matrix_cores(host):  # noqa: F811
+    """The tile kernels take what their counts hold, by the units that sequences can have
+    in a table of that width, not by all token rows over all token rows."""
+    out = host(STRUCTS + """
+w = ptr()
+for name, kw in {
+    "64 prompts of 8192": dict(T=64 * 8192, count=64, width=128, page=64, max_new=8192),
+    "a prompt of 200000": dict(T=200000, width=3125, page=64),
+    "a prompt of 262144": dict(T=262144, heads=32, kv_heads=32, width=4096, page=64),
+    "few prompts, wide table": dict(T=65536, count=8, width=1 << 14, page=64, max_new=8192),
+    "65535 single tokens": dict(T=65535, count=65535, width=512, page=64, max_new=1),
+    "the hint too small": dict(T=64 * 8192, count=64, width=128, page=64, max_new=1),
+    "2^20 by 2^20 of 64 heads": dict(T=1 << 20, width=1 << 14, page=64),
+    "2^31 - 1 entries": dict(T=1, heads=1, kv_heads=1, width=0x7fffffff, page=1),
+}.items():
+    kw = dict(dict(heads=64, kv_heads=8, dim=128), **kw)
+    result[name] = attend(w=w, **kw)
+""")
+    for name, (st, launches) in out.items():
+        tile = name not in ("2^20 by 2^20 of 64 heads", "2^31 - 1 entries")
+        assert st == 0, name
+        assert [x[0] for x in launches] == (["attend_tile", "weights_tile"] if tile else ["attend_any", "weights_any"]), name
         assert all(x[2] for x in launches), (name, launches)
