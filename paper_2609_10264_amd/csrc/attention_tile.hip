@@ -1072,9 +1072,10 @@ namespace {
 TileArgs tile_args(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq, float scale) {
     TileArgs a = {};
     a.q = q, a.kv = kv, a.sq = sq, a.tokens = tokens, a.heads = heads, a.grp = heads / kv.heads;
-    // the sign goes to q; a scale of zero as one that no score survives, so that masked places stay at -inf
+    // the sign goes to q; a scale of zero as the least number above it, which no score
+    // survives, so that masked places stay at -inf
     const float mag = scale < 0 ? -scale : scale;
-    a.sl2 = mag < 1e-30f ? 1e-30f : mag * kLog2e;
+    a.sl2 = fmaxf(mag * kLog2e, 0x1p-149f);
     a.flip = scale < 0 ? 0x80008000u : 0u;
     return a;
 }
