@@ -394,14 +394,20 @@ __device__ const u32x4 kZeroGranule = {0, 0, 0, 0};
 // from an address a lane, or from a base that the wave shares and an offset a
 // lane.  By hand: with the builtin every later LDS read waits for all loads in
 // flight, which ends the overlap.  The compiler does not count these loads;
-// wait_loads comes before their data is read.  (m0 is written and used inside
-// the statement; nothing else in this file uses it.)
+// wait_loads comes before their data is read.
 __device__ __forceinline__ void load_lds(const void* from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(uniform(to)) : "memory");
+    uint32_t saved;  // (the compiler may hold something in m0, which cannot be named as clobbered)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved)
+                 : "v"(from), "s"(uniform(to))
+                 : "memory");
 }
 __device__ __forceinline__ void load_lds(const void* base, uint32_t offset, uint32_t to) {
     const uint64_t b = (uint64_t)base, s = (uint64_t)uniform((uint32_t)(b >> 32)) << 32 | uniform((uint32_t)b);
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(s), "s"(uniform(to))
+    uint32_t saved;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved)
+                 : "v"(offset), "s"(s), "s"(uniform(to))
                  : "memory");
 }
 // All but the kNewest last loads of this wave have landed.  (The builtin, unlike
