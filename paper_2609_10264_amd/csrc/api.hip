@@ -1243,13 +1243,16 @@ struct RowSet {
     uint64_t end() const { return begin() + (n0 - 1) * s0 + (n1 - 1) * s1 + len; }
 };
 
-// Do rows of a and b share memory?  Exact where the strides are the same, as those
-// of interleaved views of one buffer are; with others, where their extents meet.
+// Do rows of a and b share memory?  Exact where the strides are the same (or one side has
+// no second row to use its own), as those of interleaved views of one buffer are; with
+// others, where their extents meet.
 bool share_memory(const RowSet& a, const RowSet& b) {
     if (!a.n0 || !a.n1 || !b.n0 || !b.n1) return false;
     if (a.end() <= b.begin() || b.end() <= a.begin()) return false;
-    if (a.s0 != b.s0 || a.s1 != b.s1 || (a.n1 | b.n1) > 65536u) return true;
-    const int64_t d = (int64_t)(b.begin() - a.begin()), s0 = (int64_t)a.s0, s1 = (int64_t)a.s1;
+    if ((a.n0 > 1 && b.n0 > 1 && a.s0 != b.s0) || (a.n1 > 1 && b.n1 > 1 && a.s1 != b.s1) || (a.n1 | b.n1) > 65536u)
+        return true;
+    const int64_t d = (int64_t)(b.begin() - a.begin());
+    const int64_t s0 = (int64_t)(a.n0 > 1 ? a.s0 : b.s0), s1 = (int64_t)(a.n1 > 1 ? a.s1 : b.s1);
     // rows (i, j) of b and (k, l) of a meet if d + (i - k) s0 + (j - l) s1 lies in (-b.len, a.len)
     for (int64_t dj = 1 - (int64_t)a.n1; dj < (int64_t)b.n1; ++dj) {
         const int64_t x = d + dj * s1, low = -(int64_t)b.len - x;  // di s0 has to exceed low

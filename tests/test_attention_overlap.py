@@ -70,3 +70,27 @@ result["w"] = [call(ptr(), wo=w, wi=x) for x in (w, None, ptr(), w + 4, w + 4 * 
                             "other strides": [no, no], "a head on": [no, no], "a token before": [no, no],
                             "beside": [yes, yes], "beside, a head short": [no, no], "halves": [yes, yes]}, dim
     assert out["w"] == [yes, yes, yes, no, no, no, yes]
+
+
+def test_strides_that_no_second_row_uses(host):  # noqa: F811
+    """One token, or one head: its stride says nothing, whatever a view happens to have."""
+    out = host(STRUCTS + """
+def call(T, heads, q, q_token, q_head, o, token, head):
+    cache, sq = kv(heads=1), seqs()
+    rec.rec_reset()
+    w = ptr()
+    st = lib.mvk_paged_attention(ref(rows(q, 0, q_token, q_head)), T, heads, ref(cache), ref(sq), 0.1,
+                                 ref(rows(o, 0, token, head)), 1.0, None, None, w, 64, 64, None)
+    return st
+call(1, 1, ptr(), 128, 128, ptr(), 128, 128)
+q = ptr()
+# q and out as the halves of each token's row of two heads
+result["one head"] = [call(3, 1, q, 256, x, q + 256, 256, y) for x, y in ((128, 128), (0, 256), (256, 128), (1 << 20, 0))]
+result["one head, meeting"] = [call(3, 1, q, 256, x, q + 254, 256, y) for x, y in ((128, 128), (1 << 20, 0))]
+# of one token, every second head
+result["one token"] = [call(1, 4, q, x, 256, q + 256, y, 256) for x, y in ((1024, 1024), (0, 1 << 30), (128, 512))]
+result["one token, meeting"] = [call(1, 4, q, x, 256, q + 512, y, 256) for x, y in ((1024, 1024), (128, 512))]
+result["one row"] = [call(1, 1, q, 7, 9, q + x, 11, 13) for x in (256, 254, -254, -256)]
+""")
+    assert out == {"one head": [0] * 4, "one head, meeting": [-1] * 2, "one token": [0] * 3,
+                   "one token, meeting": [-1] * 2, "one row": [0, -1, -1, 0]}
