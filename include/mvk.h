@@ -758,7 +758,8 @@ mvk_status mvk_rotary_table(uint32_t rot, uint32_t rows, double base, int32_t sc
  * is outside the pool, is not written).
  *   q, q_out       : T x heads x dim; both NULL: keys and values only.  q_out
  *                    may be q itself (same type and strides) and else shares
- *                    no memory with an input.
+ *                    no memory with an input (MVK_EINVAL where rows of q, k or v
+ *                    with its strides meet it, or extents of others).
  *   k, v           : T x cache->kv_heads x cache->dim, types as q's or others;
  *                    NULL (with cache and seqs): queries only.
  *   field_scale    : value of 1 in field inputs.

@@ -1352,7 +1352,8 @@ mvk_status mvk_rotary_append(const mvk_rows* q, const mvk_rows* k, const mvk_row
         if ((st = check_rows(q, T, heads)) || (st = check_rows(q_out, T, heads))) return st;
         if (!is_float_type(q_out->type)) return MVK_EINVAL;
         // in place only element for element
-        if (q->data == q_out->data && (q->type != q_out->type || q->token != q_out->token || q->head != q_out->head))
+        if ((q->data != q_out->data || q->type != q_out->type || q->token != q_out->token || q->head != q_out->head) &&
+            share_memory(row_set(q, T, heads, dim), row_set(q_out, T, heads, dim)))
             return MVK_EINVAL;
     }
     if (k) {
@@ -1360,6 +1361,10 @@ mvk_status mvk_rotary_append(const mvk_rows* q, const mvk_rows* k, const mvk_row
         if ((st = check_rows(k, T, cache->kv_heads)) || (st = check_rows(v, T, cache->kv_heads))) return st;
         if (cache->dim != dim || k->type != v->type) return MVK_EINVAL;
         if (q && (q->type != k->type || q_out->type != cache->type)) return MVK_EINVAL;
+        // k and v are read while q_out is written
+        const RowSet out = q ? row_set(q_out, T, heads, dim) : RowSet{};
+        if (share_memory(row_set(k, T, cache->kv_heads, dim), out) || share_memory(row_set(v, T, cache->kv_heads, dim), out))
+            return MVK_EINVAL;
     }
     const int src = q ? q->type : k->type, dst = q ? q_out->type : cache->type;
     if (src == MVK_TYPE_FIELD && !std::isfinite(field_scale)) return MVK_EINVAL;

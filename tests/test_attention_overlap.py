@@ -94,3 +94,30 @@ result["one row"] = [call(1, 1, q, 7, 9, q + x, 11, 13) for x in (256, 254, -254
 """)
     assert out == {"one head": [0] * 4, "one head, meeting": [-1] * 2, "one token": [0] * 3,
                    "one token, meeting": [-1] * 2, "one row": [0, -1, -1, 0]}
+
+
+def test_rotary_in_the_memory_of_its_inputs(host):  # noqa: F811
+    out = host(STRUCTS + """
+def call(q, k, v, o, type_=0, o_type=0, token=1024, q_token=1024, kv_heads=4, kv_head=128):
+    cache, sq = kv(heads=kv_heads), seqs()
+    rec.rec_reset()
+    st = lib.mvk_rotary_append(ref(rows(q, type_, q_token)), ref(rows(k, type_, q_token, kv_head)),
+                               ref(rows(v, type_, q_token, kv_head)), 3, 8, 128, 128, 0, ptr(), ptr(), 100, 1.0,
+                               ref(rows(o, o_type, token)), ref(cache), ref(sq), None)
+    return [st, rec.rec_count() > 0]
+q, k, v = ptr(), ptr(), ptr()
+result["apart"] = call(q, k, v, ptr())
+result["itself"] = call(q, k, v, q)
+result["itself, another type"] = call(q, k, v, q, type_=2)
+result["itself, other strides"] = call(q, k, v, q, token=2048)
+result["shifted"] = [call(q, k, v, q + x) for x in (256, -2048, 2 * 3 * 1024 - 2)]
+result["k, v"] = [call(q, k, v, k), call(q, k, v, v - 2048)]
+# q, k and v parts of one row (8 + 4 + 4 heads of 128), q rotated in place
+result["one row"] = call(q, q + 2048, q + 3072, q, token=2048, q_token=2048)
+result["one row of one kv head"] = [call(q, q + 2048, q + 2304, q, token=1280, q_token=1280, kv_heads=1, kv_head=x) for x in (128, 1280)]
+result["a row into its keys"] = call(q, q + 2048, q + 3072, q + 2048, token=2048, q_token=2048)
+""")
+    no, yes = [-1, False], [0, True]
+    assert out == {"apart": yes, "itself": yes, "itself, another type": no, "itself, other strides": no,
+                   "shifted": [no, no, no], "k, v": [no, no], "one row": yes, "one row of one kv head": [yes, yes],
+                   "a row into its keys": no}
