@@ -677,7 +677,9 @@ mvk_status mvk_decode_verify_seeded(const mvk_key *key, const mvk_st *st, const 
  * Values are floats (types below) or, where a call says so, field elements of
  * fixed-point numbers: the centred residue (p - x stands for -x) times a scale.
  * Unlike the rest of this library these calls round; sums, softmax statistics
- * and angles are held in 32 bits or more, every output is rounded once.
+ * and angles are held in 32 bits or more, every output is rounded once.  The
+ * softmax's weights are rounded to a 16-bit cache's type before the product with
+ * the values (mvk_paged_attention), whatever the output's type is.
  */
 #define MVK_TYPE_BF16 0
 #define MVK_TYPE_F16 1
@@ -760,8 +762,8 @@ mvk_status mvk_rotary_table(uint32_t rot, uint32_t rows, double base, int32_t sc
  *                    may be q itself (same type and strides) and else shares
  *                    no memory with an input (MVK_EINVAL where rows of q, k or v
  *                    with its strides meet it, or extents of others).
- *   k, v           : T x cache->kv_heads x cache->dim, types as q's or others;
- *                    NULL (with cache and seqs): queries only.
+ *   k, v           : T x cache->kv_heads x cache->dim, of one type (q's where
+ *                    there is a q); NULL (with cache and seqs): queries only.
  *   field_scale    : value of 1 in field inputs.
  * Types: inputs any, q_out BF16, F16 or F32, equal to the cache's where both are given.
  * Errors: MVK_EINVAL, MVK_ERANGE (dim > MVK_MAX_HEAD_DIM, buffers above 2^62 bytes).
