@@ -46,3 +46,38 @@ def test_memory_of_a_late_stream_is_left_alone(layer):  # noqa: F811
     got, _ = call(there, side)
     assert torch.equal(got, want) and torch.equal(there.w, here.w)
     assert torch.equal(there.cache.K, here.cache.K) and torch.equal(there.cache.V, here.cache.V)
+
+
+def test_two_streams_at_once():
+    """Calls in flight together on two streams, each with its own workspace and counters:
+    tiles of several workgroups in both, results as one after the other."""
+    import paper_2609_10264_amd as mvk
+    from tests.test_gpu_attention import Problem
+    problems = [Problem([9000, 70, 700], [1, 1, 1], 16, 2, 128, page=32).device(),
+                Problem([5003, 260], [150, 260], 8, 2, 64, page=16, seed=2).device()]
+
+    def call(pr, stream=None):
+        lse = torch.zeros(pr.q.shape[:2], device="cuda")
+        w = torch.zeros((len(pr.lens), 2, pr.cap), device="cuda")
+        out = torch.zeros_like(pr.dq)
+        torch.cuda.synchronize()
+
+        def go():
+            mvk.paged_attention(pr.dq, pr.cache, pr.seqs, out=out, lse=lse, weights_out=w, stream=stream)
+        go()
+        torch.cuda.synchronize()
+        return out, lse, w, go
+
+    want = [call(pr)[:3] for pr in problems]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [call(pr, s) for pr, s in zip(problems, streams)]
+    for _ in range(20):
+        for *outs, go in got:
+            for _ in range(3):
+                go()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+            for x in a[:3]:
+                x.zero_()
+        torch.cuda.synchronize()
