@@ -402,13 +402,18 @@ __device__ __forceinline__ void load_lds(const void* from, uint32_t to) {
                  : "v"(from), "s"(uniform(to))
                  : "memory");
 }
-__device__ __forceinline__ void load_lds(const void* base, uint32_t offset, uint32_t to) {
-    const uint64_t b = (uint64_t)base, s = (uint64_t)uniform((uint32_t)(b >> 32)) << 32 | uniform((uint32_t)b);
+__device__ __forceinline__ uint64_t uniform(const void* p) {
+    const uint64_t x = (uint64_t)p;
+    return (uint64_t)uniform((uint32_t)(x >> 32)) << 32 | uniform((uint32_t)x);
+}
+// Two loads, to `to` and 1024 bytes on (in one statement, so that m0 is saved once).
+__device__ __forceinline__ void load_lds(const void* base0, uint32_t offset0, const void* base1, uint32_t offset1, uint32_t to) {
     uint32_t saved;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
+                 "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %4\n\ts_mov_b32 m0, %0"
                  : "=&s"(saved)
-                 : "v"(offset), "s"(s), "s"(uniform(to))
-                 : "memory");
+                 : "v"(offset0), "s"(uniform(base0)), "v"(offset1), "s"(uniform(base1)), "s"(uniform(to))
+                 : "memory", "scc");
 }
 // All but the kNewest last loads of this wave have landed.  (The builtin, unlike
 // assembly, tells the compiler that its own loads have: it would wait for them
@@ -574,11 +579,13 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
                 // a base that the wave shares, and 32-bit offsets of which a few differ
                 const uint32_t pg = (uint32_t)__builtin_amdgcn_readlane((int)ids, (int)((j0 >> a.kv.shift) - id0));
                 const char* b = base + ((size_t)pg * page_stride + (size_t)(j0 & mask) * entry_stride) * sizeof(T);
+                auto from = [&](uint32_t i) { return b + (size_t)(kStep * i * (uint32_t)entry_stride * sizeof(T)); };
+                auto offset = [&](uint32_t i) {
+                    return (uint32_t)((lane_row * (uint32_t)entry_stride + 8 * granule(is_v, kStep * i + lane_row)) * sizeof(T));
+                };
+                static_assert(Sh::kLoads % 2 == 0, "two at a time");
 #pragma unroll
-                for (uint32_t i = 0; i < Sh::kLoads; ++i)
-                    load_lds(b + (size_t)(kStep * i * (uint32_t)entry_stride * sizeof(T)),
-                             (uint32_t)((lane_row * (uint32_t)entry_stride + 8 * granule(is_v, kStep * i + lane_row)) * sizeof(T)),
-                             to + 1024 * i);
+                for (uint32_t i = 0; i < Sh::kLoads; i += 2) load_lds(from(i), offset(i), from(i + 1), offset(i + 1), to + 1024 * i);
             } else {
                 const uint32_t used = (sp.n - 1) >> a.kv.shift;
 #pragma unroll 1
