@@ -87,7 +87,9 @@ class Sequences:
     """The sequences of a call: table (count x width int32 page numbers), lens
     (count, entries with the new ones), q_start (count + 1, where each one's new
     tokens begin; not needed for eviction).  max_new: an upper bound of the new
-    tokens of one sequence (None: the call's token rows)."""
+    tokens of one sequence (None: the call's token rows).  It chooses attention's
+    kernel, not its result: give 1 for a batch of single tokens, which without it
+    runs the form for chunks (32 sequences over 8000 entries: 238 us for 191)."""
     table: torch.Tensor
     lens: torch.Tensor
     q_start: torch.Tensor | None = None

@@ -17,8 +17,11 @@
 // already in the layout of the second operand of O^T = V^T P^T, up to an order
 // of the 16 keys of a product, which V^T's reads follow; V is stored by rows
 // and transposed by the LDS read.  The running maximum and sum are 32-bit; P is
-// rounded to the cache's type (relative 2^-9 each, independent, below the
-// output's own rounding on average).
+// rounded to the cache's type, as the second product takes it (relative 2^-8 in
+// bfloat16 and 2^-11 in half at most, independent of one another).  In the result
+// that is 0.0015 (bfloat16) and 0.00018 (half) of its size, a little less than one
+// rounding of it to the same type (0.0016, 0.00021); where the result is FIELD or
+// 32-bit floats it is nearly all of the error.
 //
 // Two forms:
 //   chunks  (kSplit false): 128 rows, the 4 waves share each tile of keys;
@@ -37,12 +40,21 @@
 // on it adds them in order, so the result does not depend on timing.
 //
 // Measured, dim 128 in bfloat16 (a large copy: 5.19 TB/s, an 8192^3 product: 1369
-// TFLOP/s): tokens, 48 sequences of 130 to 32767 entries, 64 + 8 heads: 226 us, 5.35
+// TFLOP/s): tokens, 48 sequences of 130 to 32767 entries, 64 + 8 heads: 227 us, 5.33
 // TB/s of cache; one token over 2048 entries of 32 heads 15 us, of which 6.5 are its
 // bytes, the rest starts, first loads and joins.  Chunks, a prompt of 8192, 32 heads:
-// 673 us, 816 TFLOP/s: the softmax's vector work between the products bounds it.
-// The tokens form for up to 32 rows: 32 sequences of 8 new tokens over 8000 entries,
-// 8 kv heads, take 213 us with 32 rows and 241 with the chunks form at 40.
+// 673 us, 816 TFLOP/s.  There the counters have the matrix cores busy in 39 % of the
+// cycles, vector instructions in 43 %, both at once in 17 %, the LDS in 20 % (no
+// bank conflicts), at 1.9 GHz: a wave's products, weights and reads follow one
+// another, and with two waves a SIMD a third of the cycles has neither of the first.
+//
+// Which form: tokens where a sequence has at most 32 rows a kv head, one tile.  Both
+// at 8 kv heads, tokens / chunks form in us: 32 sequences over 8000 entries, 8 rows
+// 191 / 238, 32 rows 213 / 239, 64 rows 194 / 241; 4 over 30000, 16 rows 104 / 151, 64 rows
+// 151 / 154; 64 over 500, 8 rows 26.6 / 27.5, 32 rows 28.5 / 28.1, 40 rows 44.8 / 29.5, 64
+// rows 46.9 / 30.9; 32 over 8000, 96 rows 566 / 244.  From 33 to 64 rows long contexts
+// would gain a fifth by the tokens form and short ones lose half; their lengths are
+// on the device, so the bound is where no context loses.
 #include "kv.h"
 #include "mvk_internal.h"
 #include "units.h"
