@@ -761,7 +761,7 @@ mvk_status mvk_rotary_table(uint32_t rot, uint32_t rows, double base, int32_t sc
  *   q, q_out       : T x heads x dim; both NULL: keys and values only.  q_out
  *                    may be q itself (same type and strides) and else shares
  *                    no memory with an input (MVK_EINVAL where rows of q, k or v
- *                    with its strides meet it, or extents of others).
+ *                    with its token stride meet it, or extents of others).
  *   k, v           : T x cache->kv_heads x cache->dim, of one type (q's where
  *                    there is a q); NULL (with cache and seqs): queries only.
  *   field_scale    : value of 1 in field inputs.
@@ -796,7 +796,7 @@ mvk_status mvk_rotary_append(const mvk_rows *q, const mvk_rows *k, const mvk_row
  *                shares no memory with it).
  * Sums have a fixed order: the same inputs give the same bits.
  * Errors: MVK_EINVAL (also out in q's memory and w_out in w_in's, but for the cases above:
- * rows that meet where both have the same strides, else extents that do), MVK_ERANGE (dim > MVK_MAX_HEAD_DIM, buffers above 2^62
+ * rows that meet where both have the same token stride, else extents that do), MVK_ERANGE (dim > MVK_MAX_HEAD_DIM, buffers above 2^62
  * bytes, T * heads above 2^31 - 1), MVK_ENOMEM, MVK_ECAPTURE (workspace).
  */
 mvk_status mvk_paged_attention(const mvk_rows *q, uint32_t T, uint32_t heads, const mvk_kv *cache,
@@ -818,7 +818,7 @@ mvk_status mvk_paged_attention(const mvk_rows *q, uint32_t T, uint32_t heads, co
  * dst has src's type, kv_heads, dim and any page size; dst_width * page_size of
  * dst is at least min(budget, width * page_size of src).  seqs->q_start is not used.
  * Errors: MVK_EINVAL (sinks + recent > budget, budget 0, mismatched caches, w_out in w's
- * memory: rows that meet where both have the same strides, else extents that do),
+ * memory: rows that meet where both have the same sequence stride, else extents that do),
  * MVK_ERANGE (dim > MVK_MAX_HEAD_DIM, count or kv_heads > 65535, buffers above 2^62 bytes).
  */
 mvk_status mvk_cache_evict(const mvk_kv *src, const mvk_seqs *seqs, const float *w, uint64_t w_seq, uint64_t w_head,

@@ -20,6 +20,7 @@
 #include "field.h"
 #include "kv.h"
 #include "mvk_internal.h"
+#include "overlap.h"
 
 namespace mvk {
 namespace {
@@ -1233,34 +1234,6 @@ inline bool is_float_type(int32_t type) { return type >= MVK_TYPE_BF16 && type <
 inline bool span_too_big(uint64_t a, uint64_t sa, uint64_t b, uint64_t sb, uint64_t elem) {
     if (too_big(a, sa, elem) || too_big(b, sb, elem)) return true;
     return a * sa + b * sb > (1ull << 62) / elem;
-}
-
-// Rows of `len` bytes at p + i*s0 + j*s1 (bytes), i < n0, j < n1, below 2^62 bytes in all.
-struct RowSet {
-    const void* p;
-    uint64_t n0, s0, n1, s1, len;
-    uint64_t begin() const { return (uint64_t)(uintptr_t)p; }
-    uint64_t end() const { return begin() + (n0 - 1) * s0 + (n1 - 1) * s1 + len; }
-};
-
-// Do rows of a and b share memory?  Exact where the strides are the same (or one side has
-// no second row to use its own), as those of interleaved views of one buffer are; with
-// others, where their extents meet.
-bool share_memory(const RowSet& a, const RowSet& b) {
-    if (!a.n0 || !a.n1 || !b.n0 || !b.n1) return false;
-    if (a.end() <= b.begin() || b.end() <= a.begin()) return false;
-    if ((a.n0 > 1 && b.n0 > 1 && a.s0 != b.s0) || (a.n1 > 1 && b.n1 > 1 && a.s1 != b.s1) || (a.n1 | b.n1) > 65536u)
-        return true;
-    const int64_t d = (int64_t)(b.begin() - a.begin());
-    const int64_t s0 = (int64_t)(a.n0 > 1 ? a.s0 : b.s0), s1 = (int64_t)(a.n1 > 1 ? a.s1 : b.s1);
-    // rows (i, j) of b and (k, l) of a meet if d + (i - k) s0 + (j - l) s1 lies in (-b.len, a.len)
-    for (int64_t dj = 1 - (int64_t)a.n1; dj < (int64_t)b.n1; ++dj) {
-        const int64_t x = d + dj * s1, low = -(int64_t)b.len - x;  // di s0 has to exceed low
-        int64_t di = 1 - (int64_t)a.n0;
-        if (s0) di = std::max(di, (low >= 0 ? low / s0 : -((-low + s0 - 1) / s0)) + 1);
-        if (di < (int64_t)b.n0 && di * s0 > low && x + di * s0 < (int64_t)a.len) return true;
-    }
-    return false;
 }
 
 RowSet row_set(const mvk_rows* r, uint64_t T, uint64_t heads, uint64_t dim) {

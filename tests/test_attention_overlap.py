@@ -121,3 +121,25 @@ result["a row into its keys"] = call(q, q + 2048, q + 3072, q + 2048, token=2048
     assert out == {"apart": yes, "itself": yes, "itself, another type": no, "itself, other strides": no,
                    "shifted": [no, no, no], "k, v": [no, no], "one row": yes, "one row of one kv head": [yes, yes],
                    "a row into its keys": no}
+
+
+def test_parts_of_one_row_with_head_strides_of_their_own(host):  # noqa: F811
+    """Queries one head after another, then keys and values by turns, in one row of a
+    token: the queries rotated in place meet neither; and shifted ones do."""
+    out = host(STRUCTS + """
+def call(q, k, v, o, T=3, heads=8, kv_heads=4):
+    width, cache, sq = (heads + 2 * kv_heads) * 128, kv(heads=kv_heads), seqs()
+    rec.rec_reset()
+    return lib.mvk_rotary_append(ref(rows(q, 0, width)), ref(rows(k, 0, width, 256)), ref(rows(v, 0, width, 256)), T,
+                                 heads, 128, 128, 0, ptr(), ptr(), 100, 1.0, ref(rows(o, 0, width)), ref(cache),
+                                 ref(sq), None)
+x = ptr()
+result["in place"] = [call(x, x + 2 * 128 * h, x + 2 * 128 * (h + 1), x, T, h, g) for T, h, g in ((3, 8, 4), (1, 8, 4), (2000, 64, 8), (3, 4, 1))]
+y = ptr()
+result["into the keys"] = [call(y, x, x + 256, x + 256 * i) for i in (-1, 0, 1, 5)]
+result["of the next token"] = [call(y, x, x + 256, x + 256 * i) for i in (8, 9, 15)]
+result["beside the keys"] = [call(y, x + 2 * 128 * 8, x + 2 * 128 * 9, x)]
+result["many heads"] = [call(x, x + 2 * 128 * 512, x + 2 * 128 * 513, x, 3, 512, 256)]
+""")
+    assert out == {"in place": [0] * 4, "into the keys": [-1] * 4, "of the next token": [0, -1, -1],
+                   "beside the keys": [0], "many heads": [0]}
