@@ -53,7 +53,7 @@ extern "C" {
 
 #define MVK_PRIME 2147483647u
 #define MVK_PRIME_BABYBEAR 2013265921u
-#define MVK_ABI_VERSION 10
+#define MVK_ABI_VERSION 11
 
 typedef int32_t mvk_status;
 #define MVK_OK 0
@@ -685,6 +685,8 @@ mvk_status mvk_decode_verify_seeded(const mvk_key *key, const mvk_st *st, const 
 #define MVK_TYPE_F16 1
 #define MVK_TYPE_F32 2
 #define MVK_TYPE_FIELD 3 /* uint32 field elements */
+#define MVK_TYPE_E4M3 4  /* caches only, see mvk_kv8: 8-bit floats of 4 exponent and 3 mantissa bits, */
+#define MVK_TYPE_I8 5    /* or 8-bit integers, with a power of two for every entry and head */
 
 /* Rows of heads: element d of head h of token t lies at data[t*token + h*head + d]
  * (strides in elements, at least dim apart or equal where memory is shared). */
@@ -705,6 +707,32 @@ typedef struct mvk_kv {
     uint64_t k_page, k_head, k_entry;
     uint64_t v_page, v_head, v_entry;
 } mvk_kv;
+
+/*
+ * A cache held in 8 bits: kv as above with type MVK_TYPE_E4M3 or MVK_TYPE_I8 and
+ * one byte a value, and an exponent for every entry and head of K and of V: entry
+ * e of head h of page i stands for code * 2^k_exp[i*kx_page + h*kx_head + e*kx_entry].
+ * Every call that takes an mvk_kv takes the address of `kv`; where kv.type is one
+ * of the two types it is read as part of an mvk_kv8.
+ * What a row x (the dim values of an entry and head) is held as: the exponent is
+ * the least in [MVK_EXP_LEAST, MVK_EXP_MOST] with max |x_d| <= M 2^exponent over
+ * the finite x_d (M = 448 for E4M3, 127 for I8), and the codes are the nearest to
+ * x_d / 2^exponent (ties to even; clamped to M).  The rotation before it is in
+ * 64 bits, so the codes are the nearest of the exact values.  An infinity or a not-a-number
+ * becomes a not-a-number: that value in E4M3, the row in I8, whose exponent then
+ * is MVK_EXP_NAN.  Every other value is exact in bfloat16, the type that
+ * attention over such a cache computes in: queries are BF16.  Exponents outside
+ * the range give unspecified values.
+ */
+#define MVK_EXP_LEAST (-96)
+#define MVK_EXP_MOST 119
+#define MVK_EXP_NAN (-128)
+typedef struct mvk_kv8 {
+    mvk_kv kv;
+    int8_t *k_exp, *v_exp; /* device */
+    uint64_t kx_page, kx_head, kx_entry;
+    uint64_t vx_page, vx_head, vx_entry;
+} mvk_kv8;
 
 /* `count` sequences.  Entry j of sequence s lies in page table[s*table_stride +
  * j / page_size] at j % page_size; lens[s] entries are in use, the new tokens'
@@ -765,13 +793,25 @@ mvk_status mvk_rotary_table(uint32_t rot, uint32_t rows, double base, int32_t sc
  *   k, v           : T x cache->kv_heads x cache->dim, of one type (q's where
  *                    there is a q); NULL (with cache and seqs): queries only.
  *   field_scale    : value of 1 in field inputs.
- * Types: inputs any, q_out BF16, F16 or F32, equal to the cache's where both are given.
+ * Types: inputs any, q_out BF16, F16 or F32, equal to the cache's where both are given
+ * (BF16 with a cache held in 8 bits).
  * Errors: MVK_EINVAL, MVK_ERANGE (dim > MVK_MAX_HEAD_DIM, buffers above 2^62 bytes).
  */
 mvk_status mvk_rotary_append(const mvk_rows *q, const mvk_rows *k, const mvk_rows *v, uint32_t T, uint32_t heads,
                              uint32_t dim, uint32_t rot, int32_t layout, const int32_t *positions,
                              const float *table, uint32_t table_rows, float field_scale, const mvk_rows *q_out,
                              const mvk_kv *cache, const mvk_seqs *seqs, void *stream);
+
+/*
+ * The new tokens' entries as the cache holds them: row t of k and of v is the entry
+ * that mvk_rotary_append writes for token t (rows of tokens without one, or whose page
+ * is outside the pool, are left alone), rounded once to the rows' type.
+ *   k, v           : T x cache->kv_heads x cache->dim, BF16, F16 or F32; either may
+ *                    be NULL; they share no memory with each other or the cache.
+ * Errors: MVK_EINVAL, MVK_ERANGE (as mvk_rotary_append).
+ */
+mvk_status mvk_cache_read(const mvk_kv *cache, const mvk_seqs *seqs, uint32_t T, const mvk_rows *k,
+                          const mvk_rows *v, void *stream);
 
 /*
  * Attention of the new tokens over their sequences' entries: new token i (of c)
@@ -781,7 +821,7 @@ mvk_status mvk_rotary_append(const mvk_rows *q, const mvk_rows *k, const mvk_row
  * A row that sees no entry (a sequence shorter than its new tokens) is zero.
  * Places that a row does not see, and unused places of a page, do not reach it
  * whatever they hold; a not-a-number in a place that it sees does.
- *   q          : T x heads x dim, the cache's type
+ *   q          : T x heads x dim, the cache's type (BF16 for a cache held in 8 bits)
  *   out        : T x heads x dim: BF16, F16, F32, or FIELD: o / field_scale
  *                rounded to the nearest integer and embedded in F_p (a
  *                magnitude above (p-1)/2 is clamped to it).  Rows that belong

@@ -802,8 +802,8 @@ def sample_sparse(count: int, N: int, t: int, seed: int, tag: int, p: int = P):
 
 
 # The client's attention (attention.py takes the helpers above, so it comes last)
-from .attention import (FIELD, KVCache, Sequences, cache_evict, paged_attention, rotary, rotary_append,  # noqa: E402
-                        rotary_table)
+from .attention import (FIELD, KVCache, Sequences, cache_evict, cache_read, paged_attention, rotary,  # noqa: E402
+                        rotary_append, rotary_table)
 
-__all__ += ["FIELD", "KVCache", "Sequences", "rotary_table", "rotary", "rotary_append", "paged_attention",
-            "cache_evict"]
+__all__ += ["FIELD", "KVCache", "Sequences", "rotary_table", "rotary", "rotary_append", "cache_read",
+            "paged_attention", "cache_evict"]

@@ -32,7 +32,7 @@ MVK_SEEDED_MAX_T = 4096
 MVK_STATIC_SCRATCH_BYTES = 32 << 20
 MVK_MAX_GROUP = 4
 MVK_MAX_PREP = 8
-ABI_VERSION = 10
+ABI_VERSION = 11
 # field modulus -> library built over that field
 LIB_PATHS = {MVK_PRIME: LIB_PATH, MVK_PRIME_BABYBEAR: LIB_PATH_BB}
 
@@ -85,6 +85,7 @@ EXPORTS = (
     "mvk_rotary_append",
     "mvk_paged_attention",
     "mvk_cache_evict",
+    "mvk_cache_read",
 )
 
 
@@ -123,6 +124,11 @@ MVK_TYPE_BF16 = 0
 MVK_TYPE_F16 = 1
 MVK_TYPE_F32 = 2
 MVK_TYPE_FIELD = 3
+MVK_TYPE_E4M3 = 4
+MVK_TYPE_I8 = 5
+MVK_EXP_LEAST = -96
+MVK_EXP_MOST = 119
+MVK_EXP_NAN = -128
 MVK_ROTARY_HALF = 0
 MVK_ROTARY_INTERLEAVED = 1
 MVK_SCALE_NONE = 0
@@ -156,6 +162,19 @@ class MvkKv(ctypes.Structure):
         ("v_page", ctypes.c_uint64),
         ("v_head", ctypes.c_uint64),
         ("v_entry", ctypes.c_uint64),
+    ]
+
+
+class MvkKv8(MvkKv):  # (an mvk_kv first, so its address is one's)
+    _fields_ = [
+        ("k_exp", ctypes.c_void_p),
+        ("v_exp", ctypes.c_void_p),
+        ("kx_page", ctypes.c_uint64),
+        ("kx_head", ctypes.c_uint64),
+        ("kx_entry", ctypes.c_uint64),
+        ("vx_page", ctypes.c_uint64),
+        ("vx_head", ctypes.c_uint64),
+        ("vx_entry", ctypes.c_uint64),
     ]
 
 
@@ -304,6 +323,8 @@ def load(p: int = MVK_PRIME) -> ctypes.CDLL:
     L.mvk_paged_attention.restype = st
     L.mvk_cache_evict.argtypes = [kv, seqs, vp, u64, u64, u32, u32, u32, kv, vp, u64, u32, vp, u64, u64, vp, vp, vp]
     L.mvk_cache_evict.restype = st
+    L.mvk_cache_read.argtypes = [kv, seqs, u32, rows, rows, vp]
+    L.mvk_cache_read.restype = st
     if L.mvk_abi_version() != ABI_VERSION:
         raise ImportError(f"{path}: ABI version mismatch; rebuild the library")
     if L.mvk_field_modulus() != p:

@@ -1,6 +1,6 @@
 """The client's attention between the delegated projections: rotary positions
 with the append to a paged cache, attention over it, and eviction from it
-(mvk_rotary_*, mvk_paged_attention, mvk_cache_evict in include/mvk.h).
+(mvk_rotary_*, mvk_cache_read, mvk_paged_attention, mvk_cache_evict in include/mvk.h).
 
 Decrypted queries, keys and values are field elements of fixed-point numbers;
 rotary_append takes them as they are (field_scale: the value of 1) and leaves
@@ -12,6 +12,10 @@ field elements, the query of the next projection:
     seqs = Sequences(table, lens, q_start, max_new=1)        # shared by the layers
     q = rotary_append(yq, yk, yv, positions, rot, cache, seqs, field_scale=2**-16)
     x = paged_attention(q, cache, seqs, out_dtype=FIELD, field_scale=2**-8)
+
+A cache may be held in 8 bits (dtype=torch.float8_e4m3fn or torch.int8, with one
+power of two an entry and head): rotary_append then writes codes and exponents, and
+attention, eviction and cache_read take them as they are, at half the bytes.
 
 As in the rest of the binding, every function only checks types and shapes and
 passes pointers, strides and the stream.
@@ -30,11 +34,14 @@ FIELD = torch.int32  # field elements, as everywhere in this package
 
 _TYPES = {torch.bfloat16: _lib.MVK_TYPE_BF16, torch.float16: _lib.MVK_TYPE_F16, torch.float32: _lib.MVK_TYPE_F32,
           torch.int32: _lib.MVK_TYPE_FIELD}
+_CACHE_TYPES = {torch.bfloat16: _lib.MVK_TYPE_BF16, torch.float16: _lib.MVK_TYPE_F16, torch.float32: _lib.MVK_TYPE_F32,
+                torch.float8_e4m3fn: _lib.MVK_TYPE_E4M3, torch.int8: _lib.MVK_TYPE_I8}
 _LAYOUTS = {"half": _lib.MVK_ROTARY_HALF, "interleaved": _lib.MVK_ROTARY_INTERLEAVED}
 _SCALINGS = {None: _lib.MVK_SCALE_NONE, "linear": _lib.MVK_SCALE_LINEAR, "base": _lib.MVK_SCALE_BASE,
              "parts": _lib.MVK_SCALE_PARTS}
 
-__all__ = ["FIELD", "KVCache", "Sequences", "rotary_table", "rotary", "rotary_append", "paged_attention", "cache_evict"]
+__all__ = ["FIELD", "KVCache", "Sequences", "rotary_table", "rotary", "rotary_append", "cache_read", "paged_attention",
+           "cache_evict"]
 
 
 def _rows(t: torch.Tensor, name: str, T: int, heads: int | None, dim: int):
@@ -55,22 +62,37 @@ def _rows(t: torch.Tensor, name: str, T: int, heads: int | None, dim: int):
 @dataclass
 class KVCache:
     """The pools of one layer: pages x kv_heads x page_size x dim each (views
-    with other strides will do; the last axis is contiguous)."""
+    with other strides will do; the last axis is contiguous).  A cache held in 8
+    bits (K and V float8_e4m3fn or int8) has k_exp and v_exp, pages x kv_heads x
+    page_size int8 of any strides: an entry's row is codes * 2^exponent, what
+    rotary_append rounds to and attention computes with, in bfloat16, exactly."""
     K: torch.Tensor
     V: torch.Tensor
+    k_exp: torch.Tensor | None = None
+    v_exp: torch.Tensor | None = None
 
     @classmethod
     def allocate(cls, pages: int, kv_heads: int, page_size: int, dim: int, dtype=torch.bfloat16,
                  device="cuda") -> "KVCache":
-        return cls(*(torch.zeros((pages, kv_heads, page_size, dim), dtype=dtype, device=device) for _ in range(2)))
+        shape = (pages, kv_heads, page_size)
+        pools = [torch.zeros((*shape, dim), dtype=dtype, device=device) for _ in range(2)]
+        if dtype in (torch.float8_e4m3fn, torch.int8):
+            pools += [torch.zeros(shape, dtype=torch.int8, device=device) for _ in range(2)]
+        return cls(*pools)
+
+    @property
+    def query_dtype(self):
+        """Of the queries of paged_attention over this cache (bfloat16 where it is held in 8 bits)."""
+        return torch.bfloat16 if self.k_exp is not None else self.K.dtype
 
     def struct(self):
         K, V = self.K, self.V
         if not (isinstance(K, torch.Tensor) and isinstance(V, torch.Tensor) and K.is_cuda and V.is_cuda):
             raise TypeError("K and V must be CUDA tensors")
-        kind = _TYPES.get(K.dtype, _lib.MVK_TYPE_FIELD)
-        if K.dtype != V.dtype or kind == _lib.MVK_TYPE_FIELD:
-            raise TypeError(f"K and V must both be bfloat16, float16 or float32, got {K.dtype}, {V.dtype}")
+        kind = _CACHE_TYPES.get(K.dtype)
+        if K.dtype != V.dtype or kind is None:
+            raise TypeError("K and V must both be bfloat16, float16, float32, float8_e4m3fn or int8, got "
+                            f"{K.dtype}, {V.dtype}")
         shape = K.shape
         if len(shape) != 4 or shape != V.shape:
             raise ValueError(f"K and V must be pages x kv_heads x page_size x dim, got {tuple(shape)}, {tuple(V.shape)}")
@@ -79,7 +101,18 @@ class KVCache:
         va, vb, vc, vd = V.stride()
         if (kd != 1 or vd != 1) and d > 1:
             raise ValueError("K and V: the last axis must be contiguous")
-        return _lib.MvkKv(K.data_ptr(), V.data_ptr(), kind, n, h, p, d, ka, kb, kc, va, vb, vc)
+        if kind != _lib.MVK_TYPE_E4M3 and kind != _lib.MVK_TYPE_I8:
+            if self.k_exp is not None or self.v_exp is not None:
+                raise ValueError("k_exp and v_exp belong to a cache held in 8 bits")
+            return _lib.MvkKv(K.data_ptr(), V.data_ptr(), kind, n, h, p, d, ka, kb, kc, va, vb, vc)
+        kx, vx = self.k_exp, self.v_exp
+        for x, name in ((kx, "k_exp"), (vx, "v_exp")):
+            if not isinstance(x, torch.Tensor) or x.dtype != torch.int8 or x.device != K.device:
+                raise TypeError(f"{name} must be an int8 tensor on K's device (the cache is held in 8 bits)")
+            if x.shape != shape[:3]:
+                raise ValueError(f"{name} has shape {tuple(x.shape)}, expected {tuple(shape[:3])}")
+        return _lib.MvkKv8(K.data_ptr(), V.data_ptr(), kind, n, h, p, d, ka, kb, kc, va, vb, vc, kx.data_ptr(),
+                           vx.data_ptr(), *kx.stride(), *vx.stride())
 
 
 @dataclass
@@ -167,11 +200,34 @@ def rotary_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, posi
                   field_scale: float | None = None, out: torch.Tensor | None = None, p: int = P, stream=None):
     """Rotary positions on new tokens' q and k, and k, v into their places of the
     cache, in one launch.  q: T x heads x dim (or None), k, v: T x kv_heads x dim,
-    one type.  Returns the rotated q in the cache's type."""
+    one type.  Returns the rotated q in the cache's type (bfloat16 where that is
+    held in 8 bits)."""
     if q is not None and out is None:
-        out = torch.empty(q.shape, dtype=cache.K.dtype, device=q.device)
+        out = torch.empty(q.shape, dtype=cache.query_dtype, device=q.device)
     _rotary_call(q, k, v, positions, table, cache, seqs, layout, field_scale, out, p, stream)
     return out
+
+
+def cache_read(cache: KVCache, seqs: Sequences, tokens: int | None = None, dtype=torch.bfloat16,
+               k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None, p: int = P, stream=None):
+    """The new tokens' entries as the cache holds them, as rows: (k, v), T x
+    kv_heads x dim of bfloat16, float16 or float32; T is `tokens`, or that of k_out and
+    v_out (with one of them, only that one is read).  For whole sequences: q_start
+    with their lengths summed up.  Rows of no sequence are left alone (zeros where
+    the call allocates them)."""
+    cs = cache.struct()
+    if k_out is None and v_out is None:
+        if tokens is None:
+            raise ValueError("tokens is needed where neither k_out nor v_out is given")
+        k_out, v_out = (torch.zeros((tokens, cs.kv_heads, cs.dim), dtype=dtype, device=cache.K.device) for _ in range(2))
+    T = (k_out if k_out is not None else v_out).shape[0]
+    if tokens is not None and tokens != T:
+        raise ValueError(f"the rows have {T} tokens, not {tokens}")
+    ref = ctypes.byref
+    ks, vs = (ref(_rows(x, name, T, cs.kv_heads, cs.dim)) if x is not None else None
+              for x, name in ((k_out, "k_out"), (v_out, "v_out")))
+    _lib.check("mvk_cache_read", _lib.load(p).mvk_cache_read(ref(cs), ref(seqs.struct(T)), T, ks, vs, _stream(stream)))
+    return k_out, v_out
 
 
 def paged_attention(q: torch.Tensor, cache: KVCache, seqs: Sequences, scale: float | None = None,

@@ -1227,7 +1227,12 @@ mvk_status mvk_decode_verify_seeded(const mvk_key* key, const mvk_st* st, const 
 
 namespace {
 
-inline size_t type_size(int32_t type) { return type == MVK_TYPE_BF16 || type == MVK_TYPE_F16 ? 2 : 4; }
+inline size_t type_size(int32_t type) {
+    return type == MVK_TYPE_BF16 || type == MVK_TYPE_F16 ? 2 : type == MVK_TYPE_E4M3 || type == MVK_TYPE_I8 ? 1 : 4;
+}
+inline bool in_8_bits(const mvk_kv* kv) { return kv->type == MVK_TYPE_E4M3 || kv->type == MVK_TYPE_I8; }
+// The type of queries over a cache.
+inline int32_t query_type(const mvk_kv* kv) { return in_8_bits(kv) ? MVK_TYPE_BF16 : kv->type; }
 inline bool is_float_type(int32_t type) { return type >= MVK_TYPE_BF16 && type <= MVK_TYPE_F32; }
 
 // a rows with stride sa and b of sb within, elements of size elem: beyond 2^62 bytes?
@@ -1248,7 +1253,7 @@ mvk_status check_rows(const mvk_rows* r, uint64_t T, uint64_t heads) {
 }
 
 mvk_status check_kv(const mvk_kv* kv) {
-    if (!kv || !kv->K || !kv->V || !is_float_type(kv->type)) return MVK_EINVAL;
+    if (!kv || !kv->K || !kv->V || !(is_float_type(kv->type) || in_8_bits(kv))) return MVK_EINVAL;
     if (!kv->pages || !kv->kv_heads || !kv->dim || !kv->page_size || (kv->page_size & (kv->page_size - 1)))
         return MVK_EINVAL;
     const size_t e = type_size(kv->type);
@@ -1257,6 +1262,13 @@ mvk_status check_kv(const mvk_kv* kv) {
     if (span_too_big(kv->pages, kv->k_page, kv->kv_heads, kv->k_head, e) || too_big(kv->page_size, kv->k_entry, e) ||
         span_too_big(kv->pages, kv->v_page, kv->kv_heads, kv->v_head, e) || too_big(kv->page_size, kv->v_entry, e))
         return MVK_ERANGE;
+    if (in_8_bits(kv)) {
+        const mvk_kv8* x = (const mvk_kv8*)kv;
+        if (!x->k_exp || !x->v_exp) return MVK_EINVAL;
+        if (span_too_big(kv->pages, x->kx_page, kv->kv_heads, x->kx_head, 1) || too_big(kv->page_size, x->kx_entry, 1) ||
+            span_too_big(kv->pages, x->vx_page, kv->kv_heads, x->vx_head, 1) || too_big(kv->page_size, x->vx_entry, 1))
+            return MVK_ERANGE;
+    }
     return MVK_OK;
 }
 
@@ -1272,9 +1284,15 @@ mvk_status check_seqs(const mvk_seqs* sq, const mvk_kv* kv, bool rows) {
 Rows view_of(const mvk_rows* r) { return Rows{r->data, (size_t)r->token, (size_t)r->head, r->type}; }
 
 KvView view_of(const mvk_kv* kv) {
-    return KvView{kv->K, kv->V, (size_t)kv->k_page, (size_t)kv->k_head, (size_t)kv->k_entry, (size_t)kv->v_page,
-                  (size_t)kv->v_head, (size_t)kv->v_entry, kv->pages, kv->kv_heads,
-                  (uint32_t)__builtin_ctz(kv->page_size), kv->dim};
+    KvView v = {kv->K, kv->V, (size_t)kv->k_page, (size_t)kv->k_head, (size_t)kv->k_entry, (size_t)kv->v_page,
+                (size_t)kv->v_head, (size_t)kv->v_entry, kv->pages, kv->kv_heads,
+                (uint32_t)__builtin_ctz(kv->page_size), kv->dim, kv->type};
+    if (in_8_bits(kv)) {
+        const mvk_kv8* x = (const mvk_kv8*)kv;
+        v.kx = x->k_exp, v.kxp = (size_t)x->kx_page, v.kxh = (size_t)x->kx_head, v.kxe = (size_t)x->kx_entry;
+        v.vx = x->v_exp, v.vxp = (size_t)x->vx_page, v.vxh = (size_t)x->vx_head, v.vxe = (size_t)x->vx_entry;
+    }
+    return v;
 }
 
 SeqView view_of(const mvk_seqs* sq) {
@@ -1333,7 +1351,7 @@ mvk_status mvk_rotary_append(const mvk_rows* q, const mvk_rows* k, const mvk_row
         if ((st = check_kv(cache)) || (st = check_seqs(seqs, cache, true))) return st;
         if ((st = check_rows(k, T, cache->kv_heads)) || (st = check_rows(v, T, cache->kv_heads))) return st;
         if (cache->dim != dim || k->type != v->type) return MVK_EINVAL;
-        if (q && (q->type != k->type || q_out->type != cache->type)) return MVK_EINVAL;
+        if (q && (q->type != k->type || q_out->type != query_type(cache))) return MVK_EINVAL;
         // k and v are read while q_out is written
         const RowSet out = q ? row_set(q_out, T, heads, dim) : RowSet{};
         if (share_memory(row_set(k, T, cache->kv_heads, dim), out) || share_memory(row_set(v, T, cache->kv_heads, dim), out))
@@ -1347,9 +1365,33 @@ mvk_status mvk_rotary_append(const mvk_rows* q, const mvk_rows* k, const mvk_row
     SeqView sq;
     if (q) rq = view_of(q), ro = view_of(q_out);
     if (k) rk = view_of(k), rv = view_of(v), kv = view_of(cache), sq = view_of(seqs);
+    if (k && in_8_bits(cache))
+        return hip_status(launch_append8(q ? &rq : nullptr, rk, rv, T, heads, dim, rot, layout == MVK_ROTARY_HALF,
+                                         positions, table, table_rows, field_scale, q ? &ro : nullptr, kv, sq,
+                                         (hipStream_t)stream));
     return hip_status(launch_rotary(q ? &rq : nullptr, k ? &rk : nullptr, k ? &rv : nullptr, src, dst, T, heads, dim,
                                     rot, layout == MVK_ROTARY_HALF, positions, table, table_rows, field_scale,
                                     q ? &ro : nullptr, k ? &kv : nullptr, k ? &sq : nullptr, (hipStream_t)stream));
+}
+
+mvk_status mvk_cache_read(const mvk_kv* cache, const mvk_seqs* seqs, uint32_t T, const mvk_rows* k, const mvk_rows* v,
+                          void* stream) {
+    mvk_status st = check_kv(cache);
+    if (st || (st = check_seqs(seqs, cache, true))) return st;
+    if (!k && !v) return MVK_EINVAL;
+    if (T > 0x7fffffffu) return MVK_ERANGE;
+    for (const mvk_rows* r : {k, v}) {
+        if (!r) continue;
+        if ((st = check_rows(r, T, cache->kv_heads))) return st;
+        if (!is_float_type(r->type)) return MVK_EINVAL;
+    }
+    if (k && v && share_memory(row_set(k, T, cache->kv_heads, cache->dim), row_set(v, T, cache->kv_heads, cache->dim)))
+        return MVK_EINVAL;
+    if (T == 0) return MVK_OK;
+    Rows rk = {}, rv = {};
+    if (k) rk = view_of(k);
+    if (v) rv = view_of(v);
+    return hip_status(launch_cache_read(view_of(cache), view_of(seqs), T, rk, rv, (hipStream_t)stream));
 }
 
 mvk_status mvk_paged_attention(const mvk_rows* q, uint32_t T, uint32_t heads, const mvk_kv* cache,
@@ -1360,7 +1402,7 @@ mvk_status mvk_paged_attention(const mvk_rows* q, uint32_t T, uint32_t heads, co
     if (!heads || heads % cache->kv_heads || !std::isfinite(scale)) return MVK_EINVAL;
     if ((uint64_t)T * heads > 0x7fffffffull) return MVK_ERANGE;
     if ((st = check_rows(q, T, heads)) || (st = check_rows(out, T, heads))) return st;
-    if (q->type != cache->type) return MVK_EINVAL;
+    if (q->type != query_type(cache)) return MVK_EINVAL;
     if (out->type == MVK_TYPE_FIELD && !(std::isfinite(field_scale) && field_scale > 0)) return MVK_EINVAL;
     const uint64_t cap = (uint64_t)seqs->width * cache->page_size;
     if (w_in && !w_out) return MVK_EINVAL;

@@ -8,6 +8,7 @@
 
 #include "kv.h"
 #include "mvk_internal.h"
+#include "quant.h"
 
 namespace mvk {
 
@@ -35,10 +36,14 @@ __device__ __forceinline__ float wave_sum(float x) {
 // One wave per (token, head): 64 keys at a time, each lane one product q . k,
 // then each lane the values of dims lane, lane + 64, ...  Only entries that the
 // row sees are read.
-template <typename T>
+// C: how the cache holds its values; a row of one held in 8 bits has its power of two.
+template <typename C>
 __global__ __launch_bounds__(256) void attend_any(Rows q, uint32_t tokens, uint32_t heads, KvView kv, SeqView sq,
                                                   float sl2, Rows out, float inv_scale, float* __restrict__ lse) {
-    __shared__ float sq_[4][kMaxDim], sp_[4][64];
+    typedef Held<C> H;
+    typedef typename H::Q T;
+    typedef typename H::S S;
+    __shared__ float sq_[4][kMaxDim], sp_[4][64], sv_[H::k8 ? 4 : 1][64];
     __shared__ size_t so_[4][64];
     const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     // (no barrier below spans waves)
@@ -58,14 +63,19 @@ __global__ __launch_bounds__(256) void attend_any(Rows q, uint32_t tokens, uint3
         float m = -INFINITY, l = 0.f;
         for (uint32_t j0 = 0; j0 < nv; j0 += 64) {
             const uint32_t j = j0 + lane, jn = min(64u, nv - j0);
-            float x = -INFINITY;
+            float x = -INFINITY, two = 1.f;
             size_t off = 0;
             if (j < nv) {
                 const size_t page = seq_page(sq, kv, s, j), at = j & ((1u << kv.shift) - 1);
-                const T* k = (const T*)kv.K + page * kv.kp + kh * kv.kh + at * kv.ke;
+                const S* k = (const S*)kv.K + page * kv.kp + kh * kv.kh + at * kv.ke;
                 off = page * kv.vp + kh * kv.vh + at * kv.ve;
+                float kt = 1.f;
+                if (H::k8) {
+                    kt = power(kv.kx[page * kv.kxp + kh * kv.kxh + at * kv.kxe]);
+                    two = power(kv.vx[page * kv.vxp + kh * kv.vxh + at * kv.vxe]);
+                }
                 float d0 = 0.f;
-                for (uint32_t d = 0; d < dim; ++d) d0 += sq_[wave][d] * to_float(k[d]);
+                for (uint32_t d = 0; d < dim; ++d) d0 += sq_[wave][d] * H::get(k[d], kt);
                 x = d0 * sl2;
             }
             const float top = wave_max(x), mn = fmaxf(m, top);
@@ -76,6 +86,7 @@ __global__ __launch_bounds__(256) void attend_any(Rows q, uint32_t tokens, uint3
             m = mn;
             sp_[wave][lane] = p;
             so_[wave][lane] = off;
+            if (H::k8) sv_[H::k8 ? wave : 0][lane] = two;
             wave_sync();
 #pragma unroll
             for (uint32_t i = 0; i < kMaxDim / 64; ++i) {
@@ -83,7 +94,8 @@ __global__ __launch_bounds__(256) void attend_any(Rows q, uint32_t tokens, uint3
                 if (64 * i < dim) {
                     float o = acc[i] * a;
                     if (d < dim)
-                        for (uint32_t u = 0; u < jn; ++u) o += sp_[wave][u] * to_float(((const T*)kv.V)[so_[wave][u] + d]);
+                        for (uint32_t u = 0; u < jn; ++u)
+                            o += sp_[wave][u] * H::get(((const S*)kv.V)[so_[wave][u] + d], H::k8 ? sv_[H::k8 ? wave : 0][u] : 1.f);
                     acc[i] = o;
                 }
             }
@@ -101,24 +113,28 @@ __global__ __launch_bounds__(256) void attend_any(Rows q, uint32_t tokens, uint3
 
 // Collected weights: one thread per (sequence, kv head, entry), the rows that
 // see the entry in order.
-template <typename T>
+template <typename C>
 __global__ __launch_bounds__(256) void weights_any(Rows q, uint32_t tokens, uint32_t heads, KvView kv, SeqView sq,
                                                    float sl2, const float* __restrict__ lse, const float* w_in,
                                                    float* w_out, size_t w_seq, size_t w_head) {
+    typedef Held<C> H;
+    typedef typename H::Q T;
+    typedef typename H::S S;
     const uint32_t kh = blockIdx.y, s = blockIdx.z;
     const SeqSpan sp = seq_span(sq, kv.shift, s, tokens);
     const uint32_t grp = heads / kv.heads;
     for (uint32_t j = blockIdx.x * 256 + threadIdx.x; j < sp.n; j += gridDim.x * 256) {
         const int64_t base = (int64_t)sp.n - sp.c;  // entries before the new tokens
         const size_t page = seq_page(sq, kv, s, j), at = j & ((1u << kv.shift) - 1);
-        const T* k = (const T*)kv.K + page * kv.kp + kh * kv.kh + at * kv.ke;
+        const S* k = (const S*)kv.K + page * kv.kp + kh * kv.kh + at * kv.ke;
+        const float kt = H::k8 ? power(kv.kx[page * kv.kxp + kh * kv.kxh + at * kv.kxe]) : 1.f;
         float sum = 0.f;
         for (uint32_t i = j > base ? (uint32_t)(j - base) : 0u; i < sp.c; ++i)
             for (uint32_t g = 0; g < grp; ++g) {
                 const uint32_t t = sp.q0 + i, h = kh * grp + g;
                 const T* qr = (const T*)q.p + (size_t)t * q.token + (size_t)h * q.head;
                 float d0 = 0.f;
-                for (uint32_t d = 0; d < kv.dim; ++d) d0 += to_float(qr[d]) * to_float(k[d]);
+                for (uint32_t d = 0; d < kv.dim; ++d) d0 += to_float(qr[d]) * H::get(k[d], kt);
                 const float z = lse[(size_t)t * heads + h];
                 sum += z == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(d0 * sl2 - z * kLog2e);
             }
@@ -137,9 +153,11 @@ hipError_t launch_attend_any(const Rows& q, uint32_t tokens, uint32_t heads, con
         hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, q, tokens, heads, kv, sq, scale * kLog2e, out, inv_scale, lse);
         return hipGetLastError();
     };
-    switch (q.type) {
+    switch (kv.type) {
         case MVK_TYPE_BF16: return go(attend_any<__bf16>);
         case MVK_TYPE_F16: return go(attend_any<_Float16>);
+        case MVK_TYPE_E4M3: return go(attend_any<E4M3>);
+        case MVK_TYPE_I8: return go(attend_any<I8>);
         default: return go(attend_any<float>);
     }
 }
@@ -154,9 +172,11 @@ hipError_t launch_weights_any(const Rows& q, uint32_t tokens, uint32_t heads, co
                            w_seq, w_head);
         return hipGetLastError();
     };
-    switch (q.type) {
+    switch (kv.type) {
         case MVK_TYPE_BF16: return go(weights_any<__bf16>);
         case MVK_TYPE_F16: return go(weights_any<_Float16>);
+        case MVK_TYPE_E4M3: return go(weights_any<E4M3>);
+        case MVK_TYPE_I8: return go(weights_any<I8>);
         default: return go(weights_any<float>);
     }
 }

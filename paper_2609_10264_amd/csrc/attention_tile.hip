@@ -1070,7 +1070,7 @@ inline bool in16(const void* p, size_t a, size_t b, size_t c) { return (uintptr_
 }  // namespace
 
 bool attend_tile_fits(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq, bool split) {
-    if ((q.type != MVK_TYPE_BF16 && q.type != MVK_TYPE_F16) || kv.dim % 8 || kv.dim > 256 || tokens == 0) return false;
+    if (kv.kx || (q.type != MVK_TYPE_BF16 && q.type != MVK_TYPE_F16) || kv.dim % 8 || kv.dim > 256 || tokens == 0) return false;
     if (!in16(q.p, q.token, q.head, 0) || !in16(kv.K, kv.kp, kv.kh, kv.ke) || !in16(kv.V, kv.vp, kv.vh, kv.ve))
         return false;
     const uint64_t cap = (uint64_t)sq.width << kv.shift;

@@ -378,6 +378,18 @@ __global__ __launch_bounds__(256) void evict_copy(CopyArgs a, uint32_t dims, uin
             kd[u] = dp * a.dst.kp + h * a.dst.kh + de * a.dst.ke;
             vd[u] = dp * a.dst.vp + h * a.dst.vh + de * a.dst.ve;
         }
+        if (a.src.kx && threadIdx.x % per == 0) {
+            // the exponents of a cache held in 8 bits
+#pragma unroll
+            for (uint32_t u = 0; u < kRowsEach; ++u) {
+                if (!on[u]) continue;
+                const uint32_t r = r0 + u * rows, e = (uint32_t)at[u], se = e & ((1u << a.src.shift) - 1);
+                const uint32_t de = r & ((1u << a.dst.shift) - 1);
+                const size_t sp = seq_page(a.sq, a.src, s, e), dp = (uint32_t)a.dtable[(size_t)s * a.dts + (r >> a.dst.shift)];
+                a.dst.kx[dp * a.dst.kxp + h * a.dst.kxh + de * a.dst.kxe] = a.src.kx[sp * a.src.kxp + h * a.src.kxh + se * a.src.kxe];
+                a.dst.vx[dp * a.dst.vxp + h * a.dst.vxh + de * a.dst.vxe] = a.src.vx[sp * a.src.vxp + h * a.src.vxh + se * a.src.vxe];
+            }
+        }
         for (uint32_t c = threadIdx.x % per; c < dims; c += per) {
             T k[kRowsEach], v[kRowsEach];
 #pragma unroll
@@ -428,6 +440,7 @@ hipError_t launch_evict(const KvView& src, const SeqView& sq, size_t elem, const
     const uint32_t per = (uint32_t)(16 / elem);
     if (in_granules(c.src, per) && in_granules(c.dst, per)) return go(evict_copy<u32x4>, src.dim / per);
     c.src = src, c.dst = dst;
+    if (elem == 1) return go(evict_copy<uint8_t>, src.dim);
     return elem == 2 ? go(evict_copy<uint16_t>, src.dim) : go(evict_copy<uint32_t>, src.dim);
 }
 

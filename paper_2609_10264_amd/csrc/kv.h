@@ -20,6 +20,10 @@ struct KvView {
     void *K, *V;
     size_t kp, kh, ke, vp, vh, ve;  // strides in elements: page, head, entry
     uint32_t pages, heads, shift, dim;  // 2^shift entries a page
+    int type;
+    // exponents of a cache held in 8 bits (null otherwise), and their strides
+    int8_t *kx, *vx;
+    size_t kxp, kxh, kxe, vxp, vxh, vxe;
 };
 
 struct SeqView {
@@ -60,6 +64,21 @@ __device__ __forceinline__ uint32_t seq_of(const SeqView& sq, uint32_t t) {
 __device__ __forceinline__ uint32_t seq_page(const SeqView& sq, const KvView& kv, uint32_t s, uint32_t j) {
     const int32_t pg = sq.table[(size_t)s * sq.ts + (j >> kv.shift)];
     return pg < 0 ? 0u : min((uint32_t)pg, kv.pages - 1);
+}
+
+// Where token t's entry of the cache lies (of T token rows): false if it has none, or
+// its page is outside the pool.
+__device__ __forceinline__ bool token_entry(const SeqView& sq, const KvView& kv, uint32_t T, uint32_t t, uint32_t& page,
+                                            uint32_t& at) {
+    const uint32_t s = seq_of(sq, t);
+    const SeqSpan sp = seq_span(sq, kv.shift, s, T);
+    const int64_t e = (int64_t)sp.n - sp.c + ((int64_t)t - sp.q0);
+    if (t < sp.q0 || t >= sp.q0 + sp.c || e < 0) return false;
+    const int32_t pg = sq.table[(size_t)s * sq.ts + (size_t)(e >> kv.shift)];
+    if (pg < 0 || (uint32_t)pg >= kv.pages) return false;
+    page = (uint32_t)pg;
+    at = (uint32_t)e & ((1u << kv.shift) - 1);
+    return true;
 }
 
 __device__ __forceinline__ float to_float(float x) { return x; }

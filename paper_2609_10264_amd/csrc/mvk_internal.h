@@ -283,6 +283,13 @@ hipError_t launch_rotary(const Rows* q, const Rows* k, const Rows* v, int src, i
                          uint32_t dim, uint32_t rot, bool half, const int32_t* positions, const float* table,
                          uint32_t table_rows, float scale, const Rows* qo, const KvView* kv, const SeqView* sq,
                          hipStream_t s);
+// cache8.hip: the same with a cache held in 8 bits (q with qo may be null); entries
+// of any cache as rows (k or v without data: not read).
+hipError_t launch_append8(const Rows* q, const Rows& k, const Rows& v, uint32_t T, uint32_t heads, uint32_t dim,
+                          uint32_t rot, bool half, const int32_t* positions, const float* table, uint32_t table_rows,
+                          float scale, const Rows* qo, const KvView& kv, const SeqView& sq, hipStream_t s);
+hipError_t launch_cache_read(const KvView& kv, const SeqView& sq, uint32_t T, const Rows& k, const Rows& v,
+                             hipStream_t s);
 // Any types, dims and strides; tokens > 0; lse (tokens x heads floats) may be null.
 hipError_t launch_attend_any(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
                              float scale, const Rows& out, float inv_scale, float* lse, hipStream_t s);

@@ -55,17 +55,8 @@ struct RotaryArgs {
     bool has_q, has_kv;
 };
 
-// Where token t's entry of the cache lies: false if it has none.
 __device__ __forceinline__ bool entry_of(const RotaryArgs& a, uint32_t t, uint32_t& page, uint32_t& at) {
-    const uint32_t s = seq_of(a.sq, t);
-    const SeqSpan sp = seq_span(a.sq, a.kv.shift, s, a.T);
-    const int64_t e = (int64_t)sp.n - sp.c + ((int64_t)t - sp.q0);
-    if (t < sp.q0 || t >= sp.q0 + sp.c || e < 0) return false;
-    const int32_t pg = a.sq.table[(size_t)s * a.sq.ts + (size_t)(e >> a.kv.shift)];
-    if (pg < 0 || (uint32_t)pg >= a.kv.pages) return false;
-    page = (uint32_t)pg;
-    at = (uint32_t)e & ((1u << a.kv.shift) - 1);
-    return true;
+    return token_entry(a.sq, a.kv, a.T, t, page, at);
 }
 
 // Any dim, rot, strides: one thread per pair (rotated or passed) of a head's row.
