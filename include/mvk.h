@@ -866,6 +866,101 @@ mvk_status mvk_cache_evict(const mvk_kv *src, const mvk_seqs *seqs, const float 
                            const int32_t *dst_table, uint64_t dst_table_stride, uint32_t dst_width, float *w_out,
                            uint64_t o_seq, uint64_t o_head, int32_t *kept, int32_t *lens_out, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * The client's other nonlinear operations: the norms around a block, the gated
+ * activation of the feed-forward part, and the token that answers.  Rows are
+ * T x n, element i of row t at data[t*token + i] (mvk_rows, whose head is not
+ * used); values, rounding and types as above.
+ */
+#define MVK_NORM_RMS 0   /* v rsqrt(mean v^2 + eps) weight + bias */
+#define MVK_NORM_LAYER 1 /* the same of v - mean v */
+
+/* A norm over the n values of a row.  weight, bias: device, n values of `type`
+ * (BF16, F16 or F32), NULL for ones and zeros. */
+typedef struct mvk_norm {
+    const void *weight;
+    const void *bias;
+    int32_t type;
+    int32_t kind; /* MVK_NORM_* */
+    float eps;
+} mvk_norm;
+
+/* Longest row of mvk_block_norm. */
+#define MVK_MAX_NORM 32768u
+
+/*
+ * The end of a block and the beginning of the next:
+ *   h = residual + scale * gate * after(x),   out = before(h)
+ *   x            : the block's result, floats or FIELD times x_scale; NULL: h is the residual
+ *   residual     : BF16, F16 or F32; NULL: zeros (one of x and residual is given)
+ *   after        : norm of x, or NULL
+ *   gate         : floats of any type, T x n, or one row for all (token stride 0), or NULL
+ *   residual_out : h, BF16, F16 or F32, or NULL
+ *   before, out  : out is before(h) (before NULL: h) in BF16, F16, F32 or FIELD (over
+ *                  out_scale, rounded to nearest and clamped); out NULL: only residual_out
+ * Both norms are of values in 32 bits (h before it is rounded).  With a FIELD out
+ * everything is computed in 64 bits, so that its whole numbers are the nearest ones.
+ * residual_out may be residual itself and out x itself (same type and stride);
+ * else outputs share no memory with inputs or each other (MVK_EINVAL where rows meet).
+ * Errors: MVK_EINVAL, MVK_ERANGE (n > MVK_MAX_NORM, T above 2^31 - 1, buffers above 2^62 bytes).
+ */
+mvk_status mvk_block_norm(const mvk_rows *x, float x_scale, const mvk_rows *residual, uint32_t T, uint32_t n,
+                          const mvk_norm *after, const mvk_rows *gate, float scale, const mvk_rows *residual_out,
+                          const mvk_norm *before, const mvk_rows *out, float out_scale, void *stream);
+
+#define MVK_ACT_SILU 0      /* g / (1 + exp(-g)) */
+#define MVK_ACT_GELU 1      /* g Phi(g), Phi the normal distribution function */
+#define MVK_ACT_GELU_TANH 2 /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+#define MVK_ACT_RELU 3      /* max(g, 0) */
+
+/*
+ * out = act(gate) * up, value by value, in 32 bits.
+ *   gate, up : T x n, one type, floats or FIELD times in_scale
+ *   out      : floats, or FIELD (over out_scale, rounded to nearest and clamped); may be
+ *              gate or up itself (same type and stride), else shares no memory with them
+ * Errors: MVK_EINVAL, MVK_ERANGE (T or n above 2^31 - 1, buffers above 2^62 bytes).
+ */
+mvk_status mvk_gated_activation(const mvk_rows *gate, const mvk_rows *up, uint32_t T, uint32_t n, int32_t act,
+                                float in_scale, const mvk_rows *out, float out_scale, void *stream);
+
+/*
+ * How tokens are drawn: one value for all rows, or, where the pointer is not NULL,
+ * one a row (device).  temperature <= 0: the largest logit.  top_k < 1: off.
+ * top_p >= 1: off.  min_p <= 0: off.  A not-a-number is off (a temperature: the
+ * largest logit).
+ */
+typedef struct mvk_sampling {
+    double temperature;
+    double top_p;
+    double min_p;
+    int32_t top_k;
+    const float *temperatures;
+    const float *top_ps;
+    const float *min_ps;
+    const int32_t *top_ks;
+} mvk_sampling;
+
+/*
+ * A token for every row of logits x (R rows of n, floats, or FIELD times
+ * field_scale > 0), from given random numbers.  In the order of falling logits
+ * (ties: the lowest index first) the weights are w_i = exp((x_i - max x) / temperature);
+ * kept are those among the first top_k, in the shortest prefix whose weights reach
+ * top_p of what top_k left, and of at least min_p (min_p <= 1).  The token is the first
+ * index, in the order of the vocabulary, up to which the kept weights sum to more
+ * than u times their total.
+ *   u      : device, R floats in [0, 1) (clamped to it; not-a-number: 0)
+ *   tokens : device, R int32, written; -1 where no logit is above -inf
+ *   probs  : NULL, or device, R floats: the token's share of the kept weights
+ * A not-a-number counts as -inf, which is never drawn; logits of +inf share all
+ * the weight.  Weights are whole multiples of 2^-44 (n up to 2^17; one bit less for
+ * every doubling of n), so sums are exact and have no order.
+ * Errors: MVK_EINVAL (null, n zero, outputs in each other's or the inputs' memory,
+ * field_scale not finite and positive), MVK_ERANGE (R or n above 2^24, buffers
+ * above 2^62 bytes), MVK_ENOMEM, MVK_ECAPTURE (workspace).
+ */
+mvk_status mvk_sample_tokens(const mvk_rows *logits, uint32_t R, uint32_t n, float field_scale,
+                             const mvk_sampling *how, const float *u, int32_t *tokens, float *probs, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

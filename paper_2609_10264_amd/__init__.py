@@ -807,3 +807,7 @@ from .attention import (FIELD, KVCache, Sequences, cache_evict, cache_read, page
 
 __all__ += ["FIELD", "KVCache", "Sequences", "rotary_table", "rotary", "rotary_append", "cache_read",
             "paged_attention", "cache_evict"]
+
+from .steps import Norm, block_norm, gated_activation, sample  # noqa: E402
+
+__all__ += ["Norm", "block_norm", "gated_activation", "sample"]

@@ -86,6 +86,9 @@ EXPORTS = (
     "mvk_paged_attention",
     "mvk_cache_evict",
     "mvk_cache_read",
+    "mvk_block_norm",
+    "mvk_gated_activation",
+    "mvk_sample_tokens",
 )
 
 
@@ -187,6 +190,38 @@ class MvkSeqs(ctypes.Structure):
         ("lens", ctypes.c_void_p),
         ("q_start", ctypes.c_void_p),
         ("max_new", ctypes.c_uint32),
+    ]
+
+
+MVK_NORM_RMS = 0
+MVK_NORM_LAYER = 1
+MVK_MAX_NORM = 32768
+MVK_ACT_SILU = 0
+MVK_ACT_GELU = 1
+MVK_ACT_GELU_TANH = 2
+MVK_ACT_RELU = 3
+
+
+class MvkNorm(ctypes.Structure):
+    _fields_ = [
+        ("weight", ctypes.c_void_p),
+        ("bias", ctypes.c_void_p),
+        ("type", ctypes.c_int32),
+        ("kind", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+    ]
+
+
+class MvkSampling(ctypes.Structure):
+    _fields_ = [
+        ("temperature", ctypes.c_double),
+        ("top_p", ctypes.c_double),
+        ("min_p", ctypes.c_double),
+        ("top_k", ctypes.c_int32),
+        ("temperatures", ctypes.c_void_p),
+        ("top_ps", ctypes.c_void_p),
+        ("min_ps", ctypes.c_void_p),
+        ("top_ks", ctypes.c_void_p),
     ]
 
 
@@ -325,6 +360,13 @@ def load(p: int = MVK_PRIME) -> ctypes.CDLL:
     L.mvk_cache_evict.restype = st
     L.mvk_cache_read.argtypes = [kv, seqs, u32, rows, rows, vp]
     L.mvk_cache_read.restype = st
+    norm, how = ctypes.POINTER(MvkNorm), ctypes.POINTER(MvkSampling)
+    L.mvk_block_norm.argtypes = [rows, f32, rows, u32, u32, norm, rows, f32, rows, norm, rows, f32, vp]
+    L.mvk_block_norm.restype = st
+    L.mvk_gated_activation.argtypes = [rows, rows, u32, u32, i32, f32, rows, f32, vp]
+    L.mvk_gated_activation.restype = st
+    L.mvk_sample_tokens.argtypes = [rows, u32, u32, f32, how, vp, vp, vp, vp]
+    L.mvk_sample_tokens.restype = st
     if L.mvk_abi_version() != ABI_VERSION:
         raise ImportError(f"{path}: ABI version mismatch; rebuild the library")
     if L.mvk_field_modulus() != p:

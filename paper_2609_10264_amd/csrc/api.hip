@@ -21,6 +21,7 @@
 #include "kv.h"
 #include "mvk_internal.h"
 #include "overlap.h"
+#include "rowio.h"
 
 namespace mvk {
 namespace {
@@ -1472,6 +1473,126 @@ mvk_status mvk_cache_evict(const mvk_kv* src, const mvk_seqs* seqs, const float*
     return hip_status(launch_evict(view_of(src), view_of(seqs), type_size(src->type), w, w_seq, w_head, budget, recent,
                                    sinks, view_of(dst), dst_table, dst_table_stride, dst_width, w_out, o_seq, o_head,
                                    kept, lens_out, (hipStream_t)stream));
+}
+
+// ---------------------------------------------------------------------------
+// The client's other nonlinear operations
+// ---------------------------------------------------------------------------
+}  // extern "C"
+
+namespace {
+
+Matrix matrix_of(const mvk_rows* r, uint32_t T) {
+    return r ? Matrix{r->data, (size_t)r->token, r->type, is_wide(r->data, r->token, r->type, T)} : Matrix{};
+}
+
+// Do rows of a and b meet, other than as the same rows?
+bool meet(const mvk_rows* a, const mvk_rows* b, uint32_t T, uint32_t n, bool same_is_fine) {
+    if (!a || !b) return false;
+    if (same_is_fine && a->data == b->data && a->type == b->type && (a->token == b->token || T <= 1)) return false;
+    return share_memory(row_set(a, T, 1, n), row_set(b, T, 1, n));
+}
+
+// Rows of n values that are written: each its own memory.
+mvk_status check_written(const mvk_rows* r, uint32_t T, uint32_t n) {
+    return T > 1 && r->token < n ? MVK_EINVAL : MVK_OK;
+}
+
+mvk_status check_norm(const mvk_norm* w) {
+    if (!w) return MVK_OK;
+    if (w->kind != MVK_NORM_RMS && w->kind != MVK_NORM_LAYER) return MVK_EINVAL;
+    if (!is_float_type(w->type) || !(w->eps >= 0) || !std::isfinite(w->eps)) return MVK_EINVAL;
+    const size_t e = type_size(w->type);
+    return ((uintptr_t)w->weight | (uintptr_t)w->bias) % e ? MVK_EINVAL : MVK_OK;
+}
+
+NormView norm_of(const mvk_norm* w) {
+    if (!w) return NormView{};
+    const bool wide = ((uintptr_t)w->weight | (uintptr_t)w->bias) % 16 == 0;
+    return NormView{w->weight, w->bias, w->type, w->kind, w->eps, wide, true};
+}
+
+inline bool is_scale(float x) { return std::isfinite(x) && x > 0; }
+
+}  // namespace
+
+extern "C" {
+
+mvk_status mvk_block_norm(const mvk_rows* x, float x_scale, const mvk_rows* residual, uint32_t T, uint32_t n,
+                          const mvk_norm* after, const mvk_rows* gate, float scale, const mvk_rows* residual_out,
+                          const mvk_norm* before, const mvk_rows* out, float out_scale, void* stream) {
+    if ((!x && !residual) || (!residual_out && !out) || (!x && (after || gate)) || (before && !out) || !n) return MVK_EINVAL;
+    if (!std::isfinite(scale)) return MVK_EINVAL;
+    if (n > MVK_MAX_NORM || T > 0x7fffffffu) return MVK_ERANGE;
+    mvk_status st = MVK_OK;
+    for (const mvk_rows* r : {x, residual, gate, residual_out, out}) {
+        if (!r) continue;
+        if ((st = check_rows(r, T, 1))) return st;
+        if (r->type == MVK_TYPE_FIELD && r != x && r != out) return MVK_EINVAL;
+    }
+    if ((st = check_norm(after)) || (st = check_norm(before))) return st;
+    if (x && x->type == MVK_TYPE_FIELD && !std::isfinite(x_scale)) return MVK_EINVAL;
+    if (out && out->type == MVK_TYPE_FIELD && !is_scale(out_scale)) return MVK_EINVAL;
+    for (const mvk_rows* w : {residual_out, out}) {
+        if (!w) continue;
+        if ((st = check_written(w, T, n))) return st;
+        // (a row is read before any of it is written)
+        if (meet(w, x, T, n, w == out) || meet(w, residual, T, n, w == residual_out) || meet(w, gate, T, n, false))
+            return MVK_EINVAL;
+        for (const mvk_norm* m : {after, before}) {
+            if (!m) continue;
+            const uint64_t len = n * type_size(m->type);
+            for (const void* p : {m->weight, m->bias})
+                if (p && share_memory({p, 1, 0, 1, 0, len}, row_set(w, T, 1, n))) return MVK_EINVAL;
+        }
+    }
+    if (meet(residual_out, out, T, n, false)) return MVK_EINVAL;
+    if (T == 0) return MVK_OK;
+    NormArgs a = {matrix_of(x, T), matrix_of(residual, T), matrix_of(gate, T), matrix_of(residual_out, T), matrix_of(out, T),
+                  norm_of(after), norm_of(before), T, n, x_scale, scale, out_scale};
+    return hip_status(launch_block_norm(a, (hipStream_t)stream));
+}
+
+mvk_status mvk_gated_activation(const mvk_rows* gate, const mvk_rows* up, uint32_t T, uint32_t n, int32_t act,
+                                float in_scale, const mvk_rows* out, float out_scale, void* stream) {
+    if (act < MVK_ACT_SILU || act > MVK_ACT_RELU || !n) return MVK_EINVAL;
+    if (n > 0x7fffffffu || T > 0x7fffffffu) return MVK_ERANGE;
+    mvk_status st = MVK_OK;
+    for (const mvk_rows* r : {gate, up, out})
+        if ((st = check_rows(r, T, 1))) return st;
+    if (too_big(T, n, 4)) return MVK_ERANGE;
+    if (gate->type != up->type || (st = check_written(out, T, n))) return MVK_EINVAL;
+    if (gate->type == MVK_TYPE_FIELD && !std::isfinite(in_scale)) return MVK_EINVAL;
+    if (out->type == MVK_TYPE_FIELD && !is_scale(out_scale)) return MVK_EINVAL;
+    // (a value is read before its place is written, by the same thread)
+    if (meet(out, gate, T, n, true) || meet(out, up, T, n, true)) return MVK_EINVAL;
+    if (T == 0) return MVK_OK;
+    const GatedArgs a = {matrix_of(gate, T), matrix_of(up, T), matrix_of(out, T), T, n, act, in_scale,
+                         out->type == MVK_TYPE_FIELD ? 1.f / out_scale : 1.f};
+    return hip_status(launch_gated(a, (hipStream_t)stream));
+}
+
+mvk_status mvk_sample_tokens(const mvk_rows* logits, uint32_t R, uint32_t n, float field_scale,
+                             const mvk_sampling* how, const float* u, int32_t* tokens, float* probs, void* stream) {
+    mvk_status st = check_rows(logits, R, 1);
+    if (st) return st;
+    if (!how || !n || (R && (!u || !tokens))) return MVK_EINVAL;
+    if (R > (1u << 24) || n > (1u << 24)) return MVK_ERANGE;
+    if (logits->type == MVK_TYPE_FIELD && !is_scale(field_scale)) return MVK_EINVAL;
+    for (const void* w : {(const void*)tokens, (const void*)probs}) {
+        if (!w) continue;
+        const RowSet rows = {w, 1, 0, 1, 0, 4ull * R};
+        if (share_memory(rows, row_set(logits, R, 1, n))) return MVK_EINVAL;
+        for (const void* p : {(const void*)u, (const void*)how->temperatures, (const void*)how->top_ks,
+                              (const void*)how->top_ps, (const void*)how->min_ps, (const void*)(w == tokens ? probs : nullptr)})
+            if (p && share_memory(rows, {p, 1, 0, 1, 0, 4ull * R})) return MVK_EINVAL;
+    }
+    if (R == 0) return MVK_OK;
+    DrawArgs a = {matrix_of(logits, R), R, n, field_scale, *how, u, tokens, probs};
+    void* ws = nullptr;
+    const size_t bytes = draw_bytes(a);
+    if (bytes && (st = workspace((hipStream_t)stream, bytes, &ws))) return st;
+    return hip_status(launch_draw(a, ws, (hipStream_t)stream));
 }
 
 }  // extern "C"

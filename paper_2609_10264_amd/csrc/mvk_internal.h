@@ -316,6 +316,17 @@ hipError_t launch_evict(const KvView& src, const SeqView& sq, size_t elem, const
                         size_t dts, uint32_t dwidth, float* wo, size_t o_seq, size_t o_head, int32_t* kept,
                         int32_t* lens_out, hipStream_t s);
 
+// norm.hip, gated.hip, draw.hip (rows: rowio.h) --------------------------------
+struct Matrix;
+struct NormArgs;
+struct GatedArgs;
+struct DrawArgs;
+hipError_t launch_block_norm(const NormArgs& a, hipStream_t s);
+hipError_t launch_gated(const GatedArgs& a, hipStream_t s);
+// ws: draw_bytes.
+size_t draw_bytes(const DrawArgs& a);
+hipError_t launch_draw(const DrawArgs& a, void* ws, hipStream_t s);
+
 inline uint32_t ceil_div(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
 
 }  // namespace mvk

@@ -1,0 +1,394 @@
+"""mvk_block_norm and mvk_gated_activation against their definitions in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from tests import attention_ref as ref
+from tests import steps_ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+BF, HF, F32, FIELD = torch.bfloat16, torch.float16, torch.float32, torch.int32
+P, BB = 2**31 - 1, 15 * 2**27 + 1
+U = 2.0**-24
+
+
+def _make(shape, dtype, seed, spread=1.0, p=P):
+    x = torch.randn(shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64) * spread
+    return ref.embed((x * 2**16).round().long(), p) if dtype == FIELD else x.to(dtype)
+
+
+def _close(got, want, err, what):
+    got = got.double().cpu()
+    assert torch.equal(got.isnan(), want.isnan()), what
+    ok = (got == want) | ((got - want).abs() <= err) | want.isnan()
+    assert bool(ok.all()), (what, int((~ok).sum()), float((got - want).abs().nan_to_num(0).max()))
+
+
+class Case:
+    def __init__(self, T, n, x=BF, res=BF, params=F32, kind="rms", after=True, before=True, gate="channel", scale=0.5,
+                 bias=None, weight=True, seed=1, p=P, eps=1e-6):
+        import paper_2609_10264_amd as mvk
+        self.p, self.scale, self.T, self.n = p, scale, T, n
+        self.x = _make((T, n), x, seed, p=p) if x else None
+        self.res = _make((T, n), res, seed + 1, 3.0) if res else None
+        bias = kind == "layer" if bias is None else bias
+        self.norms = {}
+        for i, (name, on) in enumerate((("after", after), ("before", before))):
+            w = (1 + 0.3 * _make((n,), F32, seed + 5 + i)).to(params) if weight else None
+            b = _make((n,), params, seed + 7 + i) if bias else None
+            self.norms[name] = (w, b, kind, eps) if on else None
+        self.gate = {"none": None, "channel": _make((n,), params, seed + 9), "token": _make((T, n), params, seed + 9)}[gate]
+        self.dev = {k: mvk.Norm(*(t.cuda() if isinstance(t, torch.Tensor) else t for t in v)) if v else None
+                    for k, v in self.norms.items()}
+
+    def call(self, **kw):
+        import paper_2609_10264_amd as mvk
+        args = dict(before=self.dev["before"], after=self.dev["after"], scale=self.scale, field_scale=2.0**-16, p=self.p)
+        for name, t in (("x", self.x), ("residual", self.res), ("gate", self.gate)):
+            if name not in kw:  # (nothing is copied within a capture)
+                args[name] = t.cuda() if t is not None else None
+        return mvk.block_norm(**args, **kw)
+
+    def check(self, out, h, out_scale=None):
+        lift = lambda t: ref.lift(t, 2.0**-16, self.p) if t is not None else None  # noqa: E731
+        x, res = lift(self.x), self.res.double() if self.res is not None else None
+        y, want = steps_ref.block(x, res, self.norms["before"], self.norms["after"], self.gate, self.scale)
+        n = self.n
+        # Sizes that the rounding errors of 32 bits are relative to: of after(x), then of h.  A mean of n
+        # values by a tree and 32 in a row is off by (32 + log2 n + 2) roundings of the mean of their sizes,
+        # and each step after it by one.
+        many = (32 + math.log2(n) + 10) * U
+
+        def grown(v, dv, w):  # error of norm(v) from that of v
+            weight, bias, kind, eps = w
+            size = v.abs()
+            if kind == "layer":
+                dv = dv + dv.mean(-1, keepdim=True) + many * (size + size.mean(-1, keepdim=True))
+                v = v - v.mean(-1, keepdim=True)
+                size = v.abs()
+            rms = (v.square().mean(-1, keepdim=True) + eps).sqrt()
+            # relative error of the norm: of the squares' mean (half of it) with what dv does to it
+            dr = many + (v.abs() * dv).mean(-1, keepdim=True) / rms**2
+            g = weight.double().abs() if weight is not None else 1.0
+            e = (dv + size * dr) / rms * g
+            return e + 4 * U * (bias.double().abs() + size / rms * g if bias is not None else size / rms * g)
+
+        t, dt = x, (x.abs() * 2 * U if x is not None else None)  # (a field element in 24 bits)
+        if t is not None:
+            if self.norms["after"]:
+                dt = grown(t, dt, self.norms["after"])
+                t = steps_ref.norm(t, *self.norms["after"])
+            g = self.gate.double().abs() if self.gate is not None else 1.0
+            dt = (dt + 3 * U * t.abs()) * g * abs(self.scale)
+            dh = dt + U * want.abs() * 2
+        else:
+            dh = torch.zeros_like(want)
+        if h is not None:
+            _close(h, want, dh + ROUND(h) * want.abs() * 1.0001 + TINY(h), "h")
+        if out is None:
+            return
+        dy = grown(want, dh, self.norms["before"]) if self.norms["before"] else dh
+        if out.dtype == FIELD:
+            # 64 bits: the nearest whole number, but for one next to a border
+            got = ref.lift(out.cpu(), 1.0, self.p)
+            one = float(torch.tensor(out_scale, dtype=F32))  # (the call takes a 32-bit float: 1e-3 is none)
+            exact = (y / one).clamp(-(self.p // 2), self.p // 2)
+            assert bool(((got - exact).abs() <= 0.5 + 2.0**-40 * (1 + exact.abs()) * n).all())
+        else:
+            _close(out, y, dy + ROUND(out) * (y.abs() + dy) + TINY(out), "out")
+
+
+def ROUND(t):
+    return steps_ref.ROUND[t.dtype]
+
+
+def TINY(t):  # half the spacing of the smallest numbers
+    return {BF: 2.0**-134, HF: 2.0**-25, F32: 2.0**-150}[t.dtype]
+
+
+@pytest.mark.parametrize("n", [1, 2, 7, 8, 9, 63, 64, 65, 511, 512, 520, 1000, 2048, 4096, 4097, 8192, 11008, 16384, 20001, 32768])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_widths(n, kind):
+    print(f"norm n={n} {kind}", flush=True)
+    c = Case(5, n, kind=kind)
+    out, h = c.call()
+    assert out.dtype == h.dtype == BF
+    c.check(out, h)
+    c = Case(3, n, x=FIELD, res=F32, kind=kind, after=False, gate="none", scale=1.0, seed=3)
+    c.check(*c.call())
+    out, h = c.call(out_dtype=FIELD, out_scale=2.0**-16)
+    c.check(out, h, 2.0**-16)
+
+
+@pytest.mark.parametrize("x", [BF, HF, F32, FIELD])
+@pytest.mark.parametrize("res", [BF, HF, F32])
+@pytest.mark.parametrize("out", [BF, HF, F32, FIELD])
+@pytest.mark.parametrize("params", [BF, HF, F32])
+def test_types(x, res, out, params):
+    for n in (72, 77):
+        c = Case(4, n, x=x, res=res, params=params, kind="layer", gate="token")
+        y, h = c.call(out_dtype=out, out_scale=2.0**-12)
+        assert y.dtype == out and h.dtype == res
+        c.check(y, h, 2.0**-12)
+
+
+@pytest.mark.parametrize("after", [False, True])
+@pytest.mark.parametrize("before", [False, True])
+@pytest.mark.parametrize("gate", ["none", "channel", "token"])
+@pytest.mark.parametrize("res", [None, F32])
+def test_parts(after, before, gate, res):
+    c = Case(6, 264, after=after, before=before, gate=gate, res=res, scale=-1.5, weight=gate != "none", bias=gate == "token")
+    y, h = c.call()
+    assert (y is None) == (not before) and h.dtype == F32
+    c.check(y, h)
+    y, h = c.call(out_dtype=HF)  # without `before`: h itself
+    c.check(y, h)
+
+
+def test_without_a_block():
+    c = Case(6, 264, x=None, after=False, gate="none")
+    y, h = c.call()
+    c.check(y, h)
+    assert torch.equal(h.cpu(), c.res)
+
+
+@pytest.mark.parametrize("T", [0, 1, 2, 257, 3000])
+def test_rows(T):
+    c = Case(T, 136)
+    c.check(*c.call())
+
+
+@pytest.mark.parametrize("p", [P, BB])
+def test_field_both_ways(p):
+    c = Case(7, 1000, x=FIELD, res=F32, p=p)
+    for scale in (2.0**-16, 2.0**-25, 1e-3):
+        y, h = c.call(out_dtype=FIELD, out_scale=scale)
+        assert int(y.min()) >= 0 and int(y.max()) < p
+        c.check(y, h, scale)
+    y, h = c.call(out_dtype=FIELD, out_scale=1e-12)  # most are clamped (values below 0.001 are not)
+    c.check(y, h, 1e-12)
+    assert int((ref.lift(y.cpu(), 1.0, p).abs() == (p - 1) // 2).sum()) > 6900
+
+
+def test_in_place():
+    c = Case(9, 520, x=BF, res=BF)
+    want_y, want_h = c.call()
+    x, res = c.x.cuda(), c.res.cuda()
+    y, h = c.call(x=x, residual=res, out=x, residual_out=res)
+    assert y is x and h is res and torch.equal(y, want_y) and torch.equal(h, want_h)
+
+
+@pytest.mark.parametrize("n", [128, 100])
+def test_strides(n):
+    import paper_2609_10264_amd as mvk
+    c = Case(9, n, gate="token")
+    want = c.call()
+
+    def wide(t, lead):
+        b = torch.full((9, n + 24), 5.0, dtype=t.dtype, device="cuda")
+        b[:, lead:lead + n] = t.cuda()
+        return b, b[:, lead:lead + n]
+
+    for lead in (8, 3):
+        (_, x), (_, res), (_, g) = wide(c.x, lead), wide(c.res, 8 - lead), wide(c.gate, lead)
+        whole_y, y = wide(torch.zeros_like(c.x), lead)
+        whole_h, h = wide(torch.zeros_like(c.x), lead)
+        c.call(x=x, residual=res, gate=g, out=y, residual_out=h)
+        assert torch.equal(y, want[0]) and torch.equal(h, want[1])
+        for b in (whole_y, whole_h):  # nothing else was written
+            assert bool((b[:, :lead] == 5).all()) and bool((b[:, lead + n:] == 5).all())
+    one = c.gate[:1].cuda()
+    a = c.call(gate=one.expand(9, n))
+    b = c.call(gate=one[0])
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    assert isinstance(mvk.Norm(), mvk.Norm)
+
+
+def test_not_finite_rows_stay_by_themselves():
+    c = Case(5, 300, x=F32, res=F32, after=False, gate="none")
+    c.x[1, 7] = math.nan
+    c.x[3, 299] = math.inf
+    y, h = c.call()
+    assert bool(y[1].isnan().all()) and bool(y[3].isnan().any())
+    keep = torch.tensor([0, 2, 4])
+    sub = Case(5, 300, x=F32, res=F32, after=False, gate="none")
+    y2, h2 = sub.call()
+    assert torch.equal(y[keep.cuda()], y2[keep.cuda()])
+    f, _ = c.call(out_dtype=FIELD, out_scale=2.0**-16)  # a not-a-number is 0
+    assert bool((f[1] == 0).all())
+
+
+def test_zero_rows_and_large_values():
+    for eps in (1e-6, 1e-12):
+        c = Case(4, 256, x=F32, res=F32, after=False, gate="none", scale=1.0, eps=eps)
+        c.x[0], c.res[0] = 0, 0
+        c.x[1] *= 1e15
+        c.x[2] *= 1e-6
+        c.res[2] *= 1e-6
+        c.check(*c.call())
+
+
+def test_in_a_graph_and_on_another_stream():
+    c = Case(33, 520)
+    x, res = c.x.cuda(), c.res.cuda()
+    want = c.call()
+    y, h = torch.zeros_like(x), torch.zeros_like(res)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    c.call(x=x, residual=res, out=y, residual_out=h, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(y, want[0]) and torch.equal(h, want[1])
+    gate = c.gate.cuda()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        c.call(x=x, residual=res, gate=gate, out=y, residual_out=h)
+    for i in range(3):
+        x.mul_(0.5)
+        y.zero_(), h.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = c.call(x=x, residual=res)
+        assert torch.equal(y, eager[0]) and torch.equal(h, eager[1])
+
+
+def test_refusals():
+    import paper_2609_10264_amd as mvk
+    c = Case(4, 64)
+    x, res = c.x.cuda(), c.res.cuda()
+    w = mvk.Norm(c.norms["before"][0].cuda())
+    for bad in (dict(x=None, residual=None), dict(x=None, residual=res, gate=x), dict(x=x, after=mvk.Norm(kind="batch")),
+                dict(x=x, before=mvk.Norm(torch.ones(63, device="cuda"))), dict(x=x, residual=res[:, :32]),
+                dict(x=x, residual=res[:2]), dict(x=x, gate=x[:, :5]), dict(x=x.t(), residual=None),
+                dict(x=x, out_dtype=FIELD), dict(x=ref.embed(c.x.long()).cuda())):
+        with pytest.raises((ValueError, mvk.MvkError)):
+            mvk.block_norm(**{"x": x, **bad})
+    for bad in (dict(x=x.cpu()), dict(x=x.double()), dict(x=x, before=mvk.Norm(torch.ones(64))),
+                dict(x=x, before=mvk.Norm(w.weight, w.weight.half()))):
+        with pytest.raises(TypeError):
+            mvk.block_norm(**bad)
+    buf = torch.zeros((4, 70), dtype=BF, device="cuda")
+    a, b = buf[:, :64], buf[:, 4:68]
+    for bad in (dict(x=a, out=b, before=w), dict(x=a, residual_out=b), dict(x=x, residual=a, residual_out=b),
+                dict(x=a, residual_out=a), dict(x=x, residual=a, out=a, before=w), dict(x=x, gate=a, out=a),
+                dict(x=x, out=a, residual_out=b), dict(x=x, out=a, residual_out=a),
+                dict(x=x, residual_out=torch.zeros((1, 64), dtype=BF, device="cuda").expand(4, 64)),
+                dict(x=x, residual=res.to(torch.int32)), dict(x=x, scale=math.inf), dict(x=x, before=mvk.Norm(eps=-1.0)),
+                dict(x=x, out_dtype=FIELD, out_scale=0.0)):
+        with pytest.raises(mvk.MvkError):
+            mvk.block_norm(**bad)
+    wide = torch.zeros((1, 32769), device="cuda")
+    with pytest.raises(mvk.MvkError):
+        mvk.block_norm(wide)
+
+
+# ---------------------------------------------------------------------------
+ACTS = ["silu", "gelu", "gelu_tanh", "relu"]
+
+
+def _gated_err(g, u, act, want):
+    # the argument in 24 bits, the exponent's argument in 32 bits (a relative error of |g| (or its
+    # polynomial) roundings in the exponential), and a few roundings after it; expf and erfcf to 4 units
+    if act == "relu":
+        return 6 * U * want.abs()
+    arg = {"silu": g.abs(), "gelu": g.square(), "gelu_tanh": 1.6 * g.abs() + 0.15 * g.abs()**3}[act]
+    # (below the smallest normal number an exponential or a result may be lost)
+    return (16 + 6 * arg) * U * want.abs() + 2.0**-126 * (1 + g.abs()) * (1 + u.abs())
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", [BF, HF, F32, FIELD])
+@pytest.mark.parametrize("n", [1, 8, 77, 1000])
+def test_gated(act, dtype, n):
+    import paper_2609_10264_amd as mvk
+    g, u = _make((13, n), dtype, 1, 3.0), _make((13, n), dtype, 2)
+    gd, ud = ref.lift(g, 2.0**-16), ref.lift(u, 2.0**-16)
+    want = steps_ref.activation(gd, act) * ud
+    err = _gated_err(gd, ud, act, want)
+    for out in (BF, HF, F32):
+        y = mvk.gated_activation(g.cuda(), u.cuda(), act=act, field_scale=2.0**-16, out_dtype=out)
+        _close(y, want, err + ROUND(y) * (want.abs() + err) + TINY(y), (act, out))
+    y = mvk.gated_activation(g.cuda(), u.cuda(), act=act, field_scale=2.0**-16)
+    assert y.dtype == (F32 if dtype == FIELD else dtype)
+    f = mvk.gated_activation(g.cuda(), u.cuda(), act=act, field_scale=2.0**-16, out_dtype=FIELD, out_scale=2.0**-10)
+    assert bool(((ref.lift(f.cpu()) - want * 2**10).abs() <= 0.5 + (err + U * want.abs()) * 2**10).all())
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_gated_far_values(act):
+    import paper_2609_10264_amd as mvk
+    g = torch.tensor([[-200.0, -104.0, -88.0, -40.0, -12.0, -5.5, -1e-30, -0.0, 0.0, 1e-30, 5.5, 12.0, 40.0, 88.0, 104.0, 200.0,
+                       1e30, -1e30, math.inf]], dtype=F32)
+    u = torch.full_like(g, -3.0)
+    y = mvk.gated_activation(g.cuda(), u.cuda(), act=act)
+    want = steps_ref.activation(g.double(), act) * u.double()
+    want[0, -2] = 0.0 if act != "relu" else want[0, -2]
+    _close(y, want, _gated_err(g.double().clamp(-1e3, 1e3), u.double(), act, want).nan_to_num(0), act)
+    bad = torch.tensor([[math.nan, 1.0, -math.inf]], dtype=F32)
+    y = mvk.gated_activation(bad.cuda(), torch.ones_like(bad).cuda(), act=act)
+    assert bool(y[0, 0].isnan()) and bool(y[0, 1].isfinite())
+
+
+@pytest.mark.parametrize("n", [128, 100])
+def test_gated_views_and_places(n):
+    import paper_2609_10264_amd as mvk
+    both = _make((9, 2 * n), BF, 4).cuda()
+    g, u = both[:, :n], both[:, n:]
+    want = mvk.gated_activation(g.contiguous(), u.contiguous())
+    assert torch.equal(mvk.gated_activation(g, u), want)
+    for i in (0, 1):
+        b = both.clone()
+        parts = b[:, :n], b[:, n:]
+        out = mvk.gated_activation(*parts, out=parts[i])
+        assert out is parts[i] and torch.equal(out, want)
+        assert torch.equal(parts[1 - i], (g, u)[1 - i])
+    assert mvk.gated_activation(g[:0], u[:0]).shape == (0, n)
+
+
+def test_gated_in_a_graph():
+    import paper_2609_10264_amd as mvk
+    g, u = _make((9, 200), FIELD, 4).cuda(), _make((9, 200), FIELD, 5).cuda()
+    out = torch.zeros((9, 200), dtype=FIELD, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def call(**kw):
+        return mvk.gated_activation(g, u, field_scale=2.0**-16, out_scale=2.0**-9, **kw)
+
+    call(out=out, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(out, call(out_dtype=FIELD))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call(out=out)
+    for i in range(3):
+        g.copy_(_make((9, 200), FIELD, 10 + i))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, call(out_dtype=FIELD))
+
+
+def test_gated_refusals():
+    import paper_2609_10264_amd as mvk
+    x = torch.zeros((4, 64), dtype=BF, device="cuda")
+    for bad in (dict(act="tanh"), dict(up=x[:2]), dict(up=x[:, :8]), dict(gate=x.t()), dict(out_dtype=FIELD),
+                dict(gate=x.int(), up=x.int())):
+        with pytest.raises(ValueError):
+            mvk.gated_activation(**{"gate": x, "up": x, **bad})
+    with pytest.raises(TypeError):
+        mvk.gated_activation(x.cpu(), x)
+    buf = torch.zeros((4, 70), dtype=BF, device="cuda")
+    for bad in (dict(up=x.half()), dict(gate=buf[:, :64], out=buf[:, 4:68]), dict(up=buf[:, :64], out=buf[:, 4:68]),
+                dict(out=x[:1].expand(4, 64)), dict(out_dtype=FIELD, out_scale=-1.0)):
+        with pytest.raises(mvk.MvkError):
+            mvk.gated_activation(**{"gate": x, "up": x, **bad})
