@@ -57,6 +57,7 @@
 // on the device, so the bound is where no context loses.
 #include "kv.h"
 #include "mvk_internal.h"
+#include "quant.h"
 #include "units.h"
 
 namespace mvk {
@@ -521,10 +522,13 @@ __device__ __forceinline__ void put_row(const TileArgs& a, const SeqSpan& sp, ui
 
 constexpr uint32_t kCounterStride = 16;
 
-template <typename T, uint32_t kDim, bool kSplit>
+// C: how the cache holds its values (T itself, or in 8 bits).
+template <typename T, typename C, uint32_t kDim, bool kSplit>
 __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs a) {
     typedef Shape<T, kDim, kSplit> Sh;
     typedef typename Mma<T>::V8 V8;
+    typedef typename Held<C>::S S;
+    constexpr bool k8 = Held<C>::k8;
     constexpr uint32_t G = kDim / 8;  // granules a row
     __shared__ __attribute__((aligned(65536))) u32x4 lds[Sh::kLds];  // (at 0: see kTile)
     __shared__ float red[4][32][2];
@@ -567,8 +571,8 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
         const uint32_t rows = sp.c * a.grp, tile0 = st.tile * Sh::kRows, row0 = tile0 + (kSplit ? 0 : 32 * wave);
         const uint32_t known = min(row0 + col, rows - 1);
         // keys
-        const char* const kb = (const char*)((const T*)a.kv.K + (size_t)st.kh * a.kv.kh);
-        const char* const vb = (const char*)((const T*)a.kv.V + (size_t)st.kh * a.kv.vh);
+        const char* const kb = (const char*)((const S*)a.kv.K + (size_t)st.kh * a.kv.kh);
+        const char* const vb = (const char*)((const S*)a.kv.V + (size_t)st.kh * a.kv.vh);
         const uint32_t mask = (1u << a.kv.shift) - 1;
         const uint32_t key0 = (max(u0, Sh::kExtra) - Sh::kExtra) * Sh::kUnit, key1 = (max(u1, Sh::kExtra) - Sh::kExtra) * Sh::kUnit;
         const uint32_t first = key0 + (kSplit ? wave * Sh::kKeys : 0);
@@ -615,8 +619,61 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
         auto load_v = [&](uint32_t j0, uint32_t stage) {
             load(vb, a.kv.vp, a.kv.ve, true, j0, lds0 + 16 * ((kSplit ? wave : stage) * 2 * Sh::kGranules + Sh::kGranules + part0));
         };
+        // A cache held in 8 bits: this wave's granules of a tile go by way of registers, where
+        // they are widened.  An exponent a row; lane i has that of the wave's row i.
+        constexpr uint32_t kMine = 64 * Sh::kLoads / G;  // rows
+        struct Codes {
+            u32x2 c[k8 ? Sh::kLoads : 1];
+            int e;
+        };
+        auto fetch = [&](bool is_v, uint32_t j0, Codes& to) {
+            const char* base = is_v ? vb : kb;
+            const size_t page_stride = is_v ? a.kv.vp : a.kv.kp, entry_stride = is_v ? a.kv.ve : a.kv.ke;
+            const int8_t* ex = is_v ? a.kv.vx + (size_t)st.kh * a.kv.vxh : a.kv.kx + (size_t)st.kh * a.kv.kxh;
+            const size_t xp = is_v ? a.kv.vxp : a.kv.kxp, xe = is_v ? a.kv.vxe : a.kv.kxe;
+            const uint32_t row = part0 / G + lane % kMine;
+            if (a.whole_page) {
+                const uint32_t pg = (uint32_t)__builtin_amdgcn_readlane((int)ids, (int)((j0 >> a.kv.shift) - id0));
+                const char* b = base + (size_t)pg * page_stride + (size_t)(j0 & mask) * entry_stride;
+#pragma unroll
+                for (uint32_t i = 0; i < Sh::kLoads; ++i)
+                    to.c[k8 ? i : 0] = *(const u32x2*)(b + (lane_row * (uint32_t)entry_stride + 8 * granule(is_v, kStep * i + lane_row)) +
+                                              (size_t)(kStep * i * (uint32_t)entry_stride));
+                to.e = ex[(size_t)pg * xp + (size_t)(j0 & mask) * xe + row * (uint32_t)xe];
+            } else {
+                const uint32_t used = (sp.n - 1) >> a.kv.shift;
+#pragma unroll
+                for (uint32_t i = 0; i < Sh::kLoads; ++i) {
+                    const uint32_t r = kStep * i + lane_row, g = granule(is_v, r), j = j0 + r;
+                    const size_t pg = (uint32_t)__shfl((int)ids, (int)(min(j >> a.kv.shift, used) - id0));
+                    const char* from = base + pg * page_stride + (size_t)(j & mask) * entry_stride + 8 * g;
+                    to.c[k8 ? i : 0] = *(const u32x2*)(g < live ? from : (const char*)&kZeroGranule);
+                }
+                const uint32_t j = j0 + row;
+                const size_t pg = (uint32_t)__shfl((int)ids, (int)(min(j >> a.kv.shift, used) - id0));
+                to.e = ex[pg * xp + (size_t)(j & mask) * xe];
+            }
+            __builtin_amdgcn_sched_barrier(0);  // (all asked for here, not where they are used)
+        };
+        auto put = [&](bool is_v, const Codes& from, uint32_t stage) {
+            u32x4* const to = lds + (kSplit ? wave : stage) * 2 * Sh::kGranules + (is_v ? Sh::kGranules : 0) + part0 + lane;
+            const float two = power(from.e);
+#pragma unroll
+            for (uint32_t i = 0; i < Sh::kLoads; ++i) {
+                const float f = __shfl(two, (int)((kStep * i + lane / G) % kMine));
+                to[64 * i] = __builtin_bit_cast(u32x4, widen<C>(from.c[k8 ? i : 0], f));
+            }
+            asm volatile("" ::: "memory");
+        };
+        Codes ck, cv;
         // the first loads of keys, then the rows, which arrive behind them
-        if (first < stop) {
+        if (k8) {
+            if (first < stop) {
+                pages(first);
+                fetch(false, first, ck);
+                fetch(true, first, cv);
+            }
+        } else if (first < stop) {
             pages(first);
             load_k(first, 0);
             load_v(first, 0);
@@ -652,7 +709,27 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
         const bool idle = !kSplit && row0 >= rows;  // a wave without rows
 
         x.places(lane, lds0 + (kSplit ? wave * 32 * Sh::kGranules : 0), lds0 + (kSplit ? wave * 32 * Sh::kGranules : 0) + 16 * Sh::kGranules);
-        if (kSplit) {
+        if (kSplit && k8) {
+            // (a wave's writes and reads of LDS are in its own order)
+#pragma unroll 1
+            for (uint32_t j0 = first; j0 < stop; j0 += Sh::kUnit) {
+                const bool more = j0 + Sh::kUnit < stop, masked = j0 + Sh::kKeys > lim_lo;
+                put(false, ck, 0);
+                if (more) {
+                    pages(j0 + Sh::kUnit);
+                    fetch(false, j0 + Sh::kUnit, ck);
+                }
+                V8 k[kDim / 16];
+                x.read_k(k, 0);
+                f32x16 s = x.scores(k);
+                float most = x.largest(s);
+                x.rescale(s, most, j0, masked, a.sl2);
+                put(true, cv, 0);
+                if (more) fetch(true, j0 + Sh::kUnit, cv);
+                if (masked && __any(clean<T>(mine + Sh::kGranules, lane, 64, Sh::kGranules))) cleaned[turn] = 1;
+                x.template step<false, 0>(s, k, 0, a.sl2, most);
+            }
+        } else if (kSplit) {
 #pragma unroll 1
             for (uint32_t j0 = first; j0 < stop; j0 += Sh::kUnit) {
                 const bool more = j0 + Sh::kUnit < stop, masked = j0 + Sh::kKeys > lim_lo;
@@ -682,7 +759,17 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
             constexpr uint32_t kTile = 32 * Sh::kGranules, kBlock = 8 * Sh::kGranules;  // bytes
             static_assert((kTile & (kTile - 1)) == 0, "one bit tells the tiles apart");
             uint32_t stage = 0;
-            wait_loads<0>();
+            if (k8) {
+                put(false, ck, 0);
+                put(true, cv, 0);
+                if (first + Sh::kUnit < stop) {
+                    pages(first + Sh::kUnit);
+                    fetch(false, first + Sh::kUnit, ck);
+                    put(false, ck, 1);
+                }
+            } else {
+                wait_loads<0>();
+            }
             __syncthreads();
             f32x16 s0 = {}, s1 = {};
             V8 k[kDim / 16];
@@ -695,12 +782,21 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
             x.read_k(k, kBlock);
 #pragma unroll 1
             for (uint32_t j0 = first; j0 < stop; j0 += Sh::kUnit) {
-                wait_loads<0>();
+                if (!k8) wait_loads<0>();
                 __syncthreads();
-                if (j0 + Sh::kUnit < stop) load_v(j0 + Sh::kUnit, stage ^ 1);
-                if (j0 + 2 * Sh::kUnit < stop) {
-                    pages(j0 + 2 * Sh::kUnit);
-                    load_k(j0 + 2 * Sh::kUnit, stage);
+                const bool next_v = j0 + Sh::kUnit < stop, next_k = j0 + 2 * Sh::kUnit < stop;
+                if (k8) {
+                    if (next_v) fetch(true, j0 + Sh::kUnit, cv);
+                    if (next_k) {
+                        pages(j0 + 2 * Sh::kUnit);
+                        fetch(false, j0 + 2 * Sh::kUnit, ck);
+                    }
+                } else {
+                    if (next_v) load_v(j0 + Sh::kUnit, stage ^ 1);
+                    if (next_k) {
+                        pages(j0 + 2 * Sh::kUnit);
+                        load_k(j0 + 2 * Sh::kUnit, stage);
+                    }
                 }
                 if (j0 + Sh::kKeys > lim_0) {  // for all waves alike
                     if (clean<T>(mine + (2 * stage + 1) * Sh::kGranules, tid, 256, Sh::kGranules)) cleaned[turn] = 1;
@@ -723,6 +819,10 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
                     __builtin_amdgcn_s_setprio(0);
                 }
                 x.va ^= kTile;
+                if (k8) {  // (stage is the next tile's by now; the K that goes to this one's place has been read)
+                    if (next_v) put(true, cv, stage);
+                    if (next_k) put(false, ck, stage ^ 1);
+                }
             }
         }
 
@@ -735,15 +835,17 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
             const bool mine_first = !kSplit || wave == 0;  // (the waves of the tokens form are added)
 #pragma unroll 1
             for (uint32_t j = fix0; j < stop; ++j) {
-                const T* v = (const T*)vb + seq_page(a.sq, a.kv, st.s, j) * a.kv.vp + (j & mask) * a.kv.ve;
+                const size_t pg = seq_page(a.sq, a.kv, st.s, j);
+                const S* v = (const S*)vb + pg * a.kv.vp + (j & mask) * a.kv.ve;
+                const float two = k8 ? power(a.kv.vx[pg * a.kv.vxp + (size_t)st.kh * a.kv.vxh + (j & mask) * a.kv.vxe]) : 1.f;
 #pragma unroll
                 for (uint32_t i = 0; i < kDim / 8; ++i) {
-                    typedef T T4 __attribute__((ext_vector_type(4)));
+                    typedef S T4 __attribute__((ext_vector_type(4)));
                     if (i >= live || j >= x.lim || !mine_first) continue;
                     const T4 f = *(const T4*)(v + 8 * i + 4 * half);
 #pragma unroll
                     for (uint32_t k = 0; k < 4; ++k) {
-                        const float y = (float)f[k];
+                        const float y = Held<C>::get(f[k], two);
                         if (y - y != 0.f) x.o[i / 4][4 * (i % 4) + k] += y;
                     }
                 }
@@ -938,7 +1040,7 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
 // 128, 35 us (3.5 TB/s of K); a chunk of 256 over 6000, 46 us, 280 TFLOP/s: 392
 // workgroups, so some compute units have two and others one.
 constexpr uint32_t kWeightKeys = 128;
-template <typename T, uint32_t kDim>
+template <typename T, typename C, uint32_t kDim>
 __global__ __launch_bounds__(256) void weights_tile(TileArgs a, const float* __restrict__ lse, const float* w_in,
                                                     float* w_out, size_t w_seq, size_t w_head) {
     typedef typename Mma<T>::V8 V8;
@@ -958,7 +1060,8 @@ __global__ __launch_bounds__(256) void weights_tile(TileArgs a, const float* __r
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
     const u32x4* const zero = &kZeroGranule;
     {
-        const T* const kb = (const T*)a.kv.K + (size_t)kh * a.kv.kh;
+        typedef typename Held<C>::S S;
+        const S* const kb = (const S*)a.kv.K + (size_t)kh * a.kv.kh;
         size_t page[kLoadsK];  // (all looked up before the first load waits for its own)
 #pragma unroll
         for (uint32_t i = 0; i < kLoadsK; ++i) page[i] = seq_page(a.sq, a.kv, s, min(j0 + kStep * i + lane / G, sp.n - 1));
@@ -966,7 +1069,12 @@ __global__ __launch_bounds__(256) void weights_tile(TileArgs a, const float* __r
         for (uint32_t i = 0; i < kLoadsK; ++i) {
             const uint32_t r = kStep * i + lane / G, g = k_at<kDim>(r, lane % G) % G;
             const uint32_t at = min(j0 + r, sp.n - 1) & ((1u << a.kv.shift) - 1);
-            load_lds(g < live ? (const void*)(kb + page[i] * a.kv.kp + at * a.kv.ke + 8 * g) : zero, lds0 + 16 * (wave * kGranules + 64 * i));
+            const void* const from = g < live ? (const void*)(kb + page[i] * a.kv.kp + at * a.kv.ke + 8 * g) : zero;
+            if (Held<C>::k8)
+                lds[wave * kGranules + 64 * i + lane] = __builtin_bit_cast(
+                    u32x4, widen<C>(*(const u32x2*)from, power(a.kv.kx[page[i] * a.kv.kxp + (size_t)kh * a.kv.kxh + at * a.kv.kxe])));
+            else
+                load_lds(from, lds0 + 16 * (wave * kGranules + 64 * i));
         }
     }
     // rows of the first token that sees entry `first`, from a whole 32 on
@@ -1044,25 +1152,25 @@ __global__ __launch_bounds__(256) void weights_tile(TileArgs a, const float* __r
 
 constexpr uint32_t kGroups = 512;  // two workgroups a compute unit
 
-template <typename T, uint32_t kDim, bool kSplit>
+template <typename T, typename C, uint32_t kDim, bool kSplit>
 hipError_t launch_shape(TileArgs a, hipStream_t s) {
     a.whole_page = (1u << a.kv.shift) >= Shape<T, kDim, kSplit>::kKeys && a.kv.dim == kDim &&
-                   a.kv.ke < (1u << 20) && a.kv.ve < (1u << 20);
-    hipLaunchKernelGGL((attend_tile<T, kDim, kSplit>), dim3(kGroups), dim3(256), 0, s, a);
+                   a.kv.ke < (1u << 20) && a.kv.ve < (1u << 20) && a.kv.kxe < (1u << 20) && a.kv.vxe < (1u << 20);
+    hipLaunchKernelGGL((attend_tile<T, C, kDim, kSplit>), dim3(kGroups), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, typename C>
 hipError_t launch_type(const TileArgs& a, bool split, hipStream_t s) {
     const uint32_t d = a.kv.dim;
     if (split) {
-        if (d <= 64) return launch_shape<T, 64, true>(a, s);
-        if (d <= 128) return launch_shape<T, 128, true>(a, s);
-        return launch_shape<T, 256, true>(a, s);
+        if (d <= 64) return launch_shape<T, C, 64, true>(a, s);
+        if (d <= 128) return launch_shape<T, C, 128, true>(a, s);
+        return launch_shape<T, C, 256, true>(a, s);
     }
-    if (d <= 64) return launch_shape<T, 64, false>(a, s);
-    if (d <= 128) return launch_shape<T, 128, false>(a, s);
-    return launch_shape<T, 256, false>(a, s);
+    if (d <= 64) return launch_shape<T, C, 64, false>(a, s);
+    if (d <= 128) return launch_shape<T, C, 128, false>(a, s);
+    return launch_shape<T, C, 256, false>(a, s);
 }
 
 inline bool in16(const void* p, size_t a, size_t b, size_t c) { return (uintptr_t)p % 16 == 0 && (a | b | c) % 8 == 0; }
@@ -1070,9 +1178,10 @@ inline bool in16(const void* p, size_t a, size_t b, size_t c) { return (uintptr_
 }  // namespace
 
 bool attend_tile_fits(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq, bool split) {
-    if (kv.kx || (q.type != MVK_TYPE_BF16 && q.type != MVK_TYPE_F16) || kv.dim % 8 || kv.dim > 256 || tokens == 0) return false;
-    if (!in16(q.p, q.token, q.head, 0) || !in16(kv.K, kv.kp, kv.kh, kv.ke) || !in16(kv.V, kv.vp, kv.vh, kv.ve))
-        return false;
+    if ((q.type != MVK_TYPE_BF16 && q.type != MVK_TYPE_F16) || kv.dim % 8 || kv.dim > 256 || tokens == 0) return false;
+    // granules of eight values: 16 bytes, or 8 of a cache held in 8 bits
+    const uintptr_t part = ((uintptr_t)kv.K | (uintptr_t)kv.V) % (kv.kx ? 8 : 16);
+    if (!in16(q.p, q.token, q.head, 0) || part || (kv.kp | kv.kh | kv.ke | kv.vp | kv.vh | kv.ve) % 8) return false;
     const uint64_t cap = (uint64_t)sq.width << kv.shift;
     if ((cap + kWeightKeys - 1) / kWeightKeys * 256 >= (1ull << 32)) return false;  // threads of the weights' launch
     typedef Shape<__bf16, 128, true> Tokens;  // (rows and units are the same for every type and dim)
@@ -1118,9 +1227,16 @@ hipError_t launch_weights_tile(const Rows& q, uint32_t tokens, uint32_t heads, c
         return hipGetLastError();
     };
     const uint32_t d = kv.dim <= 64 ? 0 : kv.dim <= 128 ? 1 : 2;
-    if (q.type == MVK_TYPE_BF16)
-        return d == 0 ? go(weights_tile<__bf16, 64>) : d == 1 ? go(weights_tile<__bf16, 128>) : go(weights_tile<__bf16, 256>);
-    return d == 0 ? go(weights_tile<_Float16, 64>) : d == 1 ? go(weights_tile<_Float16, 128>) : go(weights_tile<_Float16, 256>);
+    switch (kv.type) {
+        case MVK_TYPE_BF16:
+            return d == 0 ? go(weights_tile<__bf16, __bf16, 64>) : d == 1 ? go(weights_tile<__bf16, __bf16, 128>) : go(weights_tile<__bf16, __bf16, 256>);
+        case MVK_TYPE_E4M3:
+            return d == 0 ? go(weights_tile<__bf16, E4M3, 64>) : d == 1 ? go(weights_tile<__bf16, E4M3, 128>) : go(weights_tile<__bf16, E4M3, 256>);
+        case MVK_TYPE_I8:
+            return d == 0 ? go(weights_tile<__bf16, I8, 64>) : d == 1 ? go(weights_tile<__bf16, I8, 128>) : go(weights_tile<__bf16, I8, 256>);
+        default:
+            return d == 0 ? go(weights_tile<_Float16, _Float16, 64>) : d == 1 ? go(weights_tile<_Float16, _Float16, 128>) : go(weights_tile<_Float16, _Float16, 256>);
+    }
 }
 
 hipError_t launch_attend_tile(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
@@ -1131,7 +1247,12 @@ hipError_t launch_attend_tile(const Rows& q, uint32_t tokens, uint32_t heads, co
     a.inv_scale = inv_scale, a.lse = lse, a.part = (float*)ws, a.counters = counters;
     const bool half = out.type == MVK_TYPE_BF16 || out.type == MVK_TYPE_F16;
     a.wide_out = (uintptr_t)out.p % (half ? 8 : 16) == 0 && (out.token | out.head) % 4 == 0;
-    return q.type == MVK_TYPE_BF16 ? launch_type<__bf16>(a, split, s) : launch_type<_Float16>(a, split, s);
+    switch (kv.type) {
+        case MVK_TYPE_BF16: return launch_type<__bf16, __bf16>(a, split, s);
+        case MVK_TYPE_E4M3: return launch_type<__bf16, E4M3>(a, split, s);
+        case MVK_TYPE_I8: return launch_type<__bf16, I8>(a, split, s);
+        default: return launch_type<_Float16, _Float16>(a, split, s);
+    }
 }
 
 }  // namespace mvk

@@ -55,6 +55,34 @@ __device__ __forceinline__ float power(int e) {
     return __uint_as_float(e == MVK_EXP_NAN ? 0x7fc00000u : (uint32_t)(e + 127) << 23);
 }
 
+// Eight consecutive values in bfloat16, exactly (of a value: codes of one byte, the first lowest).
+typedef uint32_t u32x2_ __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4q __attribute__((ext_vector_type(4)));
+template <typename C>
+__device__ __forceinline__ u32x4q widen(u32x2_ codes, float two) {
+    u32x4q y;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        if (__is_same(C, E4M3)) {
+            y[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[w], two, false));
+            y[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[w], two, true));
+        } else {
+            // from 128 on, as bytes convert in one instruction: (u - 128) two, without a rounding
+            typedef float F2 __attribute__((ext_vector_type(2)));
+            typedef __bf16 B2 __attribute__((ext_vector_type(2)));
+            const uint32_t u = codes[w] ^ 0x80808080u;
+            const float low = -128.f * two;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const F2 f = {__builtin_fmaf((float)(u >> (16 * h) & 0xffu), two, low),
+                              __builtin_fmaf((float)(u >> (16 * h + 8) & 0xffu), two, low)};
+                y[2 * w + h] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, B2));
+            }
+        }
+    }
+    return y;
+}
+
 // The first 32 bits of |x|, the last of them set where later ones are: orders as |x|
 // does against any value whose later bits are zero.  0 of infinities and not-a-numbers.
 __device__ __forceinline__ uint32_t top_bits(double x) {
