@@ -6,9 +6,8 @@
 // and every output written once; the sums of a norm go across its waves by way of
 // LDS.  Bound by memory for many rows, by the chain load, sums, store for few.
 // Values and sums are in 32 bits, in 64 with a FIELD output: its whole numbers are
-// chosen next to borders and reach 2^30, beyond what 32 bits hold.  A double rounded by
-// way of float to a 16-bit type does not occur (64 bits come with FIELD alone, but for
-// residual_out, whose h is a float first: an error of 2^-25 of a step more).
+// chosen next to borders and reach 2^30, beyond what 32 bits hold.  (There h in a 16-bit
+// residual_out is rounded by way of 32 bits: 2^-16 of a step more at most in bfloat16.)
 #include "mvk_internal.h"
 #include "rowio.h"
 
@@ -23,8 +22,8 @@ __device__ __forceinline__ A wave_add(A x) {
     return x;
 }
 
-// The sum over the workgroup, the same in every thread.  `turn`: which half of `part` (no
-// half is written again before every thread has read it: a barrier lies between).
+// The sum over the workgroup, the same in every thread.  `turn`: which half of `part`;
+// none is written again before every thread has read it (a barrier lies between).
 template <typename A>
 __device__ __forceinline__ A group_sum(A x, A (*part)[16], uint32_t& turn) {
     const uint32_t wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
@@ -39,104 +38,261 @@ __device__ __forceinline__ A group_sum(A x, A (*part)[16], uint32_t& turn) {
     return sum;
 }
 
-// kEach chunks of eight values a thread: chunk tid, tid + threads, ...
-template <typename A, int kEach>
-__global__ __launch_bounds__(1024) void block_norm(NormArgs a) {
+// Eight values as they lie in memory, of an element size known when it is compiled.  Which
+// of the two types of a size they have is a select: branches would end every load's flight.
+template <int kSize>
+struct Chunk;
+template <>
+struct Chunk<2> {
+    u32x4_ r;
+    __device__ __forceinline__ void load(const void* p, size_t i) { r = *(const u32x4_*)((const uint16_t*)p + i); }
+    template <typename A>
+    __device__ __forceinline__ typename Eight<A>::V values(int type, float) const {
+        typedef __bf16 B8 __attribute__((ext_vector_type(8)));
+        typedef _Float16 H8 __attribute__((ext_vector_type(8)));
+        const B8 b = __builtin_bit_cast(B8, r);
+        const H8 h = __builtin_bit_cast(H8, r);
+        typename Eight<A>::V v;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = (A)(type == MVK_TYPE_BF16 ? (float)b[k] : (float)h[k]);
+        return v;
+    }
+};
+template <>
+struct Chunk<4> {
+    u32x4_ lo, hi;
+    __device__ __forceinline__ void load(const void* p, size_t i) {
+        lo = ((const u32x4_*)((const uint32_t*)p + i))[0];
+        hi = ((const u32x4_*)((const uint32_t*)p + i))[1];
+    }
+    template <typename A>
+    __device__ __forceinline__ typename Eight<A>::V values(int type, float scale) const {
+        typename Eight<A>::V v;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t x = k < 4 ? lo[k & 3] : hi[k & 3];
+            const A f = (A)__uint_as_float(x), y = Eight<A>::lift(x, scale);
+            v[k] = type == MVK_TYPE_F32 ? f : y;
+        }
+        return v;
+    }
+};
+
+// Eight values of a norm's parameters or a gate.
+template <typename A>
+__device__ __forceinline__ typename Eight<A>::V load_params(const void* p, int type, size_t i) {
+    if (type == MVK_TYPE_F32) {
+        Chunk<4> c;
+        c.load(p, i);
+        return c.values<A>(MVK_TYPE_F32, 0.f);
+    }
+    Chunk<2> c;
+    c.load(p, i);
+    return c.values<A>(type, 0.f);
+}
+
+// A norm of v, rows of n = 1 / share values (zeros where a chunk is not `live`), by parameters as
+// `params` loads them.
+template <typename A, int kEach, typename Params>
+__device__ __forceinline__ void apply_norm(typename Eight<A>::V (&v)[kEach], const uint32_t (&count)[kEach], const NormView& w, A share,
+                                           A (*part)[16], uint32_t& turn, Params params) {
+    if (w.kind == MVK_NORM_LAYER) {
+        A sum = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k) sum += v[i][k];
+        const A mean = group_sum(sum, part, turn) * share;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k) v[i][k] = k < count[i] ? v[i][k] - mean : (A)0;
+    }
+    A sq = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) sq += v[i][k] * v[i][k];
+    const A r = (A)1 / sqrt(group_sum(sq, part, turn) * share + (A)w.eps);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) v[i] *= r;
+    if (w.weight) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) v[i] *= params(w.weight, i);
+    }
+    if (w.bias) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) v[i] += params(w.bias, i);
+    }
+}
+
+// Rows of whole aligned granules.  kEach chunks of eight values a thread: chunk tid, tid +
+// threads, ...; kX, kS: element sizes of x and of the residual.
+template <typename A, int kThreads, int kEach, int kX, int kS>
+__global__ __launch_bounds__(kThreads) void block_norm(NormArgs a) {
     typedef typename Eight<A>::V V;
     __shared__ A part[2][16];
     uint32_t turn = 0;
-    const uint32_t n = a.n, tid = threadIdx.x, threads = blockDim.x;
+    const uint32_t n = a.n;
+    uint32_t at[kEach], count[kEach];  // (a chunk beyond the row reads the first one, as zeros)
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const uint32_t p = 8 * (threadIdx.x + i * blockDim.x);
+        count[i] = p < n ? 8u : 0u;
+        at[i] = p < n ? p : 0u;
+    }
     const A share = (A)1 / (A)n;
-    auto count = [&](int i) {  // values of chunk i
-        const uint32_t at = 8 * (tid + i * threads);
-        return at < n ? min(8u, n - at) : 0u;
-    };
-    auto normed = [&](V (&v)[kEach], const NormView& w) {
-        if (w.kind == MVK_NORM_LAYER) {
-            A sum = 0;
-#pragma unroll
-            for (int i = 0; i < kEach; ++i)
-#pragma unroll
-                for (uint32_t k = 0; k < 8; ++k) sum += v[i][k];  // (zeros beyond the row)
-            const A mean = group_sum(sum, part, turn) * share;
-#pragma unroll
-            for (int i = 0; i < kEach; ++i)
-#pragma unroll
-                for (uint32_t k = 0; k < 8; ++k) v[i][k] = k < count(i) ? v[i][k] - mean : (A)0;
-        }
-        A sq = 0;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i)
-#pragma unroll
-            for (uint32_t k = 0; k < 8; ++k) sq += v[i][k] * v[i][k];
-        const A r = (A)1 / sqrt(group_sum(sq, part, turn) * share + (A)w.eps);
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const uint32_t c = count(i), at = 8 * (tid + i * threads);
-            if (!c) continue;
-            v[i] *= r;
-            if (w.weight) v[i] *= load8<A>(w.weight, w.type, w.wide, at, c, 0.f);
-            if (w.bias) v[i] += load8<A>(w.bias, w.type, w.wide, at, c, 0.f);
-        }
-    };
     for (uint32_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-        V v[kEach], h[kEach];
+        Chunk<kX> x[kEach];
+        Chunk<kS> res[kEach];
         if (a.x.p) {
 #pragma unroll
-            for (int i = 0; i < kEach; ++i)
-                v[i] = load8<A>(a.x.p, a.x.type, a.x.wide, t * a.x.stride + 8 * (tid + i * threads), count(i), a.x_scale);
+            for (int i = 0; i < kEach; ++i) x[i].load(a.x.p, t * a.x.stride + at[i]);
         }
         if (a.res.p) {
 #pragma unroll
-            for (int i = 0; i < kEach; ++i)
-                h[i] = load8<A>(a.res.p, a.res.type, a.res.wide, t * a.res.stride + 8 * (tid + i * threads), count(i), 0.f);
+            for (int i = 0; i < kEach; ++i) res[i].load(a.res.p, t * a.res.stride + at[i]);
         }
+        V v[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) v[i] = V{};
         if (a.x.p) {
-            if (a.after.on) normed(v, a.after);
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const uint32_t at = 8 * (tid + i * threads), c = count(i);
-                if (a.gate.p && c) v[i] *= load8<A>(a.gate.p, a.gate.type, a.gate.wide, t * a.gate.stride + at, c, 0.f);
-                v[i] *= (A)a.scale;
-                if (a.res.p) v[i] += h[i];
+            for (int i = 0; i < kEach; ++i) v[i] = x[i].template values<A>(a.x.type, a.x_scale) * (A)(count[i] ? 1 : 0);
+            if (a.after.on)
+                apply_norm<A, kEach>(v, count, a.after, share, part, turn,
+                                     [&](const void* p, int i) { return load_params<A>(p, a.after.type, at[i]); });
+            if (a.gate.p) {
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) v[i] *= load_params<A>(a.gate.p, a.gate.type, t * a.gate.stride + at[i]);
             }
-        } else {
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) v[i] = h[i];
+            for (int i = 0; i < kEach; ++i) v[i] *= (A)a.scale;
         }
+        if (a.res.p) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) v[i] += res[i].template values<A>(a.res.type, 0.f);
+        }
+        // (chunks beyond the row: not what the first one's residual and biases made of them)
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (!count[i]) v[i] = V{};
         if (a.res_out.p) {
 #pragma unroll
             for (int i = 0; i < kEach; ++i)
-                if (count(i))
-                    store8<A>(a.res_out.p, a.res_out.type, a.res_out.wide, t * a.res_out.stride + 8 * (tid + i * threads),
-                              count(i), v[i], (A)1);
+                if (count[i]) store8<A>(a.res_out.p, a.res_out.type, true, t * a.res_out.stride + at[i], 8, v[i], (A)1);
         }
         if (!a.out.p) continue;
-        if (a.before.on) normed(v, a.before);
+        if (a.before.on)
+            apply_norm<A, kEach>(v, count, a.before, share, part, turn,
+                                 [&](const void* p, int i) { return load_params<A>(p, a.before.type, at[i]); });
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
-            if (count(i))
-                store8<A>(a.out.p, a.out.type, a.out.wide, t * a.out.stride + 8 * (tid + i * threads), count(i), v[i],
-                          (A)1 / (A)a.out_scale);
+            if (count[i]) store8<A>(a.out.p, a.out.type, true, t * a.out.stride + at[i], 8, v[i], (A)1 / (A)a.out_scale);
     }
+}
+
+// Any width, strides and alignment: value by value.
+template <typename A, int kEach>
+__global__ __launch_bounds__(1024) void block_norm_any(NormArgs a) {
+    typedef typename Eight<A>::V V;
+    __shared__ A part[2][16];
+    uint32_t turn = 0;
+    const uint32_t n = a.n;
+    uint32_t at[kEach], count[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        at[i] = 8 * (threadIdx.x + i * blockDim.x);
+        count[i] = at[i] < n ? min(8u, n - at[i]) : 0u;
+    }
+    const A share = (A)1 / (A)n;
+    auto load = [&](const void* p, int type, size_t row, int i, float scale) {
+        V v;
+#pragma unroll 1
+        for (uint32_t k = 0; k < 8; ++k) {
+            const A x = k < count[i] ? load_one<A>(p, type, row + at[i] + k, scale) : (A)0;
+            // (no address of a register: the index is not known when this is compiled)
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) v[j] = j == k ? x : v[j];
+        }
+        return v;
+    };
+    for (uint32_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+        V v[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) v[i] = V{};
+        if (a.x.p) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) v[i] = load(a.x.p, a.x.type, t * a.x.stride, i, a.x_scale);
+            if (a.after.on)
+                apply_norm<A, kEach>(v, count, a.after, share, part, turn,
+                                     [&](const void* p, int i) { return load(p, a.after.type, 0, i, 0.f); });
+            if (a.gate.p) {
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) v[i] *= load(a.gate.p, a.gate.type, t * a.gate.stride, i, 0.f);
+            }
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) v[i] *= (A)a.scale;
+        }
+        if (a.res.p) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) v[i] += load(a.res.p, a.res.type, t * a.res.stride, i, 0.f);
+        }
+        auto store = [&](const Matrix& m, A inv_scale) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) store8<A>(m.p, m.type, false, t * m.stride + at[i], count[i], v[i], inv_scale);
+        };
+        if (a.res_out.p) store(a.res_out, (A)1);
+        if (!a.out.p) continue;
+        if (a.before.on)
+            apply_norm<A, kEach>(v, count, a.before, share, part, turn,
+                                 [&](const void* p, int i) { return load(p, a.before.type, 0, i, 0.f); });
+        store(a.out, (A)1 / (A)a.out_scale);
+    }
+}
+
+inline int size_of(const Matrix& m) { return m.type <= MVK_TYPE_F16 ? 2 : 4; }
+
+template <typename A, int kX, int kS>
+hipError_t launch_norm_of(const NormArgs& a, hipStream_t s) {
+    const uint32_t chunks = a.n / 8;
+    const dim3 grid(a.T < (1u << 20) ? a.T : 1u << 20);
+    auto go = [&](auto kernel, uint32_t most, uint32_t each) {
+        const uint32_t threads = ((chunks + each - 1) / each + 63) / 64 * 64;
+        hipLaunchKernelGGL(kernel, grid, dim3(threads < most ? threads : most), 0, s, a);
+        return hipGetLastError();
+    };
+    // Few rows: as many threads as the row can use.  Many: fewer with more values each, so that
+    // more rows share a compute unit and one's loads hide another's sums.
+    if (chunks <= 256) return go(block_norm<A, 256, 1, kX, kS>, 256, 1);
+    if (chunks <= 1024 && a.T <= 512) return go(block_norm<A, 1024, 1, kX, kS>, 1024, 1);
+    if (chunks <= 512) return go(block_norm<A, 256, 2, kX, kS>, 256, 2);
+    if (chunks <= 1024) return go(block_norm<A, 512, 2, kX, kS>, 512, 2);
+    return go(block_norm<A, 1024, 4, kX, kS>, 1024, 4);
+}
+
+template <typename A>
+hipError_t launch_norm_in(const NormArgs& a, bool wide, hipStream_t s) {
+    if (wide) {
+        const int kx = a.x.p ? size_of(a.x) : 4, ks = a.res.p ? size_of(a.res) : 4;
+        if (kx == 2) return ks == 2 ? launch_norm_of<A, 2, 2>(a, s) : launch_norm_of<A, 2, 4>(a, s);
+        return ks == 2 ? launch_norm_of<A, 4, 2>(a, s) : launch_norm_of<A, 4, 4>(a, s);
+    }
+    const uint32_t chunks = (a.n + 7) / 8, each = chunks <= 1024 ? 1 : 4;
+    const uint32_t threads = ((chunks + each - 1) / each + 63) / 64 * 64;
+    const dim3 grid(a.T < (1u << 20) ? a.T : 1u << 20), block(threads < 1024 ? threads : 1024);
+    if (each == 1) hipLaunchKernelGGL((block_norm_any<A, 1>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((block_norm_any<A, 4>), grid, block, 0, s, a);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_block_norm(const NormArgs& a, hipStream_t s) {
-    // four chunks a thread at most
-    const uint32_t chunks = (a.n + 7) / 8;
-    uint32_t threads = 64;
-    while (threads < 1024 && threads < chunks) threads *= 2;
-    const uint32_t each = (chunks + threads - 1) / threads;
-    const dim3 grid(a.T < (1u << 20) ? a.T : 1u << 20);
-    auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a);
-        return hipGetLastError();
-    };
-    if (a.out.p && a.out.type == MVK_TYPE_FIELD)
-        return each == 1 ? go(block_norm<double, 1>) : each == 2 ? go(block_norm<double, 2>) : go(block_norm<double, 4>);
-    return each == 1 ? go(block_norm<float, 1>) : each == 2 ? go(block_norm<float, 2>) : go(block_norm<float, 4>);
+    bool wide = a.n % 8 == 0 && (!a.after.on || a.after.wide) && (!a.before.on || a.before.wide);
+    for (const Matrix* m : {&a.x, &a.res, &a.gate, &a.res_out, &a.out}) wide &= !m->p || m->wide;
+    if (a.out.p && a.out.type == MVK_TYPE_FIELD) return launch_norm_in<double>(a, wide, s);
+    return launch_norm_in<float>(a, wide, s);
 }
 
 }  // namespace mvk
