@@ -90,6 +90,9 @@ __device__ __forceinline__ uint32_t top_bits(double x) {
     const uint32_t hi = (uint32_t)(b >> 32) & 0x7fffffffu;
     return hi >= 0x7ff00000u ? 0u : hi | ((uint32_t)b != 0 ? 1u : 0u);
 }
+// (of a float, as of the double it is)
+__device__ __forceinline__ uint32_t top_bits(float x) { return top_bits((double)x); }
+__device__ __forceinline__ bool is_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 __device__ __forceinline__ bool is_finite(double x) {
     return ((uint32_t)(__builtin_bit_cast(uint64_t, x) >> 32) & 0x7ff00000u) != 0x7ff00000u;
 }
@@ -105,13 +108,17 @@ __device__ __forceinline__ int row_exponent(uint32_t top) {
 // rounding x itself would (towards zero, the last bit set where something was lost).
 template <typename C>
 __device__ __forceinline__ float scaled(double x, int e) {
-    double y = x * __builtin_bit_cast(double, (uint64_t)(1023 - e) << 52);
-    y = fmin(fmax(y, -(double)Held<C>::kMost), (double)Held<C>::kMost);
+    const double y = x * __builtin_bit_cast(double, (uint64_t)(1023 - e) << 52);
     const float f = (float)y;
     const double d = (double)f;
     uint32_t b = __float_as_uint(f);
     if (d != y) b = (fabs(d) > fabs(y) ? b - 1 : b) | 1u;
-    return __uint_as_float(b);
+    return __builtin_amdgcn_fmed3f(__uint_as_float(b), -Held<C>::kMost, Held<C>::kMost);
+}
+// The same of a float, which is exact but where the code is zero anyway.
+template <typename C>
+__device__ __forceinline__ float scaled(float x, int e) {
+    return __builtin_amdgcn_fmed3f(x * __uint_as_float((uint32_t)(127 - e) << 23), -Held<C>::kMost, Held<C>::kMost);
 }
 
 // A field element or a float in 64 bits (a 31-bit residue times a power of two is exact).
