@@ -102,6 +102,7 @@ struct TileArgs {
     uint32_t* counters;  // one a workgroup, kCounterStride words apart: zero before and after
     bool whole_page;     // a tile of keys lies in one page, its offsets in 32 bits, and dim is kDim
     bool wide_out;  // out takes stores of 4 values at once
+    bool by_16;     // codes of a cache held in 8 bits come 16 at a time
 };
 
 // Sums that stop at kTooMany: sequences whose starts do not ascend share token rows
@@ -626,25 +627,31 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
             u32x2 c[k8 ? Sh::kLoads : 1];
             int e;
         };
+        // (the lane is unknown to the compiler in each: it would keep all their addresses in
+        // registers that the loops need)
         auto fetch = [&](bool is_v, uint32_t j0, Codes& to) {
+            uint32_t ln = lane;
+            asm volatile("" : "+v"(ln));
+            const uint32_t first_row = part0 / G + ln / G;
+            auto granule_of = [&](uint32_t r) { return (is_v ? v_at<kDim>(r, ln % G) : k_at<kDim>(r, ln % G)) % G; };
             const char* base = is_v ? vb : kb;
             const size_t page_stride = is_v ? a.kv.vp : a.kv.kp, entry_stride = is_v ? a.kv.ve : a.kv.ke;
             const int8_t* ex = is_v ? a.kv.vx + (size_t)st.kh * a.kv.vxh : a.kv.kx + (size_t)st.kh * a.kv.kxh;
             const size_t xp = is_v ? a.kv.vxp : a.kv.kxp, xe = is_v ? a.kv.vxe : a.kv.kxe;
-            const uint32_t row = part0 / G + lane % kMine;
+            const uint32_t row = part0 / G + ln % kMine;
             if (a.whole_page) {
                 const uint32_t pg = (uint32_t)__builtin_amdgcn_readlane((int)ids, (int)((j0 >> a.kv.shift) - id0));
                 const char* b = base + (size_t)pg * page_stride + (size_t)(j0 & mask) * entry_stride;
 #pragma unroll
                 for (uint32_t i = 0; i < Sh::kLoads; ++i)
-                    to.c[k8 ? i : 0] = *(const u32x2*)(b + (lane_row * (uint32_t)entry_stride + 8 * granule(is_v, kStep * i + lane_row)) +
+                    to.c[k8 ? i : 0] = *(const u32x2*)(b + (first_row * (uint32_t)entry_stride + 8 * granule_of(kStep * i + first_row)) +
                                               (size_t)(kStep * i * (uint32_t)entry_stride));
                 to.e = ex[(size_t)pg * xp + (size_t)(j0 & mask) * xe + row * (uint32_t)xe];
             } else {
                 const uint32_t used = (sp.n - 1) >> a.kv.shift;
 #pragma unroll
                 for (uint32_t i = 0; i < Sh::kLoads; ++i) {
-                    const uint32_t r = kStep * i + lane_row, g = granule(is_v, r), j = j0 + r;
+                    const uint32_t r = kStep * i + first_row, g = granule_of(r), j = j0 + r;
                     const size_t pg = (uint32_t)__shfl((int)ids, (int)(min(j >> a.kv.shift, used) - id0));
                     const char* from = base + pg * page_stride + (size_t)(j & mask) * entry_stride + 8 * g;
                     to.c[k8 ? i : 0] = *(const u32x2*)(g < live ? from : (const char*)&kZeroGranule);
@@ -656,22 +663,72 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
             __builtin_amdgcn_sched_barrier(0);  // (all asked for here, not where they are used)
         };
         auto put = [&](bool is_v, const Codes& from, uint32_t stage) {
-            u32x4* const to = lds + (kSplit ? wave : stage) * 2 * Sh::kGranules + (is_v ? Sh::kGranules : 0) + part0 + lane;
+            uint32_t ln = lane;
+            asm volatile("" : "+v"(ln));
+            u32x4* const to = lds + (kSplit ? wave : stage) * 2 * Sh::kGranules + (is_v ? Sh::kGranules : 0) + part0 + ln;
             const float two = power(from.e);
 #pragma unroll
             for (uint32_t i = 0; i < Sh::kLoads; ++i) {
-                const float f = __shfl(two, (int)((kStep * i + lane / G) % kMine));
+                const float f = __shfl(two, (int)((kStep * i + ln / G) % kMine));
                 to[64 * i] = __builtin_bit_cast(u32x4, widen<C>(from.c[k8 ? i : 0], f));
             }
             asm volatile("" ::: "memory");
         };
         Codes ck, cv;
+        // The chunks form has no registers for that while it computes: the codes go to LDS as they
+        // are, 16 a lane, into this wave's part of the place that they are widened in later.
+        constexpr uint32_t kRaw = k8 && !kSplit ? kDim / 64 : 1, kLanes = kDim / 16;  // loads a wave; lanes a row
+        struct Exps {
+            int e[kRaw];
+        };
+        auto place8 = [&](bool is_v, uint32_t stage) { return (stage * 2 + (is_v ? 1 : 0)) * Sh::kGranules + part0; };
+        auto fetch_raw = [&](bool is_v, uint32_t j0, uint32_t stage, Exps& to) {
+            uint32_t ln = lane;
+            asm volatile("" : "+v"(ln));
+            const uint32_t raw_row = part0 / G + ln / kLanes, raw_at = ln % kLanes * 16;
+            const char* base = is_v ? vb : kb;
+            const size_t page_stride = is_v ? a.kv.vp : a.kv.kp, entry_stride = is_v ? a.kv.ve : a.kv.ke;
+            const int8_t* ex = is_v ? a.kv.vx + (size_t)st.kh * a.kv.vxh : a.kv.kx + (size_t)st.kh * a.kv.kxh;
+            const size_t xp = is_v ? a.kv.vxp : a.kv.kxp, xe = is_v ? a.kv.vxe : a.kv.kxe;
+            const uint32_t used = (sp.n - 1) >> a.kv.shift;
+#pragma unroll
+            for (uint32_t i = 0; i < kRaw; ++i) {
+                const uint32_t r = raw_row + 64 / kLanes * i, j = j0 + r;
+                const size_t pg = (uint32_t)__shfl((int)ids, (int)(min(j >> a.kv.shift, used) - id0));
+                const char* from = base + pg * page_stride + (size_t)(j & mask) * entry_stride + raw_at;
+                load_lds(raw_at < dim ? from : (const char*)&kZeroGranule, lds0 + 16 * (place8(is_v, stage) + 64 * i));
+                to.e[i] = ex[pg * xp + (size_t)(j & mask) * xe];
+            }
+        };
+        // (its reads come before its writes, in this wave's order; no other wave uses the part)
+        auto widen_raw = [&](bool is_v, uint32_t stage, const Exps& from) {
+            uint32_t ln = lane;
+            asm volatile("" : "+v"(ln));
+            const uint32_t raw_row = part0 / G + ln / kLanes, raw_at = ln % kLanes * 16;
+            u32x4* const tile = lds + (stage * 2 + (is_v ? 1 : 0)) * Sh::kGranules;
+            u32x4 c[kRaw];
+#pragma unroll
+            for (uint32_t i = 0; i < kRaw; ++i) c[i] = lds[place8(is_v, stage) + 64 * i + ln];
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (uint32_t i = 0; i < kRaw; ++i) {
+                const uint32_t r = raw_row + 64 / kLanes * i;
+                const float two = power(from.e[i]);
+#pragma unroll
+                for (uint32_t h = 0; h < 2; ++h) {
+                    const uint32_t g = raw_at / 8 + h;
+                    tile[is_v ? v_at<kDim>(r, g) : k_at<kDim>(r, g)] =
+                        __builtin_bit_cast(u32x4, widen<C>(u32x2{c[i][2 * h], c[i][2 * h + 1]}, two));
+                }
+            }
+            asm volatile("" ::: "memory");
+        };
         // the first loads of keys, then the rows, which arrive behind them
         if (k8) {
             if (first < stop) {
                 pages(first);
                 fetch(false, first, ck);
-                fetch(true, first, cv);
+                if (kSplit) fetch(true, first, cv);
             }
         } else if (first < stop) {
             pages(first);
@@ -761,7 +818,8 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
             uint32_t stage = 0;
             if (k8) {
                 put(false, ck, 0);
-                put(true, cv, 0);
+                fetch(true, first, ck);
+                put(true, ck, 0);
                 if (first + Sh::kUnit < stop) {
                     pages(first + Sh::kUnit);
                     fetch(false, first + Sh::kUnit, ck);
@@ -785,11 +843,14 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
                 if (!k8) wait_loads<0>();
                 __syncthreads();
                 const bool next_v = j0 + Sh::kUnit < stop, next_k = j0 + 2 * Sh::kUnit < stop;
+                Exps ke, ve;
                 if (k8) {
-                    if (next_v) fetch(true, j0 + Sh::kUnit, cv);
-                    if (next_k) {
-                        pages(j0 + 2 * Sh::kUnit);
-                        fetch(false, j0 + 2 * Sh::kUnit, ck);
+                    if (a.by_16) {
+                        if (next_v) fetch_raw(true, j0 + Sh::kUnit, stage ^ 1, ve);
+                        if (next_k) {
+                            pages(j0 + 2 * Sh::kUnit);
+                            fetch_raw(false, j0 + 2 * Sh::kUnit, stage, ke);
+                        }
                     }
                 } else {
                     if (next_v) load_v(j0 + Sh::kUnit, stage ^ 1);
@@ -819,9 +880,20 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
                     __builtin_amdgcn_s_setprio(0);
                 }
                 x.va ^= kTile;
-                if (k8) {  // (stage is the next tile's by now; the K that goes to this one's place has been read)
-                    if (next_v) put(true, cv, stage);
-                    if (next_k) put(false, ck, stage ^ 1);
+                if (k8 && a.by_16) {  // (stage is the next tile's by now; the K that was in the other has been read)
+                    wait_loads<0>();
+                    if (next_v) widen_raw(true, stage, ve);
+                    if (next_k) widen_raw(false, stage ^ 1, ke);
+                } else if (k8) {
+                    if (next_v) {
+                        fetch(true, j0 + Sh::kUnit, ck);
+                        put(true, ck, stage);
+                    }
+                    if (next_k) {
+                        pages(j0 + 2 * Sh::kUnit);
+                        fetch(false, j0 + 2 * Sh::kUnit, ck);
+                        put(false, ck, stage ^ 1);
+                    }
                 }
             }
         }
@@ -1156,6 +1228,8 @@ template <typename T, typename C, uint32_t kDim, bool kSplit>
 hipError_t launch_shape(TileArgs a, hipStream_t s) {
     a.whole_page = (1u << a.kv.shift) >= Shape<T, kDim, kSplit>::kKeys && a.kv.dim == kDim &&
                    a.kv.ke < (1u << 20) && a.kv.ve < (1u << 20) && a.kv.kxe < (1u << 20) && a.kv.vxe < (1u << 20);
+    a.by_16 = a.kv.kx && a.kv.dim % 16 == 0 && ((uintptr_t)a.kv.K | (uintptr_t)a.kv.V) % 16 == 0 &&
+              (a.kv.kp | a.kv.kh | a.kv.ke | a.kv.vp | a.kv.vh | a.kv.ve) % 16 == 0;
     hipLaunchKernelGGL((attend_tile<T, C, kDim, kSplit>), dim3(kGroups), dim3(256), 0, s, a);
     return hipGetLastError();
 }
