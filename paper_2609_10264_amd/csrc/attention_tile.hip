@@ -723,12 +723,44 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
             }
             asm volatile("" ::: "memory");
         };
+        // The tokens form takes K from memory to the operands' registers: a lane has a key, half of
+        // its dims, 16 at a time (so product t has dims 32 (t / 2) + 16 half + 8 (t % 2) and on, of q too).
+        struct KeyCodes {
+            u32x4 c[k8 && kSplit ? kDim / 32 : 1];
+            int e;
+        };
+        auto fetch_key = [&](uint32_t j0, KeyCodes& to) {
+            uint32_t ln = lane;
+            asm volatile("" : "+v"(ln));
+            const uint32_t j = j0 + (ln & 31), at = 16 * (ln >> 5);
+            const size_t pg = (uint32_t)__shfl((int)ids, (int)((min(j, sp.n - 1) >> a.kv.shift) - id0));
+            const char* from = kb + pg * a.kv.kp + (size_t)(j & mask) * a.kv.ke + at;
+            if (a.by_16) {
+#pragma unroll
+                for (uint32_t i = 0; i < kDim / 32; ++i)
+                    to.c[k8 && kSplit ? i : 0] = *(const u32x4*)(32 * i + at < dim ? from + 32 * i : (const char*)&kZeroGranule);
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < kDim / 32; ++i) {
+                    const u32x2 x = *(const u32x2*)(32 * i + at < dim ? from + 32 * i : (const char*)&kZeroGranule);
+                    const u32x2 y = *(const u32x2*)(32 * i + at + 8 < dim ? from + 32 * i + 8 : (const char*)&kZeroGranule);
+                    to.c[k8 && kSplit ? i : 0] = u32x4{x[0], x[1], y[0], y[1]};
+                }
+            }
+            to.e = a.kv.kx[(size_t)st.kh * a.kv.kxh + pg * a.kv.kxp + (size_t)(j & mask) * a.kv.kxe];
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        KeyCodes kk;
         // the first loads of keys, then the rows, which arrive behind them
         if (k8) {
             if (first < stop) {
                 pages(first);
-                fetch(false, first, ck);
-                if (kSplit) fetch(true, first, cv);
+                if (kSplit) {
+                    fetch_key(first, kk);
+                    fetch(true, first, cv);
+                } else {
+                    fetch(false, first, ck);
+                }
             }
         } else if (first < stop) {
             pages(first);
@@ -749,7 +781,7 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
             u32x4 v[kDim / 16];  // (rows and granules that are not there: zeros, so that all loads are in flight at once)
 #pragma unroll
             for (uint32_t t = 0; t < kDim / 16; ++t) {
-                const uint32_t g = 2 * t + half;
+                const uint32_t g = k8 && kSplit ? 4 * (t / 2) + 2 * half + t % 2 : 2 * t + half;
                 v[t] = *(row0 + col < rows && g < live ? (const u32x4*)(qr + 8 * g) : &kZeroGranule);
             }
 #pragma unroll
@@ -771,13 +803,17 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
 #pragma unroll 1
             for (uint32_t j0 = first; j0 < stop; j0 += Sh::kUnit) {
                 const bool more = j0 + Sh::kUnit < stop, masked = j0 + Sh::kKeys > lim_lo;
-                put(false, ck, 0);
+                V8 k[kDim / 16];
+                const float two = power(kk.e);
+#pragma unroll
+                for (uint32_t t = 0; t < kDim / 16; ++t) {
+                    const u32x4 c = kk.c[k8 && kSplit ? t / 2 : 0];
+                    k[t] = __builtin_bit_cast(V8, widen<C>(u32x2{c[2 * (t % 2)], c[2 * (t % 2) + 1]}, two));
+                }
                 if (more) {
                     pages(j0 + Sh::kUnit);
-                    fetch(false, j0 + Sh::kUnit, ck);
+                    fetch_key(j0 + Sh::kUnit, kk);
                 }
-                V8 k[kDim / 16];
-                x.read_k(k, 0);
                 f32x16 s = x.scores(k);
                 float most = x.largest(s);
                 x.rescale(s, most, j0, masked, a.sl2);
