@@ -39,7 +39,7 @@ def library_path(p: int = P) -> str:
 def _stream(stream) -> int:
     # (the raw handle: building a Stream object takes longer than the call it is for)
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream
 
 

@@ -105,14 +105,18 @@ class KVCache:
             if self.k_exp is not None or self.v_exp is not None:
                 raise ValueError("k_exp and v_exp belong to a cache held in 8 bits")
             return _lib.MvkKv(K.data_ptr(), V.data_ptr(), kind, n, h, p, d, ka, kb, kc, va, vb, vc)
-        kx, vx = self.k_exp, self.v_exp
-        for x, name in ((kx, "k_exp"), (vx, "v_exp")):
-            if not isinstance(x, torch.Tensor) or x.dtype != torch.int8 or x.device != K.device:
-                raise TypeError(f"{name} must be an int8 tensor on K's device (the cache is held in 8 bits)")
-            if x.shape != shape[:3]:
-                raise ValueError(f"{name} has shape {tuple(x.shape)}, expected {tuple(shape[:3])}")
-        return _lib.MvkKv8(K.data_ptr(), V.data_ptr(), kind, n, h, p, d, ka, kb, kc, va, vb, vc, kx.data_ptr(),
-                           vx.data_ptr(), *kx.stride(), *vx.stride())
+        device, rows = K.get_device(), shape[:3]
+        return _lib.MvkKv8(K.data_ptr(), V.data_ptr(), kind, n, h, p, d, ka, kb, kc, va, vb, vc,
+                           _exps(self.k_exp, "k_exp", rows, device), _exps(self.v_exp, "v_exp", rows, device),
+                           *self.k_exp.stride(), *self.v_exp.stride())
+
+
+def _exps(x, name: str, shape, device: int):
+    if not isinstance(x, torch.Tensor) or x.dtype != torch.int8 or x.get_device() != device:
+        raise TypeError(f"{name} must be an int8 tensor on K's device (the cache is held in 8 bits)")
+    if x.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(x.shape)}, expected {tuple(shape)}")
+    return x.data_ptr()
 
 
 @dataclass
@@ -224,8 +228,9 @@ def cache_read(cache: KVCache, seqs: Sequences, tokens: int | None = None, dtype
     if tokens is not None and tokens != T:
         raise ValueError(f"the rows have {T} tokens, not {tokens}")
     ref = ctypes.byref
-    ks, vs = (ref(_rows(x, name, T, cs.kv_heads, cs.dim)) if x is not None else None
-              for x, name in ((k_out, "k_out"), (v_out, "v_out")))
+    hk, dim = cs.kv_heads, cs.dim
+    ks = ref(_rows(k_out, "k_out", T, hk, dim)) if k_out is not None else None
+    vs = ref(_rows(v_out, "v_out", T, hk, dim)) if v_out is not None else None
     _lib.check("mvk_cache_read", _lib.load(p).mvk_cache_read(ref(cs), ref(seqs.struct(T)), T, ks, vs, _stream(stream)))
     return k_out, v_out
 

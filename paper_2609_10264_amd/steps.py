@@ -25,7 +25,7 @@ from dataclasses import dataclass
 import torch
 
 from . import _lib
-from . import P, _stream
+from . import P
 from .attention import _TYPES, FIELD
 
 _KINDS = {"rms": _lib.MVK_NORM_RMS, "layer": _lib.MVK_NORM_LAYER}
@@ -39,23 +39,32 @@ def _on(t, name: str, device: int):
     """The type of a tensor on the current device."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
-    if t.device.index != device:
-        raise ValueError(f"{name} is on device {t.device.index}, the current device is {device}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on device {t.get_device()}, the current device is {device}")
     kind = _TYPES.get(t.dtype)
     if kind is None:
         raise TypeError(f"{name} must be bfloat16, float16, float32 or int32 (field), got {t.dtype}")
     return kind
 
 
-def _matrix(t, name: str, T: int, n: int, device: int):
-    """T x n, any stride between rows, contiguous rows."""
-    kind = _on(t, name, device)
-    if t.dim() != 2 or t.shape[0] != T or t.shape[1] != n:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(T, n)}")
-    a, b = t.stride()
-    if b != 1 and n > 1:
-        raise ValueError(f"{name}: the last axis must be contiguous")
-    return _lib.MvkRows(t.data_ptr(), kind, a, n)
+def _matrix(t, name: str, shape, device: int):
+    """T x n, any stride between rows, contiguous rows.  (These checks cost as much as a launch if
+    written with loops: the messages are found where one has failed.)"""
+    if isinstance(t, torch.Tensor) and t.get_device() == device and t.shape == shape:
+        kind = _TYPES.get(t.dtype)
+        a, b = t.stride()
+        if kind is not None and (b == 1 or shape[1] <= 1):
+            return _lib.MvkRows(t.data_ptr(), kind, a, shape[1])
+    _on(t, name, device)
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    raise ValueError(f"{name}: the last axis must be contiguous")
+
+
+def _where(stream):
+    """(current device, raw stream)"""
+    device = torch._C._cuda_getDevice()
+    return device, torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 def _scale_of(kind: int, scale, name: str) -> float:
@@ -80,17 +89,22 @@ class Norm:
     def struct(self, n: int, device: int):
         if self.kind not in _KINDS:
             raise ValueError(f"kind must be one of {sorted(_KINDS)}")
-        kind, at = _lib.MVK_TYPE_F32, [None, None]
-        for i, (t, name) in enumerate(((self.weight, "weight"), (self.bias, "bias"))):
-            if t is None:
-                continue
-            kind = _on(t, name, device)
-            if t.shape != (n,) or not t.is_contiguous():
-                raise ValueError(f"{name} must be {n} contiguous values, got {tuple(t.shape)}")
-            at[i] = t.data_ptr()
-        if None not in at and self.weight.dtype != self.bias.dtype:
-            raise TypeError("weight and bias must have one type")
-        return _lib.MvkNorm(at[0], at[1], kind, _KINDS[self.kind], self.eps)
+        w, b = self.weight, self.bias
+        kind, w_at, b_at = _lib.MVK_TYPE_F32, None, None
+        if w is not None:
+            kind, w_at = self._vector(w, "weight", n, device)
+        if b is not None:
+            kind, b_at = self._vector(b, "bias", n, device)
+            if w is not None and w.dtype != b.dtype:
+                raise TypeError("weight and bias must have one type")
+        return _lib.MvkNorm(w_at, b_at, kind, _KINDS[self.kind], self.eps)
+
+    @staticmethod
+    def _vector(t, name: str, n: int, device: int):
+        kind = _on(t, name, device)
+        if t.shape != (n,) or not t.is_contiguous():
+            raise ValueError(f"{name} must be {n} contiguous values, got {tuple(t.shape)}")
+        return kind, t.data_ptr()
 
 
 def block_norm(x: torch.Tensor | None, residual: torch.Tensor | None = None, before: Norm | None = None,
@@ -104,23 +118,24 @@ def block_norm(x: torch.Tensor | None, residual: torch.Tensor | None = None, bef
     residual's type, float32 without one), before(h) in out (may be x) or of
     out_dtype (residual's by default), FIELD: over out_scale, rounded into the field.
     Without `before`, out and out_dtype only h is computed."""
-    device = torch.cuda.current_device()
+    device, raw = _where(stream)
     like = x if x is not None else residual
     if like is None:
         raise ValueError("one of x and residual is needed")
-    if like.dim() != 2:
-        raise ValueError(f"rows are T x n, got {tuple(like.shape)}")
-    T, n = like.shape
+    shape = like.shape
+    if len(shape) != 2:
+        raise ValueError(f"rows are T x n, got {tuple(shape)}")
+    T, n = shape
     ref = ctypes.byref
-    xs = _matrix(x, "x", T, n, device) if x is not None else None
-    rs = _matrix(residual, "residual", T, n, device) if residual is not None else None
+    xs = _matrix(x, "x", shape, device) if x is not None else None
+    rs = _matrix(residual, "residual", shape, device) if residual is not None else None
     stream_type = residual.dtype if residual is not None else torch.float32
     if residual_out is None:
-        residual_out = torch.empty((T, n), dtype=stream_type, device=like.device)
+        residual_out = torch.empty(shape, dtype=stream_type, device=like.device)
     if out is None and (before is not None or out_dtype is not None):
-        out = torch.empty((T, n), dtype=out_dtype or stream_type, device=like.device)
-    ho = _matrix(residual_out, "residual_out", T, n, device)
-    os_ = _matrix(out, "out", T, n, device) if out is not None else None
+        out = torch.empty(shape, dtype=out_dtype or stream_type, device=like.device)
+    ho = _matrix(residual_out, "residual_out", shape, device)
+    os_ = _matrix(out, "out", shape, device) if out is not None else None
     gs = None
     if gate is not None:
         kind = _on(gate, "gate", device)
@@ -129,13 +144,13 @@ def block_norm(x: torch.Tensor | None, residual: torch.Tensor | None = None, bef
                 raise ValueError(f"gate must be {n} contiguous values or {(T, n)}, got {tuple(gate.shape)}")
             gs = _lib.MvkRows(gate.data_ptr(), kind, 0, n)
         else:
-            gs = _matrix(gate, "gate", T, n, device)
-    norms = [ref(w.struct(n, device)) if w is not None else None for w in (after, before)]
+            gs = _matrix(gate, "gate", shape, device)
     _lib.check("mvk_block_norm", _lib.load(p).mvk_block_norm(
         ref(xs) if xs is not None else None, _scale_of(xs.type, field_scale, "field_scale") if xs is not None else 0.0,
-        ref(rs) if rs is not None else None, T, n, norms[0], ref(gs) if gs is not None else None, scale, ref(ho),
-        norms[1], ref(os_) if os_ is not None else None,
-        _scale_of(os_.type, out_scale, "out_scale") if os_ is not None else 0.0, _stream(stream)))
+        ref(rs) if rs is not None else None, T, n, ref(after.struct(n, device)) if after is not None else None,
+        ref(gs) if gs is not None else None, scale, ref(ho), ref(before.struct(n, device)) if before is not None else None,
+        ref(os_) if os_ is not None else None,
+        _scale_of(os_.type, out_scale, "out_scale") if os_ is not None else 0.0, raw))
     return out, residual_out
 
 
@@ -148,31 +163,32 @@ def gated_activation(gate: torch.Tensor, up: torch.Tensor, act: str = "silu", fi
     rounded into the field."""
     if act not in _ACTS:
         raise ValueError(f"act must be one of {sorted(_ACTS)}")
-    device = torch.cuda.current_device()
+    device, raw = _where(stream)
     if not isinstance(gate, torch.Tensor) or gate.dim() != 2:
         raise ValueError("gate must be a tensor, T x n")
-    T, n = gate.shape
-    gs, us = _matrix(gate, "gate", T, n, device), _matrix(up, "up", T, n, device)
+    shape = gate.shape
+    T, n = shape
+    gs, us = _matrix(gate, "gate", shape, device), _matrix(up, "up", shape, device)
     if out is None:
         out_dtype = out_dtype or (torch.float32 if gate.dtype == FIELD else gate.dtype)
-        out = torch.empty((T, n), dtype=out_dtype, device=gate.device)
-    os_ = _matrix(out, "out", T, n, device)
+        out = torch.empty(shape, dtype=out_dtype, device=gate.device)
+    os_ = _matrix(out, "out", shape, device)
     ref = ctypes.byref
     _lib.check("mvk_gated_activation", _lib.load(p).mvk_gated_activation(
         ref(gs), ref(us), T, n, _ACTS[act], _scale_of(gs.type, field_scale, "field_scale"), ref(os_),
-        _scale_of(os_.type, out_scale, "out_scale"), _stream(stream)))
+        _scale_of(os_.type, out_scale, "out_scale"), raw))
     return out
+
+
+def _vector(t, name: str, dtype, R: int, device: int):
+    if isinstance(t, torch.Tensor) and t.get_device() == device and t.dtype == dtype and t.shape == (R,) and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be {R} contiguous values of {dtype} on the current device")
 
 
 def _each(v, name: str, dtype, R: int, device: int):
     """(value for all rows, pointer to one a row)"""
-    if not isinstance(v, torch.Tensor):
-        return v, None
-    if not v.is_cuda or v.dtype != dtype or v.shape != (R,) or not v.is_contiguous():
-        raise ValueError(f"{name} must be a number or {R} contiguous CUDA values of {dtype}")
-    if v.device.index != device:
-        raise ValueError(f"{name} is on device {v.device.index}, the current device is {device}")
-    return 0, v.data_ptr()
+    return (0, _vector(v, name, dtype, R, device)) if isinstance(v, torch.Tensor) else (v, None)
 
 
 def sample(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
@@ -186,28 +202,21 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_
     of these the ones with at least min_p of the largest's; among the kept ones the
     token is drawn.  probs (R float32, written): its probability among them.  A row
     without a logit above -inf gives -1."""
-    device = torch.cuda.current_device()
+    device, raw = _where(stream)
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
         raise ValueError("logits must be a tensor, R x n")
     R, n = logits.shape
-    rows = _matrix(logits, "logits", R, n, device)
+    rows = _matrix(logits, "logits", logits.shape, device)
     if out is None:
         out = torch.empty((R,), dtype=torch.int32, device=logits.device)
-    at = []
-    for t, name, dtype in ((u, "u", torch.float32), (out, "out", torch.int32), (probs, "probs", torch.float32)):
-        if t is None and name == "probs":
-            at.append(None)
-            continue
-        _on(t, name, device)
-        if t.dtype != dtype or t.shape != (R,) or not t.is_contiguous():
-            raise ValueError(f"{name} must be {R} contiguous values of {dtype}")
-        at.append(t.data_ptr())
     f32 = torch.float32
+    at = (_vector(u, "u", f32, R, device), _vector(out, "out", torch.int32, R, device),
+          _vector(probs, "probs", f32, R, device) if probs is not None else None)
     (t, ts), (k, ks), (pp, ps), (m, ms) = (_each(temperature, "temperature", f32, R, device),
                                            _each(top_k, "top_k", torch.int32, R, device),
                                            _each(top_p, "top_p", f32, R, device), _each(min_p, "min_p", f32, R, device))
     how = _lib.MvkSampling(t, pp, m, max(min(k, 2**31 - 1), 0), ts, ps, ms, ks)
     _lib.check("mvk_sample_tokens", _lib.load(p).mvk_sample_tokens(
         ctypes.byref(rows), R, n, _scale_of(rows.type, field_scale, "field_scale"), ctypes.byref(how), *at,
-        _stream(stream)))
+        raw))
     return out
