@@ -15,9 +15,10 @@
 // A workgroup takes a row.  What is near the top goes, in order, to a list in LDS, on
 // which thresholds and the draw are found without the row: with top-k, the kth largest of
 // 4096 maxima, four a thread, is a bound that k logits at least reach (and not many more);
-// with top-p alone, a histogram of the weights by the first digit of the key says where
-// to cut.  The row then is read twice or three times, but once from memory.  Where the
-// list would not hold them, the digits of the row's keys are searched to the last.
+// with min-p alone, its border; with top-p alone, a histogram of the weights by the first
+// digit of the key says where to cut.  The row then is read twice or three times, but once
+// from memory.  Where the list would not hold them, the digits of the row's keys are
+// searched to the last.
 #include "mvk_internal.h"
 #include "rowio.h"
 
@@ -25,27 +26,48 @@ namespace mvk {
 
 namespace {
 
-// A logit's key: orders as the logit does; 0 for not-a-numbers and -inf, which have
-// no weight.  (Zeros of either sign are one value.)
+// A logit as a number that compares (least: of no weight, as -inf; a not-a-number compares as
+// less than any), its key, which orders as the logit does (0 for -inf and not-a-numbers;
+// zeros of either sign are one value), and what a key stands for.
 template <typename S>
 struct Logit {
     typedef S T;
-    static __device__ __forceinline__ uint32_t key(T x) {
-        const float f = to_float(x) + 0.f;
+    typedef float N;
+    static __device__ __forceinline__ N least() { return -INFINITY; }
+    static __device__ __forceinline__ N number(T x) { return to_float(x); }
+    static __device__ __forceinline__ N larger(N a, N b) { return fmaxf(a, b); }
+    static __device__ __forceinline__ uint32_t key(N x) {
+        const float f = x + 0.f;
         const uint32_t b = __float_as_uint(f);
         if (f != f || b == 0xff800000u) return 0u;
         return b & 0x80000000u ? ~b : b | 0x80000000u;
     }
-    static __device__ __forceinline__ double value(uint32_t k, float) {
-        return (double)__uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
+    // The number of a key, the least finite one at least.
+    static __device__ __forceinline__ N number_of(uint32_t k) {
+        return __uint_as_float(k < 0x00800000u ? 0xff7fffffu : k & 0x80000000u ? k & 0x7fffffffu : ~k);
+    }
+    static __device__ __forceinline__ float coarse(uint32_t k) { return number_of(k); }
+    static __device__ __forceinline__ double value(uint32_t k, float) { return (double)number_of(k); }
+    // The key of a number next to v, below it.
+    static __device__ __forceinline__ uint32_t key_below(double v, float) {
+        const float f = (float)(v - fabs(v) * 0x1p-20 - 0x1p-100);
+        return max(key(fmaxf(f, -3.4028234e38f)), 1u);
     }
 };
 template <>
 struct Logit<Field> {
     typedef uint32_t T;
-    static __device__ __forceinline__ uint32_t key(T x) { return (x > kP / 2 ? x - kP : x) + 0x80000000u; }
-    static __device__ __forceinline__ double value(uint32_t k, float scale) {
-        return (double)(int32_t)(k - 0x80000000u) * (double)scale;
+    typedef int32_t N;
+    static __device__ __forceinline__ N least() { return (int32_t)0x80000000; }
+    static __device__ __forceinline__ N number(T x) { return (int32_t)(x > kP / 2 ? x - kP : x); }
+    static __device__ __forceinline__ N larger(N a, N b) { return max(a, b); }
+    static __device__ __forceinline__ uint32_t key(N x) { return (uint32_t)x + 0x80000000u; }
+    static __device__ __forceinline__ N number_of(uint32_t k) { return (int32_t)(k - 0x80000000u); }
+    static __device__ __forceinline__ float coarse(uint32_t k) { return (float)number_of(k); }
+    static __device__ __forceinline__ double value(uint32_t k, float scale) { return (double)number_of(k) * (double)scale; }
+    static __device__ __forceinline__ uint32_t key_below(double v, float scale) {
+        const double f = floor(v / (double)scale) - 1.;
+        return f < -2147483647. ? 1u : key((int32_t)f);
     }
 };
 
@@ -135,12 +157,12 @@ struct RowOf {
     static __device__ __forceinline__ uint32_t at(uint32_t step, uint32_t q) {
         return ((step * kAhead + q) * kThreads + threadIdx.x) * kVec;
     }
-    // Keys of a step (0 beyond the row), its loads in flight together.
-    __device__ __forceinline__ void keys(uint32_t step, uint32_t (&k)[kAhead][kVec]) const {
+    // Numbers of a step (the least beyond the row), its loads in flight together.
+    typedef typename Logit<S>::N N;
+    __device__ __forceinline__ void numbers(uint32_t step, N (&k)[kAhead][kVec]) const {
         typedef T V __attribute__((ext_vector_type(kVec)));
         V v[kAhead];
         if (wide) {
-            // (granules that the row does not fill: those of its beginning, or nothing)
             const uint32_t whole = n / kVec * kVec;
 #pragma unroll
             for (uint32_t q = 0; q < kAhead; ++q) {
@@ -156,13 +178,26 @@ struct RowOf {
 #pragma unroll
                 for (uint32_t e = 0; e < kVec; ++e) v[q][e] = x[min(at(step, q) + e, n - 1)];
         }
+        const bool inside = ((step + 1) * kAhead * kThreads) * kVec <= n;  // (the whole workgroup's)
 #pragma unroll
         for (uint32_t q = 0; q < kAhead; ++q)
 #pragma unroll
-            for (uint32_t e = 0; e < kVec; ++e) k[q][e] = at(step, q) + e < n ? Logit<S>::key(v[q][e]) : 0u;
+            for (uint32_t e = 0; e < kVec; ++e) {
+                k[q][e] = Logit<S>::number(v[q][e]);
+                if (!inside && at(step, q) + e >= n) k[q][e] = Logit<S>::least();
+            }
+    }
+    __device__ __forceinline__ void keys(uint32_t step, uint32_t (&k)[kAhead][kVec]) const {
+        N v[kAhead][kVec];
+        numbers(step, v);
+#pragma unroll
+        for (uint32_t q = 0; q < kAhead; ++q)
+#pragma unroll
+            for (uint32_t e = 0; e < kVec; ++e) k[q][e] = v[q][e] == Logit<S>::least() ? 0u : Logit<S>::key(v[q][e]);
     }
 };
 
+constexpr uint32_t kMembers = 64;  // of one bin of the list
 struct Shared {
     double table[kTable];
     uint64_t mass[kBins];
@@ -170,8 +205,10 @@ struct Shared {
     uint32_t key[kList], index[kList];
     uint64_t wave_mass[kWaves];
     uint32_t wave_num[kWaves], counts[2][64];
-    uint64_t found_above;
-    uint32_t found_bin, found_num, found_key;
+    uint64_t found_above, found_mass;
+    uint32_t found_bin, found_num, found_key, low;
+    uint64_t member_mass[kMembers];
+    uint32_t member_key[kMembers], members;
 };
 
 // Sums over the workgroup up to and with this thread, and the whole.
@@ -228,6 +265,22 @@ __device__ __forceinline__ Found find_bin(Shared& sh, bool by_mass, uint64_t nee
     return Found{above + s.all_mass >= need, sh.found_bin, sh.found_num, sh.found_above};
 }
 
+// The bin of a value, the largest in the first.  (Of not-a-numbers, which infinities make: the first.)
+__device__ __forceinline__ uint32_t bin_of(float high, float per, float x) {
+    const float b = (high - x) * per;
+    return b > 0.f ? (uint32_t)fminf(b, (float)(kBins - 1)) : 0u;
+}
+__device__ __forceinline__ uint32_t group_least(Shared& sh, uint32_t x) {
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) x = min(x, (uint32_t)__shfl_xor((int)x, d));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh.wave_num[threadIdx.x >> 6] = x;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t w = 0; w < kWaves; ++w) x = min(x, sh.wave_num[w]);
+    return x;
+}
+
 __device__ __forceinline__ void clear_bins(Shared& sh) {
     __syncthreads();
     for (uint32_t b = threadIdx.x; b < kBins; b += kThreads) sh.num[b] = 0, sh.mass[b] = 0;
@@ -263,18 +316,28 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
         const Settings s = settings_of(a, r);
         const uint32_t steps = row.steps();
 
-        // The largest key, and those of this thread.
-        uint32_t mine[kAhead] = {};
+        // The largest key, and this thread's own maxima.
+        typedef typename Logit<S>::N N;
+        uint32_t mine[kAhead], top = 0;
+        {
+            N best[kAhead];
+#pragma unroll
+            for (uint32_t q = 0; q < kAhead; ++q) best[q] = Logit<S>::least();
 #pragma unroll 1
-        for (uint32_t st = 0; st < steps; ++st) {
-            uint32_t k[kAhead][kVec];
-            row.keys(st, k);
+            for (uint32_t st = 0; st < steps; ++st) {
+                N k[kAhead][kVec];
+                row.numbers(st, k);
 #pragma unroll
-            for (uint32_t q = 0; q < kAhead; ++q)
+                for (uint32_t q = 0; q < kAhead; ++q)
 #pragma unroll
-                for (uint32_t e = 0; e < kVec; ++e) mine[q] = max(mine[q], k[q][e]);
+                    for (uint32_t e = 0; e < kVec; ++e) best[q] = Logit<S>::larger(best[q], k[q][e]);
+            }
+#pragma unroll
+            for (uint32_t q = 0; q < kAhead; ++q) {
+                mine[q] = best[q] == Logit<S>::least() ? 0u : Logit<S>::key(best[q]);
+                top = max(top, mine[q]);
+            }
         }
-        uint32_t top = max(max(mine[0], mine[1]), max(mine[2], mine[3]));
 #pragma unroll
         for (int d = 32; d >= 1; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
         __syncthreads();  // (the row before is done with everything shared)
@@ -304,15 +367,17 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
         // The list, in order; false if it does not hold them.
         auto collect = [&]() {
             uint32_t base = 0;
+            const N least_number = Logit<S>::number_of(from);
 #pragma unroll 1
             for (uint32_t st = 0; st < steps; ++st) {
-                uint32_t k[kAhead][kVec], c[kAhead], in[kAhead] = {}, any = 0;
-                row.keys(st, k);
+                N k[kAhead][kVec];
+                uint32_t c[kAhead], in[kAhead] = {}, any = 0;
+                row.numbers(st, k);
 #pragma unroll
                 for (uint32_t q = 0; q < kAhead; ++q) {
                     c[q] = 0;
 #pragma unroll
-                    for (uint32_t e = 0; e < kVec; ++e) c[q] += k[q][e] >= from ? 1u : 0u;
+                    for (uint32_t e = 0; e < kVec; ++e) c[q] += k[q][e] >= least_number ? 1u : 0u;
                     any |= c[q];
                 }
                 if (__ballot(any != 0)) {
@@ -331,8 +396,8 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
                     if (!c[q]) continue;
 #pragma unroll
                     for (uint32_t e = 0; e < kVec; ++e)
-                        if (k[q][e] >= from) {
-                            if (to < kList) sh.key[to] = k[q][e], sh.index[to] = Row::at(st, q) + e;
+                        if (k[q][e] >= least_number) {
+                            if (to < kList) sh.key[to] = Logit<S>::key(k[q][e]), sh.index[to] = Row::at(st, q) + e;
                             ++to;
                         }
                 }
@@ -394,25 +459,32 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
             }
         };
 
-        bool list_k = false, list_p = false;  // which settings are left to the list
+        bool list_k = false, list_p = false, list_m = false;  // which settings are left to the list
         if (s.k) {
             if (s.k <= kMaxima) {
-                // the kth largest of the maxima, or a little less
-                uint32_t lo = 1, hi = top;
-                uint64_t above = 0;
-                for (;;) {
-                    const uint32_t width = width_of(lo, hi);
-                    clear_bins(sh);
+                // The kth largest of the maxima, or a little less: bins by value, of which any
+                // order would do, and the least maximum in those that hold k.
+                uint32_t low = 0xffffffffu;
+#pragma unroll
+                for (uint32_t q = 0; q < kAhead; ++q)
+                    if (mine[q]) low = min(low, mine[q]);
+                low = group_least(sh, low);
+                const float high_f = Logit<S>::coarse(top), per = (float)(kBins - 1) / (high_f - Logit<S>::coarse(low));
+                clear_bins(sh);
+                uint32_t b[kAhead];
+#pragma unroll
+                for (uint32_t q = 0; q < kAhead; ++q) {
+                    b[q] = bin_of(high_f, per, Logit<S>::coarse(mine[q]));
+                    if (mine[q]) atomicAdd(&sh.num[b[q]], 1u);
+                }
+                const Found f = find_bin(sh, false, s.k, 0);
+                if (f.any) {
+                    low = 0xffffffffu;
 #pragma unroll
                     for (uint32_t q = 0; q < kAhead; ++q)
-                        if (mine[q] >= lo && mine[q] <= hi) atomicAdd(&sh.num[(hi - mine[q]) >> width], 1u);
-                    const Found f = find_bin(sh, false, s.k, above);
-                    if (!f.any) break;  // (there are fewer: all of the range)
-                    enter_bin(lo, hi, f.bin, width);
-                    if (width == 0 || f.above + f.num <= s.k + s.k / 4 + 8) break;
-                    above = f.above;
+                        if (mine[q] && b[q] <= f.bin) low = min(low, mine[q]);
+                    from = group_least(sh, low);
                 }
-                from = lo;
                 list_k = collect();
             }
             if (!list_k) {
@@ -438,6 +510,10 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
             list_p |= list_k && s.p < 1.;
         } else if (s.p < 1.) {
             if (!search_row(true, 0, true)) list_p = collect();
+        } else if (least) {
+            // (weights next to the border are looked at again)
+            from = min(top, Logit<S>::key_below(ws.top_value + (log2(s.least) - 0x1p-20) / s.c, a.scale));
+            list_m = collect();
         }
 
         uint64_t z = 0, want = 0;
@@ -451,82 +527,164 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
             if (a.probs) a.probs[r] = (float)((double)w / (double)z);
         };
 
-        if (list_k || list_p) {
-            uint32_t k[2];
+        if (list_k || list_p || list_m) {
+            // two neighbours of the list a thread
+            uint32_t k[2], b[2];
             uint64_t w[2];
+            const float high_f = Logit<S>::coarse(top), per = (float)(kBins - 1) / (high_f - Logit<S>::coarse(from));
 #pragma unroll
             for (uint32_t i = 0; i < 2; ++i) {
-                const uint32_t e = tid + i * kThreads;
+                const uint32_t e = 2 * tid + i;
                 k[i] = e < listed ? sh.key[e] : 0u;
                 w[i] = weight<S>(ws, k[i]);
+                b[i] = bin_of(high_f, per, Logit<S>::coarse(k[i]));
             }
-            auto search = [&](bool by_mass, uint64_t need) {
-                uint32_t lo = from, hi = top;
-                uint64_t above = 0;
-                for (;;) {
-                    const uint32_t width = width_of(lo, hi);
-                    clear_bins(sh);
+            uint32_t equal = 0;  // keys equal to the cut's
+            const bool by_k = list_k;
+            list_k &= listed > s.k;
+            if (list_k || list_p) {
+                clear_bins(sh);
 #pragma unroll
-                    for (uint32_t i = 0; i < 2; ++i)
-                        if (k[i] >= lo && k[i] <= hi) {
-                            const uint32_t b = (hi - k[i]) >> width;
-                            atomicAdd(&sh.num[b], 1u);
-                            if (by_mass) atomicAdd((unsigned long long*)&sh.mass[b], (unsigned long long)w[i]);
-                        }
-                    const Found f = find_bin(sh, by_mass, need, above);
-                    if (!f.any) {
-                        cut = kAll;
-                        return;
+                for (uint32_t i = 0; i < 2; ++i)
+                    if (k[i]) {
+                        atomicAdd(&sh.num[b[i]], 1u);
+                        atomicAdd((unsigned long long*)&sh.mass[b[i]], (unsigned long long)w[i]);
                     }
-                    enter_bin(lo, hi, f.bin, width);
-                    above = f.above;
-                    if (f.num == 1 || width == 0) {
-                        // one value: that of whoever has it
+                __syncthreads();
+                const uint32_t n0 = sh.num[2 * tid], n1 = sh.num[2 * tid + 1];
+                const uint64_t m0 = sh.mass[2 * tid], m1 = sh.mass[2 * tid + 1];
+                const Scan sc = group_incl(sh, n0 + n1, m0 + m1);  // of the bins
+                // The cut of the least prefix with `need` keys or units of weight; returns the prefix's weight.
+                auto search = [&](bool by_mass, uint64_t need) {
+                    const uint64_t end = by_mass ? sc.mass : sc.num, v1 = by_mass ? m1 : n1, v0 = by_mass ? m0 : n0;
+                    __syncthreads();
+                    if (tid == 0) sh.members = 0;
+                    if (end - v1 - v0 < need && need <= end) {
+                        const bool second = end - v1 < need;
+                        sh.found_bin = 2 * tid + second;
+                        sh.found_above = second ? end - v1 : end - v1 - v0;
+                        sh.found_mass = sc.mass - m1 - (second ? 0 : m0);
+                    }
+                    __syncthreads();
+                    const uint32_t bin = sh.found_bin, num = sh.num[bin];
+                    const uint64_t above = sh.found_above, above_m = sh.found_mass;
+                    if (num <= kMembers) {
+                        // the bin's keys, a lane each (in every wave): their order by comparison
 #pragma unroll
                         for (uint32_t i = 0; i < 2; ++i)
-                            if (k[i] >= lo && k[i] <= hi) sh.found_key = k[i];
+                            if (k[i] && b[i] == bin) {
+                                const uint32_t at = atomicAdd(&sh.members, 1u);
+                                sh.member_key[at] = k[i];
+                                sh.member_mass[at] = w[i];
+                            }
                         __syncthreads();
-                        const uint32_t key = sh.found_key;
-                        cut = {key, ties_of(need, above, by_mass ? weight<S>(ws, key) : 1u, f.num)};
-                        return;
+                        const bool in = lane < num;
+                        const uint32_t key = in ? sh.member_key[lane] : 0u;
+                        const uint64_t v = in ? sh.member_mass[lane] : 0u;
+                        uint32_t more = 0, same = 0;
+                        uint64_t more_m = 0;
+                        for (uint32_t j = 0; j < num; ++j) {
+                            const uint32_t kj = sh.member_key[j];
+                            if (kj > key) ++more, more_m += sh.member_mass[j];
+                            same += kj == key ? 1u : 0u;
+                        }
+                        const uint64_t start = above + (by_mass ? more_m : more), each = by_mass ? v : 1u;
+                        const uint64_t hit = __ballot(in && start < need && need <= start + same * each);
+                        const int at = hit ? __ffsll((unsigned long long)hit) - 1 : 0;
+                        const uint32_t ties = ties_of(need, start, each, same);
+                        cut = {(uint32_t)__shfl((int)key, at), (uint32_t)__shfl((int)ties, at)};
+                        equal = (uint32_t)__shfl((int)same, at);
+                        return (uint64_t)__shfl((long long)(above_m + more_m + ties * v), at);
                     }
-                }
-            };
-            // (of the list's entries, which are in order) those kept by `cut`
-            auto kept = [&](bool (&on)[2]) {
-                const Scan first = group_incl(sh, k[0] == cut.key ? 1u : 0u, 0);
-                const Scan second = group_incl(sh, k[1] == cut.key ? 1u : 0u, 0);
-                on[0] = k[0] > cut.key || (k[0] == cut.key && first.num <= cut.ties);
-                on[1] = k[1] > cut.key || (k[1] == cut.key && first.all_num + second.num <= cut.ties);
-            };
-            bool on[2] = {true, true};  // (places without an entry have no weight)
-            if (list_k && listed > s.k) {
-                search(false, s.k);
-                kept(on);
+                    // many in one bin: bit by bit of the key
+                    uint32_t key = 0;
+                    uint64_t got = above, got_m = above_m;
+                    for (int bit = 31; bit >= 0; --bit) {
+                        const uint32_t trial = key | 1u << bit;
+                        uint32_t c = 0;
+                        uint64_t m = 0;
+#pragma unroll
+                        for (uint32_t i = 0; i < 2; ++i)
+                            if (k[i] >= trial && b[i] == bin && k[i]) ++c, m += w[i];
+                        const Scan at = group_incl(sh, c, m);
+                        if (above + (by_mass ? at.all_mass : at.all_num) >= need) key = trial;
+                    }
+                    uint32_t c = 0, eq = 0;
+                    uint64_t m = 0;
+#pragma unroll
+                    for (uint32_t i = 0; i < 2; ++i)
+                        if (b[i] == bin && k[i]) {
+                            if (k[i] > key) ++c, m += w[i];
+                            eq += k[i] == key ? 1u : 0u;
+                        }
+                    const Scan over = group_incl(sh, c, m);
+                    equal = group_incl(sh, eq, 0).all_num;
+                    got += by_mass ? over.all_mass : over.all_num;
+                    got_m += over.all_mass;
+                    const uint64_t v = weight<S>(ws, key);
+                    cut = {key, ties_of(need, got, by_mass ? v : 1u, equal)};
+                    return got_m + cut.ties * v;
+                };
+                uint64_t reach = sc.all_mass;
+                if (list_k) reach = search(false, s.k);
+                if (list_p) search(true, by_k ? part_p(reach) : need_p);
             }
-            if (list_p) {
-                if (list_k) need_p = part_p(group_incl(sh, 0, (on[0] ? w[0] : 0) + (on[1] ? w[1] : 0)).all_mass);
-                search(true, need_p);
-                kept(on);
+            bool on[2] = {k[0] > cut.key, k[1] > cut.key};
+            if (cut.ties >= equal) {
+                on[0] |= k[0] == cut.key, on[1] |= k[1] == cut.key;
+            } else {
+                const uint32_t t0 = k[0] == cut.key ? 1u : 0u, t1 = k[1] == cut.key ? 1u : 0u;
+                const uint32_t rank = group_incl(sh, t0 + t1, 0).num - t0 - t1;
+                on[0] |= t0 && rank < cut.ties;
+                on[1] |= t1 && rank + t0 < cut.ties;
             }
 #pragma unroll
             for (uint32_t i = 0; i < 2; ++i)
                 if (!on[i] || w[i] < least) w[i] = 0;
-            const Scan first = group_incl(sh, 0, w[0]), second = group_incl(sh, 0, w[1]);
-            draw_of(first.all_mass + second.all_mass);
-            if (w[0] && first.mass > want && first.mass - w[0] <= want) put(sh.index[tid], w[0]);
-            const uint64_t at = first.all_mass + second.mass;
-            if (w[1] && at > want && at - w[1] <= want) put(sh.index[tid + kThreads], w[1]);
+            const Scan sum = group_incl(sh, 0, w[0] + w[1]);
+            draw_of(sum.all_mass);
+            const uint64_t at0 = sum.mass - w[0] - w[1], at1 = at0 + w[0];
+            if (w[0] && at0 <= want && want < at1) put(sh.index[2 * tid], w[0]);
+            if (w[1] && at1 <= want && want < at1 + w[1]) put(sh.index[2 * tid + 1], w[1]);
             continue;
         }
 
-        // On the row: the kept weights in the order of the vocabulary, their total, then the token.
-        for (int pass = 0; pass < 2; ++pass) {
+        uint32_t first = 0;   // step that the passes begin with
+        uint64_t first_sum = 0;
+        int first_pass = 0;
+        if (cut.key == 0u) {
+            // The whole row: the sums of its steps (1024 at most), then the step that the token is in.
+            clear_bins(sh);
+#pragma unroll 1
+            for (uint32_t st = 0; st < steps; ++st) {
+                uint32_t k[kAhead][kVec];
+                row.keys(st, k);
+                uint64_t own = 0;
+#pragma unroll
+                for (uint32_t q = 0; q < kAhead; ++q)
+#pragma unroll
+                    for (uint32_t e = 0; e < kVec; ++e) {
+                        const uint64_t w = weight<S>(ws, k[q][e]);
+                        own += w < least ? 0u : w;
+                    }
+                own = wave_incl(own);
+                if (lane == 63) atomicAdd((unsigned long long*)&sh.mass[st], (unsigned long long)own);
+            }
+            __syncthreads();
+            const uint64_t m = tid < steps ? sh.mass[tid] : 0u;
+            const Scan sc = group_incl(sh, 0, m);
+            draw_of(sc.all_mass);
+            if (sc.mass - m <= want && want < sc.mass) sh.found_bin = tid, sh.found_above = sc.mass - m;
+            __syncthreads();
+            first = sh.found_bin, first_sum = sh.found_above, first_pass = 1;
+        }
+        // The kept weights in the order of the vocabulary: their total, then the token.
+        for (int pass = first_pass; pass < 2; ++pass) {
             uint32_t seen = 0;  // ties before
-            uint64_t sum = 0;
+            uint64_t sum = first_sum;
             bool done = false;
 #pragma unroll 1
-            for (uint32_t st = 0; st < steps && !done; ++st) {
+            for (uint32_t st = first; st < steps && !done; ++st) {
                 uint32_t k[kAhead][kVec];
                 row.keys(st, k);
 #pragma unroll 1
