@@ -12,13 +12,13 @@
 // Weights are held as whole multiples of 2^-shift, so that every sum is exact, atomics
 // included, and no order of additions decides a token at a border.
 //
-// A workgroup takes a row.  What is near the top goes, in order, to a list in LDS, on
-// which thresholds and the draw are found without the row: with top-k, the kth largest of
-// 4096 maxima, four a thread, is a bound that k logits at least reach (and not many more);
-// with min-p alone, its border; with top-p alone, a histogram of the weights by the first
-// digit of the key says where to cut.  The row then is read twice or three times, but once
-// from memory.  Where the list would not hold them, the digits of the row's keys are
-// searched to the last.
+// A workgroup takes a row.  It is read once for the maxima of 4096 groups of its values,
+// four a thread.  What is near the top goes to a list in LDS, from the groups whose maximum
+// reaches it, and thresholds and the draw are found there: with top-k, the kth largest
+// maximum is a bound that k logits at least reach (and not many more); with min-p alone, its
+// border; with top-p alone, a histogram of the weights by the first digit of the key, for
+// which the row is read again, says where to cut.  Where the list would not hold them, the
+// digits of the row's keys are searched to the last.
 #include "mvk_internal.h"
 #include "rowio.h"
 
@@ -106,6 +106,21 @@ __device__ __forceinline__ uint64_t part_of(double f, uint64_t z, bool& left) {
 // rounded to 2^-44; its first 10 bits after the point are looked up, the other 34 go
 // into a cubic in 32 bits, which below 2^-10 loses 2^-33 of the weight at most.
 constexpr uint32_t kTable = 1024;
+struct Powers {
+    double p[kTable];  // 2^(j / kTable)
+};
+constexpr Powers powers() {
+    Powers t = {};
+    for (uint32_t j = 0; j < kTable; ++j) {
+        // the series of exp(j ln 2 / kTable), from its last term on
+        const double x = j * 0.69314718055994530942 / kTable;
+        double s = 1.;
+        for (int i = 22; i >= 1; --i) s = 1. + x / i * s;
+        t.p[j] = s;
+    }
+    return t;
+}
+__device__ const Powers kPowers = powers();
 struct Weights {
     double top_value, c;
     const double* table;  // 2^(j / kTable)
@@ -134,15 +149,28 @@ constexpr uint32_t kBins = 2048;  // of a digit: two a thread
 // kth largest maximum is reached by -4096 ln(1 - k / 4096) values, 1712 here.
 constexpr uint32_t kMaxima = 1400;
 
+// Sums of a wave's lanes up to and with each: within rows of 16 lanes, then by each row's last.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ uint32_t lanes_before(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, kRows, 0xf, false);
+}
+template <int kCtrl, int kRows>
+__device__ __forceinline__ uint64_t lanes_before(uint64_t x) {
+    return (uint64_t)lanes_before<kCtrl, kRows>((uint32_t)(x >> 32)) << 32 | lanes_before<kCtrl, kRows>((uint32_t)x);
+}
 template <typename N>
 __device__ __forceinline__ N wave_incl(N x) {
-    const uint32_t lane = threadIdx.x & 63;
-#pragma unroll
-    for (uint32_t s = 1; s < 64; s <<= 1) {
-        const N y = __shfl_up(x, s);
-        if (lane >= s) x += y;
-    }
+    x += lanes_before<0x111, 0xf>(x);  // row_shr by 1, 2, 4, 8
+    x += lanes_before<0x112, 0xf>(x);
+    x += lanes_before<0x114, 0xf>(x);
+    x += lanes_before<0x118, 0xf>(x);
+    x += lanes_before<0x142, 0xa>(x);  // lane 15 of the row before, to rows 1 and 3
+    x += lanes_before<0x143, 0xc>(x);  // lane 31, to rows 2 and 3
     return x;
+}
+__device__ __forceinline__ uint32_t of_lane(uint32_t x, uint32_t lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, (int)lane); }
+__device__ __forceinline__ uint64_t of_lane(uint64_t x, uint32_t lane) {
+    return (uint64_t)of_lane((uint32_t)(x >> 32), lane) << 32 | of_lane((uint32_t)x, lane);
 }
 
 // A row, by steps of kAhead granules a thread: kVec values from at(step, q) on.
@@ -152,48 +180,45 @@ struct RowOf {
     static constexpr uint32_t kVec = 16 / sizeof(T), kAhead = 4;
     const T* x;
     uint32_t n;
-    bool wide;
     __device__ __forceinline__ uint32_t steps() const { return (n + kVec * kThreads * kAhead - 1) / (kVec * kThreads * kAhead); }
     static __device__ __forceinline__ uint32_t at(uint32_t step, uint32_t q) {
         return ((step * kAhead + q) * kThreads + threadIdx.x) * kVec;
     }
-    // Numbers of a step (the least beyond the row), its loads in flight together.
     typedef typename Logit<S>::N N;
-    __device__ __forceinline__ void numbers(uint32_t step, N (&k)[kAhead][kVec]) const {
-        typedef T V __attribute__((ext_vector_type(kVec)));
-        V v[kAhead];
-        if (wide) {
-            const uint32_t whole = n / kVec * kVec;
+    typedef T V __attribute__((ext_vector_type(kVec)));
+    typedef T Unaligned __attribute__((ext_vector_type(kVec), aligned(sizeof(T))));
+    // kVec values from from(i) on, in one load whatever its alignment is: those of a granule
+    // at i, or, where the row ends within it, the row's last ones.
+    __device__ __forceinline__ uint32_t from(uint32_t i) const { return n >= kVec ? min(i, n - kVec) : 0u; }
+    __device__ __forceinline__ V granule(uint32_t i) const {
+        if (n >= kVec) return *(const Unaligned*)(x + from(i));
+        V v;  // (fewer than eight in all: the last one again)
 #pragma unroll
-            for (uint32_t q = 0; q < kAhead; ++q) {
-                const uint32_t i = at(step, q);
-                if (i < whole) v[q] = *(const V*)(x + i);
-                else
-#pragma unroll
-                    for (uint32_t e = 0; e < kVec; ++e) v[q][e] = x[min(i + e, n - 1)];
-            }
-        } else {
-#pragma unroll
-            for (uint32_t q = 0; q < kAhead; ++q)
-#pragma unroll
-                for (uint32_t e = 0; e < kVec; ++e) v[q][e] = x[min(at(step, q) + e, n - 1)];
-        }
-        const bool inside = ((step + 1) * kAhead * kThreads) * kVec <= n;  // (the whole workgroup's)
-#pragma unroll
-        for (uint32_t q = 0; q < kAhead; ++q)
-#pragma unroll
-            for (uint32_t e = 0; e < kVec; ++e) {
-                k[q][e] = Logit<S>::number(v[q][e]);
-                if (!inside && at(step, q) + e >= n) k[q][e] = Logit<S>::least();
-            }
+        for (uint32_t e = 0; e < kVec; ++e) v[e] = x[min(e, n - 1)];
+        return v;
     }
-    __device__ __forceinline__ void keys(uint32_t step, uint32_t (&k)[kAhead][kVec]) const {
-        N v[kAhead][kVec];
-        numbers(step, v);
+    __device__ __forceinline__ void load(uint32_t step, V (&v)[kAhead]) const {
 #pragma unroll
-        for (uint32_t q = 0; q < kAhead; ++q)
+        for (uint32_t q = 0; q < kAhead; ++q) v[q] = granule(at(step, q));
+    }
+    // use(key) for every value, end(i) after those from kBlock i on up to the next: four values a thread,
+    // 1024 apart.  (One copy of `use`: what is not needed often would else be most of the program.)
+    static constexpr uint32_t kBlock = 4 * kThreads;
+    template <typename Use, typename End>
+    __device__ __forceinline__ void each(Use use, End end) const {
+#pragma unroll 1
+        for (uint32_t i0 = 0; i0 < n; i0 += kBlock) {
+            T v[4];
 #pragma unroll
-            for (uint32_t e = 0; e < kVec; ++e) k[q][e] = v[q][e] == Logit<S>::least() ? 0u : Logit<S>::key(v[q][e]);
+            for (uint32_t u = 0; u < 4; ++u) v[u] = x[min(i0 + u * kThreads + threadIdx.x, n - 1)];
+#pragma unroll 1
+            for (uint32_t u = 0; u < 4; ++u) {
+                const N f = Logit<S>::number(v[0]);
+                v[0] = v[1], v[1] = v[2], v[2] = v[3];
+                if (i0 + u * kThreads + threadIdx.x < n) use(f == Logit<S>::least() ? 0u : Logit<S>::key(f));
+            }
+            end(i0 / kBlock);
+        }
     }
 };
 
@@ -202,37 +227,38 @@ struct Shared {
     double table[kTable];
     uint64_t mass[kBins];
     uint32_t num[kBins];
-    uint32_t key[kList], index[kList];
-    uint64_t wave_mass[kWaves];
-    uint32_t wave_num[kWaves], counts[2][64];
+    uint32_t key[kList], index[kList], group[kList];
+    uint64_t weight[64], wave_mass[kWaves];
+    uint32_t wave_num[kWaves], wave_low[kWaves];
     uint64_t found_above, found_mass;
-    uint32_t found_bin, found_num, found_key, low;
+    uint32_t found_bin, found_num, low, groups, listed, members;
     uint64_t member_mass[kMembers];
-    uint32_t member_key[kMembers], members;
+    uint32_t member_key[kMembers];
 };
 
 // Sums over the workgroup up to and with this thread, and the whole.
+template <typename N>
+struct Sums {
+    N incl, all;
+};
+template <typename N>
+__device__ __forceinline__ Sums<N> group_incl(N (&waves)[kWaves], N x) {
+    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    const N mine = wave_incl(x);
+    __syncthreads();  // (the sums of the call before have been read)
+    if (lane == 63) waves[wave] = mine;
+    __syncthreads();
+    const N w = lane < kWaves ? waves[lane] : N(0), up = wave_incl(w);
+    return {mine + of_lane(up - w, wave), of_lane(up, 63)};
+}
 struct Scan {
     uint32_t num, all_num;
     uint64_t mass, all_mass;
 };
 __device__ __forceinline__ Scan group_incl(Shared& sh, uint32_t num, uint64_t mass) {
-    const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    Scan r = {wave_incl(num), 0, wave_incl(mass), 0};
-    __syncthreads();  // (the sums of the call before have been read)
-    if (lane == 63) sh.wave_num[wave] = r.num, sh.wave_mass[wave] = r.mass;
-    __syncthreads();
-    uint32_t before = 0;
-    uint64_t before_m = 0;
-#pragma unroll
-    for (uint32_t w = 0; w < kWaves; ++w) {
-        const uint32_t c = sh.wave_num[w];
-        const uint64_t m = sh.wave_mass[w];
-        if (w < wave) before += c, before_m += m;
-        r.all_num += c, r.all_mass += m;
-    }
-    r.num += before, r.mass += before_m;
-    return r;
+    const Sums<uint32_t> n = group_incl(sh.wave_num, num);
+    const Sums<uint64_t> m = group_incl(sh.wave_mass, mass);
+    return {n.incl, n.all, m.incl, m.all};
 }
 
 // A threshold: kept are the keys above `key` and the first `ties` of those equal to it.
@@ -253,8 +279,8 @@ __device__ __forceinline__ Found find_bin(Shared& sh, bool by_mass, uint64_t nee
     __syncthreads();  // (the bins are filled)
     const uint32_t n0 = sh.num[b], n1 = sh.num[b + 1];
     const uint64_t v0 = by_mass ? sh.mass[b] : n0, v1 = by_mass ? sh.mass[b + 1] : n1;
-    const Scan s = group_incl(sh, 0, v0 + v1);
-    const uint64_t end = above + s.mass, mid = end - v1, begin = mid - v0;
+    const Sums<uint64_t> s = group_incl<uint64_t>(sh.wave_mass, v0 + v1);
+    const uint64_t end = above + s.incl, mid = end - v1, begin = mid - v0;
     if (begin < need && need <= end) {
         const bool second = mid < need;
         sh.found_bin = b + second;
@@ -262,7 +288,7 @@ __device__ __forceinline__ Found find_bin(Shared& sh, bool by_mass, uint64_t nee
         sh.found_above = second ? mid : begin;
     }
     __syncthreads();
-    return Found{above + s.all_mass >= need, sh.found_bin, sh.found_num, sh.found_above};
+    return Found{above + s.all >= need, sh.found_bin, sh.found_num, sh.found_above};
 }
 
 // The bin of a value, the largest in the first.  (Of not-a-numbers, which infinities make: the first.)
@@ -270,15 +296,16 @@ __device__ __forceinline__ uint32_t bin_of(float high, float per, float x) {
     const float b = (high - x) * per;
     return b > 0.f ? (uint32_t)fminf(b, (float)(kBins - 1)) : 0u;
 }
-__device__ __forceinline__ uint32_t group_least(Shared& sh, uint32_t x) {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) x = min(x, (uint32_t)__shfl_xor((int)x, d));
+// find_bin by counts alone.
+__device__ __forceinline__ Found find_count(Shared& sh, uint32_t need) {
+    const uint32_t b = 2 * threadIdx.x;
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh.wave_num[threadIdx.x >> 6] = x;
+    const uint32_t n0 = sh.num[b], n1 = sh.num[b + 1];
+    const Sums<uint32_t> s = group_incl<uint32_t>(sh.wave_num, n0 + n1);
+    const uint32_t end = s.incl, all = s.all;
+    if (end - n0 - n1 < need && need <= end) sh.found_bin = b + (end - n1 < need);
     __syncthreads();
-#pragma unroll
-    for (uint32_t w = 0; w < kWaves; ++w) x = min(x, sh.wave_num[w]);
-    return x;
+    return Found{all >= need, sh.found_bin, 0, 0};
 }
 
 __device__ __forceinline__ void clear_bins(Shared& sh) {
@@ -310,41 +337,60 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
     constexpr uint32_t kVec = Row::kVec, kAhead = Row::kAhead;
     __shared__ Shared sh;
     const uint32_t tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    sh.table[tid] = exp2((double)tid / kTable);
+    const double power = kPowers.p[tid];
     for (uint32_t r = blockIdx.x; r < a.R; r += gridDim.x) {
-        const Row row = {(const typename Row::T*)a.x.p + (size_t)r * a.x.stride, a.n, a.x.wide};
+        const Row row = {(const typename Row::T*)a.x.p + (size_t)r * a.x.stride, a.n};
         const Settings s = settings_of(a, r);
         const uint32_t steps = row.steps();
 
         // The largest key, and this thread's own maxima.
         typedef typename Logit<S>::N N;
-        uint32_t mine[kAhead], top = 0;
+        uint32_t mine[kAhead], top = 0, low = 0xffffffffu;
         {
             N best[kAhead];
 #pragma unroll
             for (uint32_t q = 0; q < kAhead; ++q) best[q] = Logit<S>::least();
+            typename Row::V v[kAhead], next[kAhead];
+            row.load(0, v);
 #pragma unroll 1
             for (uint32_t st = 0; st < steps; ++st) {
-                N k[kAhead][kVec];
-                row.numbers(st, k);
+                if (st + 1 < steps) row.load(st + 1, next);
 #pragma unroll
-                for (uint32_t q = 0; q < kAhead; ++q)
+                for (uint32_t q = 0; q < kAhead; ++q) {
+                    // (a group's maximum is one of its own values: a granule at the row's end repeats some
+                    // of the one before it, one beyond has none)
+                    const uint32_t i = Row::at(st, q), skip = i < a.n ? i - row.from(i) : kVec;
+                    if (skip == 0) {
 #pragma unroll
-                    for (uint32_t e = 0; e < kVec; ++e) best[q] = Logit<S>::larger(best[q], k[q][e]);
+                        for (uint32_t e = 0; e < kVec; ++e) best[q] = Logit<S>::larger(best[q], Logit<S>::number(v[q][e]));
+                    } else {
+#pragma unroll
+                        for (uint32_t e = 0; e < kVec; ++e)
+                            best[q] = Logit<S>::larger(best[q], e >= skip ? Logit<S>::number(v[q][e]) : Logit<S>::least());
+                    }
+                    v[q] = next[q];
+                }
             }
 #pragma unroll
             for (uint32_t q = 0; q < kAhead; ++q) {
                 mine[q] = best[q] == Logit<S>::least() ? 0u : Logit<S>::key(best[q]);
                 top = max(top, mine[q]);
+                if (mine[q]) low = min(low, mine[q]);
             }
         }
 #pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+        for (int d = 32; d >= 1; d >>= 1) {
+            top = max(top, (uint32_t)__shfl_xor((int)top, d));
+            low = min(low, (uint32_t)__shfl_xor((int)low, d));
+        }
+        sh.table[tid] = power;
         __syncthreads();  // (the row before is done with everything shared)
-        if (lane == 0) sh.wave_num[wave] = top;
+        if (lane == 0) sh.wave_num[wave] = top, sh.wave_low[wave] = low;
+        if (tid == 0) sh.low = 0xffffffffu;
+        sh.num[tid] = sh.num[tid + kThreads] = 0;
         __syncthreads();
 #pragma unroll
-        for (uint32_t w = 0; w < kWaves; ++w) top = max(top, sh.wave_num[w]);
+        for (uint32_t w = 0; w < kWaves; ++w) top = max(top, sh.wave_num[w]), low = min(low, sh.wave_low[w]);
         if (top == 0u) {  // no logit above -inf
             if (tid == 0) {
                 a.tokens[r] = -1;
@@ -364,49 +410,56 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
             const uint64_t w = part_of(s.p, z, left) + (left ? 1u : 0u);
             return w ? w : 1u;
         };
-        // The list, in order; false if it does not hold them.
+        // The list, of the groups whose maximum reaches `from`; false if it does not hold them.
         auto collect = [&]() {
-            uint32_t base = 0;
+            __syncthreads();
+            if (tid == 0) sh.groups = sh.listed = 0;
+            __syncthreads();
+#pragma unroll
+            for (uint32_t q = 0; q < kAhead; ++q)
+                if (mine[q] >= from) {
+                    const uint32_t to = atomicAdd(&sh.groups, 1u);
+                    if (to < kList) sh.group[to] = q * kThreads + tid;
+                }
+            __syncthreads();
+            const uint32_t groups = sh.groups;
+            if (groups > kList) return false;
             const N least_number = Logit<S>::number_of(from);
+            const uint32_t items = groups * steps;  // granules (below 2^21)
+            constexpr uint32_t kFlight = 4;
 #pragma unroll 1
-            for (uint32_t st = 0; st < steps; ++st) {
-                N k[kAhead][kVec];
-                uint32_t c[kAhead], in[kAhead] = {}, any = 0;
-                row.numbers(st, k);
+            for (uint32_t it = tid; it < items; it += kFlight * kThreads) {
+                typename Row::V v[kFlight];
+                uint32_t at[kFlight];
 #pragma unroll
-                for (uint32_t q = 0; q < kAhead; ++q) {
-                    c[q] = 0;
-#pragma unroll
-                    for (uint32_t e = 0; e < kVec; ++e) c[q] += k[q][e] >= least_number ? 1u : 0u;
-                    any |= c[q];
+                for (uint32_t u = 0; u < kFlight; ++u) {
+                    const uint32_t i = min(it + u * kThreads, items - 1), g = sh.group[i % groups];
+                    at[u] = (i / groups * kAhead * kThreads + g) * kVec;
+                    v[u] = row.granule(at[u]);
                 }
-                if (__ballot(any != 0)) {
+#pragma unroll 1
+                for (uint32_t u = 0; u < kFlight; ++u) {
+                    const typename Row::V x = v[0];
+                    const uint32_t own = at[0], first = row.from(own);
 #pragma unroll
-                    for (uint32_t q = 0; q < kAhead; ++q) in[q] = wave_incl(c[q]);
-                }
-                if (lane == 63) {
-#pragma unroll
-                    for (uint32_t q = 0; q < kAhead; ++q) sh.counts[st & 1][q * kWaves + wave] = in[q];
-                }
-                __syncthreads();
-                const uint32_t own = sh.counts[st & 1][lane], up = wave_incl(own);
-#pragma unroll
-                for (uint32_t q = 0; q < kAhead; ++q) {
-                    uint32_t to = base + (uint32_t)__shfl((int)(up - own), (int)(q * kWaves + wave)) + in[q] - c[q];
-                    if (!c[q]) continue;
+                    for (uint32_t w = 0; w + 1 < kFlight; ++w) v[w] = v[w + 1], at[w] = at[w + 1];
+                    uint32_t hits = 0;
 #pragma unroll
                     for (uint32_t e = 0; e < kVec; ++e)
-                        if (k[q][e] >= least_number) {
-                            if (to < kList) sh.key[to] = Logit<S>::key(k[q][e]), sh.index[to] = Row::at(st, q) + e;
-                            ++to;
-                        }
+                        hits |= Logit<S>::number(x[e]) >= least_number && first + e >= own && first + e < a.n ? 1u << e : 0u;
+                    if (it + u * kThreads >= items) hits = 0;
+                    while (hits) {
+                        const uint32_t e = (uint32_t)__ffs((int)hits) - 1;
+                        hits &= hits - 1;
+                        const uint32_t to = atomicAdd(&sh.listed, 1u);
+                        // (again from memory: an index that is not known when this is compiled)
+                        if (to < kList) sh.key[to] = Logit<S>::key(Logit<S>::number(row.x[first + e])), sh.index[to] = first + e;
+                    }
                 }
-                base += (uint32_t)__shfl((int)up, 63);
-                if (base > kList) break;  // (for all alike)
             }
             __syncthreads();
-            listed = base;
-            return base <= kList;
+            listed = sh.listed;
+            return listed <= kList;
         };
         // The least prefix of the row with `need` keys or units of weight (`of_whole`: with top-p's part of
         // the whole): its cut, or false and where the list begins as soon as that can hold it.
@@ -416,31 +469,22 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
             for (;;) {
                 const uint32_t width = width_of(lo, hi);
                 clear_bins(sh);
-#pragma unroll 1
-                for (uint32_t st = 0; st < steps; ++st) {
-                    uint32_t k[kAhead][kVec];
-                    row.keys(st, k);
-#pragma unroll
-                    for (uint32_t q = 0; q < kAhead; ++q)
-#pragma unroll
-                        for (uint32_t e = 0; e < kVec; ++e) {
-                            const uint32_t key = k[q][e];
-                            if (key < lo || key > hi) continue;
-                            const uint32_t b = (hi - key) >> width;
-                            atomicAdd(&sh.num[b], 1u);
-                            if (by_mass) atomicAdd((unsigned long long*)&sh.mass[b], (unsigned long long)weight<S>(ws, key));
-                        }
-                }
+                row.each([&](uint32_t key) {
+                    if (key < lo || key > hi) return;
+                    const uint32_t b = (hi - key) >> width;
+                    atomicAdd(&sh.num[b], 1u);
+                    if (by_mass) atomicAdd((unsigned long long*)&sh.mass[b], (unsigned long long)weight<S>(ws, key));
+                }, [](uint32_t) {});
                 __syncthreads();
                 if (of_whole) {
-                    need_p = need = part_p(group_incl(sh, 0, sh.mass[tid] + sh.mass[tid + kThreads]).all_mass);
+                    need_p = need = part_p(group_incl<uint64_t>(sh.wave_mass, sh.mass[tid] + sh.mass[tid + kThreads]).all);
                     of_whole = false;
                 }
                 const Found f = find_bin(sh, by_mass, need, above);
                 const uint32_t past = f.any ? f.bin : kBins - 1;
                 uint32_t c = 0;
                 for (uint32_t b = tid; b <= past; b += kThreads) c += sh.num[b];
-                const uint32_t all = group_incl(sh, c, 0).all_num;
+                const uint32_t all = group_incl<uint32_t>(sh.wave_num, c).all;
                 if (f.any) enter_bin(lo, hi, f.bin, width);
                 if (number + all <= kList) {
                     from = lo;
@@ -463,27 +507,21 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
         if (s.k) {
             if (s.k <= kMaxima) {
                 // The kth largest of the maxima, or a little less: bins by value, of which any
-                // order would do, and the least maximum in those that hold k.
-                uint32_t low = 0xffffffffu;
-#pragma unroll
-                for (uint32_t q = 0; q < kAhead; ++q)
-                    if (mine[q]) low = min(low, mine[q]);
-                low = group_least(sh, low);
+                // order would do, and the least maximum in those that hold k.  (The bins are zero.)
                 const float high_f = Logit<S>::coarse(top), per = (float)(kBins - 1) / (high_f - Logit<S>::coarse(low));
-                clear_bins(sh);
                 uint32_t b[kAhead];
 #pragma unroll
                 for (uint32_t q = 0; q < kAhead; ++q) {
                     b[q] = bin_of(high_f, per, Logit<S>::coarse(mine[q]));
                     if (mine[q]) atomicAdd(&sh.num[b[q]], 1u);
                 }
-                const Found f = find_bin(sh, false, s.k, 0);
+                const Found f = find_count(sh, s.k);
                 if (f.any) {
-                    low = 0xffffffffu;
 #pragma unroll
                     for (uint32_t q = 0; q < kAhead; ++q)
-                        if (mine[q] && b[q] <= f.bin) low = min(low, mine[q]);
-                    from = group_least(sh, low);
+                        if (mine[q] && b[q] <= f.bin) atomicMin(&sh.low, mine[q]);
+                    __syncthreads();
+                    from = sh.low;
                 }
                 list_k = collect();
             }
@@ -493,17 +531,8 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
                 } else if (s.p < 1.) {
                     // the weight of what top-k leaves
                     uint64_t z = 0;
-#pragma unroll 1
-                    for (uint32_t st = 0; st < steps; ++st) {
-                        uint32_t k[kAhead][kVec];
-                        row.keys(st, k);
-#pragma unroll
-                        for (uint32_t q = 0; q < kAhead; ++q)
-#pragma unroll
-                            for (uint32_t e = 0; e < kVec; ++e)
-                                if (k[q][e] > cut.key) z += weight<S>(ws, k[q][e]);
-                    }
-                    need_p = part_p(group_incl(sh, 0, z).all_mass + (uint64_t)cut.ties * weight<S>(ws, cut.key));
+                    row.each([&](uint32_t key) { z += key > cut.key ? weight<S>(ws, key) : 0u; }, [](uint32_t) {});
+                    need_p = part_p(group_incl<uint64_t>(sh.wave_mass, z).all + (uint64_t)cut.ties * weight<S>(ws, cut.key));
                     if (!search_row(true, need_p, false)) list_p = collect();
                 }
             }
@@ -528,14 +557,60 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
         };
 
         if (list_k || list_p || list_m) {
-            // two neighbours of the list a thread
-            uint32_t k[2], b[2];
+            if (listed <= 64) {
+                // One wave, an entry a lane: order, thresholds and draw by comparison.
+                if (wave) continue;
+                const bool in = lane < listed;
+                const uint32_t key = in ? sh.key[lane] : 0u, index = in ? sh.index[lane] : 0xffffffffu;
+                const uint64_t v = weight<S>(ws, key);
+                sh.weight[lane] = v;
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                uint32_t rank = 0;  // entries before this one in the order of the weights, and their weight
+                uint64_t before = 0;
+                for (uint32_t j = 0; j < listed; ++j) {
+                    const uint32_t kj = sh.key[j];
+                    const uint64_t vj = sh.weight[j];
+                    if (kj > key || (kj == key && sh.index[j] < index)) ++rank, before += vj;
+                }
+                bool on = in && (!list_k || rank < s.k);
+                if (list_p) {
+                    uint64_t need = need_p;
+                    if (list_k) {
+                        // the weight that top-k leaves
+                        uint64_t all = on ? before + v : 0u;
+#pragma unroll
+                        for (int d = 32; d >= 1; d >>= 1) {
+                            const uint64_t o = (uint64_t)__shfl_xor((long long)all, d);
+                            all = o > all ? o : all;
+                        }
+                        need = part_p(all);
+                    }
+                    on = on && before < need;
+                }
+                const uint64_t w = on && v >= least ? v : 0u;
+                sh.weight[lane] = w;
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                uint64_t start = 0, total = 0;  // in the order of the vocabulary
+                for (uint32_t j = 0; j < listed; ++j) {
+                    const uint64_t wj = sh.weight[j];
+                    total += wj;
+                    if (sh.index[j] < index) start += wj;
+                }
+                draw_of(total);
+                if (w && start <= want && want < start + w) put(index, w);
+                continue;
+            }
+            // two entries of the list a thread
+            uint32_t k[2], b[2], at[2];
             uint64_t w[2];
             const float high_f = Logit<S>::coarse(top), per = (float)(kBins - 1) / (high_f - Logit<S>::coarse(from));
 #pragma unroll
             for (uint32_t i = 0; i < 2; ++i) {
                 const uint32_t e = 2 * tid + i;
                 k[i] = e < listed ? sh.key[e] : 0u;
+                at[i] = e < listed ? sh.index[e] : 0xffffffffu;
                 w[i] = weight<S>(ws, k[i]);
                 b[i] = bin_of(high_f, per, Logit<S>::coarse(k[i]));
             }
@@ -618,7 +693,7 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
                             eq += k[i] == key ? 1u : 0u;
                         }
                     const Scan over = group_incl(sh, c, m);
-                    equal = group_incl(sh, eq, 0).all_num;
+                    equal = group_incl<uint32_t>(sh.wave_num, eq).all;
                     got += by_mass ? over.all_mass : over.all_num;
                     got_m += over.all_mass;
                     const uint64_t v = weight<S>(ws, key);
@@ -633,96 +708,120 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
             if (cut.ties >= equal) {
                 on[0] |= k[0] == cut.key, on[1] |= k[1] == cut.key;
             } else {
-                const uint32_t t0 = k[0] == cut.key ? 1u : 0u, t1 = k[1] == cut.key ? 1u : 0u;
-                const uint32_t rank = group_incl(sh, t0 + t1, 0).num - t0 - t1;
-                on[0] |= t0 && rank < cut.ties;
-                on[1] |= t1 && rank + t0 < cut.ties;
+                // the first of them: the greatest bound of indices that leaves so many
+                uint32_t bound = 0;
+                for (int bit = 31; bit >= 0; --bit) {
+                    const uint32_t trial = bound | 1u << bit;
+                    uint32_t c = 0;
+#pragma unroll
+                    for (uint32_t i = 0; i < 2; ++i) c += k[i] == cut.key && at[i] < trial ? 1u : 0u;
+                    if (group_incl<uint32_t>(sh.wave_num, c).all <= cut.ties) bound = trial;
+                }
+#pragma unroll
+                for (uint32_t i = 0; i < 2; ++i) on[i] |= k[i] == cut.key && at[i] < bound;
             }
 #pragma unroll
             for (uint32_t i = 0; i < 2; ++i)
                 if (!on[i] || w[i] < least) w[i] = 0;
-            const Scan sum = group_incl(sh, 0, w[0] + w[1]);
-            draw_of(sum.all_mass);
-            const uint64_t at0 = sum.mass - w[0] - w[1], at1 = at0 + w[0];
-            if (w[0] && at0 <= want && want < at1) put(sh.index[2 * tid], w[0]);
-            if (w[1] && at1 <= want && want < at1 + w[1]) put(sh.index[2 * tid + 1], w[1]);
+            // The draw, in the order of the vocabulary: bins of indices, then one bin's entries by comparison.
+            const uint32_t have = 32 - __clz((int)a.n), narrow = have > 11 ? have - 11 : 0u;
+            clear_bins(sh);
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i)
+                if (w[i]) {
+                    atomicAdd(&sh.num[at[i] >> narrow], 1u);
+                    atomicAdd((unsigned long long*)&sh.mass[at[i] >> narrow], (unsigned long long)w[i]);
+                }
+            __syncthreads();
+            const uint64_t m0 = sh.mass[2 * tid], m1 = sh.mass[2 * tid + 1];
+            const Sums<uint64_t> sum = group_incl<uint64_t>(sh.wave_mass, m0 + m1);
+            draw_of(sum.all);
+            if (tid == 0) sh.members = 0;
+            if (sum.incl - m0 - m1 <= want && want < sum.incl) {
+                const bool second = sum.incl - m1 <= want;
+                sh.found_bin = 2 * tid + second;
+                sh.found_above = second ? sum.incl - m1 : sum.incl - m1 - m0;
+            }
+            __syncthreads();
+            const uint32_t bin = sh.found_bin;
+            if (sh.num[bin] <= kMembers) {
+#pragma unroll
+                for (uint32_t i = 0; i < 2; ++i)
+                    if (w[i] && at[i] >> narrow == bin) {
+                        const uint32_t to = atomicAdd(&sh.members, 1u);
+                        sh.member_key[to] = at[i];
+                        sh.member_mass[to] = w[i];
+                    }
+                __syncthreads();
+                if (wave) continue;
+                const uint32_t num = sh.members, index = lane < num ? sh.member_key[lane] : 0u;
+                const uint64_t v = lane < num ? sh.member_mass[lane] : 0u;
+                uint64_t start = sh.found_above;
+                for (uint32_t j = 0; j < num; ++j)
+                    if (sh.member_key[j] < index) start += sh.member_mass[j];
+                if (v && start <= want && want < start + v) put(index, v);
+                continue;
+            }
+            // many in one bin: the least bound of indices below which the weight is above `want`
+            uint32_t bound = 0;  // the greatest below which it is not
+            for (int bit = 31; bit >= 0; --bit) {
+                const uint32_t trial = bound | 1u << bit;
+                const uint64_t m = group_incl<uint64_t>(sh.wave_mass, (at[0] < trial ? w[0] : 0u) + (at[1] < trial ? w[1] : 0u)).all;
+                if (m <= want) bound = trial;
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i)
+                if (w[i] && at[i] == bound) put(bound, w[i]);
             continue;
         }
 
-        uint32_t first = 0;   // step that the passes begin with
+        uint32_t first = 0;  // value that the passes begin with
         uint64_t first_sum = 0;
         int first_pass = 0;
         if (cut.key == 0u) {
-            // The whole row: the sums of its steps (1024 at most), then the step that the token is in.
+            // The whole row: the sums of its parts, two blocks each (2048 parts at most), then the part that
+            // the token is in.
             clear_bins(sh);
-#pragma unroll 1
-            for (uint32_t st = 0; st < steps; ++st) {
-                uint32_t k[kAhead][kVec];
-                row.keys(st, k);
-                uint64_t own = 0;
-#pragma unroll
-                for (uint32_t q = 0; q < kAhead; ++q)
-#pragma unroll
-                    for (uint32_t e = 0; e < kVec; ++e) {
-                        const uint64_t w = weight<S>(ws, k[q][e]);
-                        own += w < least ? 0u : w;
-                    }
-                own = wave_incl(own);
-                if (lane == 63) atomicAdd((unsigned long long*)&sh.mass[st], (unsigned long long)own);
+            uint64_t own = 0;
+            row.each([&](uint32_t key) {
+                const uint64_t w = weight<S>(ws, key);
+                own += w < least ? 0u : w;
+            }, [&](uint32_t block) {
+                const uint64_t of_wave = wave_incl(own);
+                if (lane == 63) atomicAdd((unsigned long long*)&sh.mass[block / 2], (unsigned long long)of_wave);
+                own = 0;
+            });
+            __syncthreads();
+            const uint64_t m0 = sh.mass[2 * tid], m1 = sh.mass[2 * tid + 1];
+            const Sums<uint64_t> sc = group_incl<uint64_t>(sh.wave_mass, m0 + m1);
+            draw_of(sc.all);
+            if (sc.incl - m0 - m1 <= want && want < sc.incl) {
+                const bool second = sc.incl - m1 <= want;
+                sh.found_bin = 2 * tid + second;
+                sh.found_above = second ? sc.incl - m1 : sc.incl - m1 - m0;
             }
             __syncthreads();
-            const uint64_t m = tid < steps ? sh.mass[tid] : 0u;
-            const Scan sc = group_incl(sh, 0, m);
-            draw_of(sc.all_mass);
-            if (sc.mass - m <= want && want < sc.mass) sh.found_bin = tid, sh.found_above = sc.mass - m;
-            __syncthreads();
-            first = sh.found_bin, first_sum = sh.found_above, first_pass = 1;
+            first = sh.found_bin * 2 * Row::kBlock, first_sum = sh.found_above, first_pass = 1;
         }
         // The kept weights in the order of the vocabulary: their total, then the token.
+#pragma unroll 1
         for (int pass = first_pass; pass < 2; ++pass) {
             uint32_t seen = 0;  // ties before
             uint64_t sum = first_sum;
-            bool done = false;
 #pragma unroll 1
-            for (uint32_t st = first; st < steps && !done; ++st) {
-                uint32_t k[kAhead][kVec];
-                row.keys(st, k);
-#pragma unroll 1
-                for (uint32_t q = 0; q < kAhead && !done; ++q) {
-                    uint32_t kq[kVec], ties = 0;
-#pragma unroll
-                    for (uint32_t e = 0; e < kVec; ++e) {
-                        kq[e] = k[0][e];
-                        ties += kq[e] == cut.key ? 1u : 0u;
-                    }
-#pragma unroll
-                    for (uint32_t v = 0; v + 1 < kAhead; ++v)
-#pragma unroll
-                        for (uint32_t e = 0; e < kVec; ++e) k[v][e] = k[v + 1][e];
-                    const Scan t = group_incl(sh, ties, 0);
-                    uint32_t rank = seen + t.num - ties;
-                    seen += t.all_num;
-                    uint64_t w[kVec], own = 0;
-#pragma unroll
-                    for (uint32_t e = 0; e < kVec; ++e) {
-                        bool keep = kq[e] > cut.key;
-                        if (kq[e] == cut.key) keep = rank++ < cut.ties;
-                        w[e] = keep ? weight<S>(ws, kq[e]) : 0u;
-                        if (w[e] < least) w[e] = 0;
-                        own += w[e];
-                    }
-                    const Scan m = group_incl(sh, 0, own);
-                    uint64_t at = sum + m.mass - own;
-                    sum += m.all_mass;
-                    if (pass == 1 && sum > want) {
-#pragma unroll
-                        for (uint32_t e = 0; e < kVec; ++e) {
-                            if (w[e] && at <= want && at + w[e] > want) put(Row::at(st, q) + e, w[e]);
-                            at += w[e];
-                        }
-                        done = true;
-                    }
-                }
+            for (uint32_t i0 = first; i0 < a.n; i0 += kThreads) {
+                const uint32_t i = i0 + tid;
+                const N f = i < a.n ? Logit<S>::number(row.x[i]) : Logit<S>::least();
+                const uint32_t key = f == Logit<S>::least() ? 0u : Logit<S>::key(f), tie = key == cut.key && key ? 1u : 0u;
+                const uint64_t w = key >= cut.key ? weight<S>(ws, key) : 0u;
+                const Sums<uint32_t> t = group_incl<uint32_t>(sh.wave_num, tie);
+                const bool keep = w >= least && (key > cut.key || (tie && seen + t.incl - 1 < cut.ties));
+                seen += t.all;
+                const Sums<uint64_t> m = group_incl<uint64_t>(sh.wave_mass, keep ? w : 0u);
+                const uint64_t end = sum + m.incl;
+                sum += m.all;
+                if (pass == 1 && keep && end - w <= want && want < end) put(i, w);
+                if (pass == 1 && sum > want) break;  // (for all alike)
             }
             if (pass == 0) draw_of(sum);
         }
