@@ -228,12 +228,13 @@ struct Shared {
     uint64_t mass[kBins];
     uint32_t num[kBins];
     uint32_t key[kList], index[kList], group[kList];
-    uint64_t weight[64], wave_mass[kWaves];
+    uint64_t wave_mass[kWaves];
     uint32_t wave_num[kWaves], wave_low[kWaves];
     uint64_t found_above, found_mass;
     uint32_t found_bin, found_num, low, groups, listed, members;
     uint64_t member_mass[kMembers];
-    uint32_t member_key[kMembers];
+    uint32_t member_key[kMembers], rank[64];
+    uint64_t before[64], start[64];
 };
 
 // Sums over the workgroup up to and with this thread, and the whole.
@@ -517,9 +518,13 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
                 }
                 const Found f = find_count(sh, s.k);
                 if (f.any) {
+                    low = 0xffffffffu;
 #pragma unroll
                     for (uint32_t q = 0; q < kAhead; ++q)
-                        if (mine[q] && b[q] <= f.bin) atomicMin(&sh.low, mine[q]);
+                        if (mine[q] && b[q] <= f.bin) low = min(low, mine[q]);
+#pragma unroll
+                    for (int d = 32; d >= 1; d >>= 1) low = min(low, (uint32_t)__shfl_xor((int)low, d));
+                    if (lane == 0) atomicMin(&sh.low, low);
                     __syncthreads();
                     from = sh.low;
                 }
@@ -558,21 +563,28 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
 
         if (list_k || list_p || list_m) {
             if (listed <= 64) {
-                // One wave, an entry a lane: order, thresholds and draw by comparison.
-                if (wave) continue;
+                // An entry a lane, in every wave: order, thresholds and draw by comparison with four of
+                // them a wave.
+                if (wave == 0) sh.rank[lane] = 0, sh.before[lane] = sh.start[lane] = 0;
+                __syncthreads();
+                const uint32_t j0 = 4 * (uint32_t)__builtin_amdgcn_readfirstlane((int)wave);
                 const bool in = lane < listed;
                 const uint32_t key = in ? sh.key[lane] : 0u, index = in ? sh.index[lane] : 0xffffffffu;
                 const uint64_t v = weight<S>(ws, key);
-                sh.weight[lane] = v;
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
                 uint32_t rank = 0;  // entries before this one in the order of the weights, and their weight
                 uint64_t before = 0;
-                for (uint32_t j = 0; j < listed; ++j) {
-                    const uint32_t kj = sh.key[j];
-                    const uint64_t vj = sh.weight[j];
-                    if (kj > key || (kj == key && sh.index[j] < index)) ++rank, before += vj;
+#pragma unroll
+                for (uint32_t j = j0; j < j0 + 4; ++j) {  // (lanes without an entry have a key of 0)
+                    const uint32_t kj = of_lane(key, j);
+                    const uint64_t vj = of_lane(v, j);
+                    const bool first = kj > key || (kj == key && of_lane(index, j) < index);
+                    rank += first ? 1u : 0u;
+                    before += first ? vj : 0u;
                 }
+                atomicAdd(&sh.rank[lane], rank);
+                atomicAdd((unsigned long long*)&sh.before[lane], (unsigned long long)before);
+                __syncthreads();
+                rank = sh.rank[lane], before = sh.before[lane];
                 bool on = in && (!list_k || rank < s.k);
                 if (list_p) {
                     uint64_t need = need_p;
@@ -589,17 +601,15 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
                     on = on && before < need;
                 }
                 const uint64_t w = on && v >= least ? v : 0u;
-                sh.weight[lane] = w;
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                uint64_t start = 0, total = 0;  // in the order of the vocabulary
-                for (uint32_t j = 0; j < listed; ++j) {
-                    const uint64_t wj = sh.weight[j];
-                    total += wj;
-                    if (sh.index[j] < index) start += wj;
-                }
+                const uint64_t total = of_lane(wave_incl(w), 63);
+                uint64_t start = 0;  // in the order of the vocabulary
+#pragma unroll
+                for (uint32_t j = j0; j < j0 + 4; ++j) start += of_lane(index, j) < index ? of_lane(w, j) : 0u;
+                atomicAdd((unsigned long long*)&sh.start[lane], (unsigned long long)start);
+                __syncthreads();
+                start = sh.start[lane];
                 draw_of(total);
-                if (w && start <= want && want < start + w) put(index, w);
+                if (wave == 0 && w && start <= want && want < start + w) put(index, w);
                 continue;
             }
             // two entries of the list a thread
