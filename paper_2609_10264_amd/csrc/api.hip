@@ -1442,8 +1442,9 @@ mvk_status mvk_paged_attention(const mvk_rows* q, uint32_t T, uint32_t heads, co
     else if (T)
         e = launch_attend_any(rq, T, heads, kv, sq, scale, ro, inv_scale, lse, s);
     if (e == hipSuccess && w_out)
-        e = (tile ? launch_weights_tile : launch_weights_any)(rq, T, heads, kv, sq, scale, lse, w_in, w_out, w_seq,
-                                                              w_head, s);
+        e = tile ? launch_weights_tile(rq, T, heads, kv, sq, scale, lse, w_in, w_out, w_seq, w_head,
+                                       std::min(seqs->max_new, T), s)
+                 : launch_weights_any(rq, T, heads, kv, sq, scale, lse, w_in, w_out, w_seq, w_head, s);
     return hip_status(e);
 }
 

@@ -1144,20 +1144,28 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
 // p = exp(scale S - lse).  K is read once and stays in registers; the rows pass
 // through LDS 32 at a time, one tile in flight, for the four waves together.
 // A launch of its own, since a weight needs its row's whole sum; without atomics.
+// With many rows a sequence kGroups groups of four waves take the tiles of rows in turn,
+// over the same entries, and their sums are added in order: a tile is a chain of load,
+// products and weights, and one group's fill another's gaps.
 // Measured: single tokens of 8 sequences over 4096 to 12000 entries, 32 + 8 heads of
 // 128, 35 us (3.5 TB/s of K); a chunk of 256 over 6000, 46 us, 280 TFLOP/s: 392
 // workgroups, so some compute units have two and others one.
 constexpr uint32_t kWeightKeys = 128;
-template <typename T, typename C, uint32_t kDim>
-__global__ __launch_bounds__(256) void weights_tile(TileArgs a, const float* __restrict__ lse, const float* w_in,
+template <typename T, typename C, uint32_t kDim, uint32_t kGroups>
+__global__ __launch_bounds__(256 * kGroups) void weights_tile(TileArgs a, const float* __restrict__ lse, const float* w_in,
                                                     float* w_out, size_t w_seq, size_t w_head) {
     typedef typename Mma<T>::V8 V8;
     constexpr uint32_t G = kDim / 8, kT = kDim / 16, kGranules = 32 * G;  // of 32 keys or rows
     constexpr uint32_t kLoadsK = kGranules / 64, kLoadsQ = kGranules / 256, kStep = 64 / G;
-    __shared__ __attribute__((aligned(65536))) u32x4 lds[6 * kGranules];  // K of the waves, two tiles of rows
-    __shared__ float row_lse[2][32];
-    __shared__ uint32_t row_lim[2][32];
-    const uint32_t tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
+    // K of a group's waves, then two tiles of rows a group (in K's place where there are several: loads
+    // to LDS stay below 64 KB)
+    constexpr uint32_t kTiles = kGroups > 1 ? 0 : 4;
+    __shared__ __attribute__((aligned(65536))) u32x4 lds[(kGroups > 1 ? 2 * kGroups : 6) * kGranules];
+    __shared__ __attribute__((aligned(16))) float row_lse[kGroups][2][32];
+    __shared__ uint32_t row_lim[kGroups][2][32];
+    __shared__ float sums[kGroups > 1 ? kGroups : 1][kWeightKeys];
+    const uint32_t tid = threadIdx.x & 255, lane = tid & 63, col = lane & 31, half = lane >> 5;
+    const uint32_t group = uniform(threadIdx.x >> 8), wave = uniform(tid >> 6);  // (of the group)
     const uint32_t kh = blockIdx.y, s = blockIdx.z, live = a.kv.dim / 8;
     SeqSpan sp = seq_span(a.sq, a.kv.shift, s, a.tokens);
     sp = {uniform(sp.q0), uniform(sp.c), uniform(sp.n)};
@@ -1167,7 +1175,7 @@ __global__ __launch_bounds__(256) void weights_tile(TileArgs a, const float* __r
     const uint32_t rows = sp.c * a.grp;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
     const u32x4* const zero = &kZeroGranule;
-    {
+    if (group == 0) {
         typedef typename Held<C>::S S;
         const S* const kb = (const S*)a.kv.K + (size_t)kh * a.kv.kh;
         size_t page[kLoadsK];  // (all looked up before the first load waits for its own)
@@ -1186,7 +1194,7 @@ __global__ __launch_bounds__(256) void weights_tile(TileArgs a, const float* __r
         }
     }
     // rows of the first token that sees entry `first`, from a whole 32 on
-    uint32_t r0 = first > base ? (uint32_t)((int64_t)first - base) * a.grp / 32 * 32 : 0u, stage = 0;
+    uint32_t r0 = (first > base ? (uint32_t)((int64_t)first - base) * a.grp / 32 * 32 : 0u) + 32 * group, stage = 0;
     auto load = [&](uint32_t r, uint32_t to) {
 #pragma unroll
         for (uint32_t i = 0; i < kLoadsQ; ++i) {
@@ -1194,7 +1202,7 @@ __global__ __launch_bounds__(256) void weights_tile(TileArgs a, const float* __r
             const uint32_t tok = row / a.grp, head = kh * a.grp + row % a.grp;
             const T* qr = (const T*)a.q.p + (size_t)(sp.q0 + tok) * a.q.token + (size_t)head * a.q.head;
             load_lds(g < live && row < rows ? (const void*)(qr + 8 * g) : zero,
-                     lds0 + 16 * ((4 + to) * kGranules + 64 * (kLoadsQ * wave + i)));
+                     lds0 + 16 * ((kTiles + 2 * group + to) * kGranules + 64 * (kLoadsQ * wave + i)));
         }
     };
     // of row r + tid (32 threads): what is taken from its scores, and the entries that it sees
@@ -1213,45 +1221,58 @@ __global__ __launch_bounds__(256) void weights_tile(TileArgs a, const float* __r
     };
     float sum = 0.f, sum2 = 0.f;
     V8 k[kT];
-    if (r0 < rows) {
-        load(r0, 0);
-        about(r0);
-    }
+    if (kGroups == 1 && r0 < rows) load(r0, 0);
     wait_loads<0>();
+    if (kGroups > 1) __syncthreads();
 #pragma unroll
     for (uint32_t t = 0; t < kT; ++t)  // (a negative scale: its sign goes to K here)
         k[t] = __builtin_bit_cast(V8, lds[wave * kGranules + k_at<kDim>(col, 2 * t + half)] ^ a.flip);
+    if (kGroups > 1) {
+        wait_reads();
+        __syncthreads();  // (K's place is free)
+        if (r0 - 32 * group < rows) load(r0, 0);
+    }
+    about(r0);
+    // (as many tiles for every group: those beyond the rows are zeros, and seen by nobody)
 #pragma unroll 1
-    for (; r0 < rows; r0 += 32) {
-        if (tid < 32) row_lse[stage][tid] = z, row_lim[stage][tid] = lim;
+    for (; r0 - 32 * group < rows; r0 += 32 * kGroups) {
+        if (tid < 32) row_lse[group][stage][tid] = z, row_lim[group][stage][tid] = lim;
         wait_loads<0>();
         __syncthreads();  // these rows are there, and every wave has passed the other tile
-        if (r0 + 32 < rows) {
-            load(r0 + 32, stage ^ 1);
-            about(r0 + 32);
+        if (r0 - 32 * group + 32 * kGroups < rows) {
+            load(r0 + 32 * kGroups, stage ^ 1);
+            about(r0 + 32 * kGroups);
         }
         f32x16 x = {};
         V8 q[kT];
 #pragma unroll
         for (uint32_t t = 0; t < kT; ++t)
-            q[t] = __builtin_bit_cast(V8, lds[(4 + stage) * kGranules + k_at<kDim>(col, 2 * t + half)]);
+            q[t] = __builtin_bit_cast(V8, lds[(kTiles + 2 * group + stage) * kGranules + k_at<kDim>(col, 2 * t + half)]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (uint32_t t = 0; t < kT; ++t) x = Mma<T>::mul(q[t], k[t], x);
-        const bool masked = j0 + 32 > row_lim[stage][0] || r0 + 32 > rows;
+        const bool masked = j0 + 32 > row_lim[group][stage][0] || r0 + 32 > rows;
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) {
-            const f32x4 zs = *(const f32x4*)&row_lse[stage][8 * i + 4 * half];
+            const f32x4 zs = *(const f32x4*)&row_lse[group][stage][8 * i + 4 * half];
 #pragma unroll
             for (uint32_t u = 0; u < 4; ++u) {
                 float p = __builtin_amdgcn_exp2f(x[4 * i + u] * a.sl2 - zs[u]);
-                if (masked && j >= row_lim[stage][8 * i + 4 * half + u]) p = 0.f;
+                if (masked && j >= row_lim[group][stage][8 * i + 4 * half + u]) p = 0.f;
                 (u & 1 ? sum2 : sum) += p;
             }
         }
         stage ^= 1;
     }
     sum = sum_halves(sum + sum2);
+    if (kGroups > 1) {
+        if (half == 0) sums[kGroups > 1 ? group : 0][32 * wave + col] = sum;
+        __syncthreads();
+        if (group) return;
+        sum = 0.f;
+#pragma unroll
+        for (uint32_t g = 0; g < kGroups; ++g) sum += sums[kGroups > 1 ? g : 0][32 * wave + col];
+    }
     if (half == 0 && j < sp.n) {
         const size_t o = (size_t)s * w_seq + (size_t)kh * w_head + j;
         w_out[o] = ((int64_t)j < base && w_in ? w_in[o] : 0.f) + sum;
@@ -1328,24 +1349,29 @@ TileArgs tile_args(const Rows& q, uint32_t tokens, uint32_t heads, const KvView&
 
 hipError_t launch_weights_tile(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
                                float scale, const float* lse, const float* w_in, float* w_out, size_t w_seq,
-                               size_t w_head, hipStream_t s) {
+                               size_t w_head, uint32_t max_new, hipStream_t s) {
     const TileArgs a = tile_args(q, tokens, heads, kv, sq, scale);
     const uint64_t cap = (uint64_t)sq.width << kv.shift;
     const dim3 grid((uint32_t)((cap + kWeightKeys - 1) / kWeightKeys), kv.heads, sq.count);
-    auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, lse, w_in, w_out, w_seq, w_head);
+    // four tiles of rows and more in a sequence, as far as the caller knows: groups (one launch takes
+    // fewer than 2^32 threads)
+    const bool many = (uint64_t)max_new * (heads / kv.heads) > 96 && cap < (1u << 28);
+    auto go = [&](auto one, auto several, uint32_t groups) {
+        hipLaunchKernelGGL(many ? several : one, grid, dim3(many ? 256 * groups : 256), 0, s, a, lse, w_in, w_out, w_seq, w_head);
         return hipGetLastError();
     };
-    const uint32_t d = kv.dim <= 64 ? 0 : kv.dim <= 128 ? 1 : 2;
+    auto of = [&](auto t, auto c) {
+        typedef decltype(t) T;
+        typedef decltype(c) C;
+        if (kv.dim <= 64) return go(weights_tile<T, C, 64, 1>, weights_tile<T, C, 64, 4>, 4);
+        if (kv.dim <= 128) return go(weights_tile<T, C, 128, 1>, weights_tile<T, C, 128, 4>, 4);
+        return go(weights_tile<T, C, 256, 1>, weights_tile<T, C, 256, 2>, 2);
+    };
     switch (kv.type) {
-        case MVK_TYPE_BF16:
-            return d == 0 ? go(weights_tile<__bf16, __bf16, 64>) : d == 1 ? go(weights_tile<__bf16, __bf16, 128>) : go(weights_tile<__bf16, __bf16, 256>);
-        case MVK_TYPE_E4M3:
-            return d == 0 ? go(weights_tile<__bf16, E4M3, 64>) : d == 1 ? go(weights_tile<__bf16, E4M3, 128>) : go(weights_tile<__bf16, E4M3, 256>);
-        case MVK_TYPE_I8:
-            return d == 0 ? go(weights_tile<__bf16, I8, 64>) : d == 1 ? go(weights_tile<__bf16, I8, 128>) : go(weights_tile<__bf16, I8, 256>);
-        default:
-            return d == 0 ? go(weights_tile<_Float16, _Float16, 64>) : d == 1 ? go(weights_tile<_Float16, _Float16, 128>) : go(weights_tile<_Float16, _Float16, 256>);
+        case MVK_TYPE_BF16: return of(__bf16(), __bf16());
+        case MVK_TYPE_E4M3: return of(__bf16(), E4M3());
+        case MVK_TYPE_I8: return of(__bf16(), I8());
+        default: return of(_Float16(), _Float16());
     }
 }
 
