@@ -8,7 +8,8 @@ Per layer and batch of B query columns the client encodes four inputs
 and the client verifies and decrypts the seven responses.  In the schedules
 below every input is a fresh synthetic query; run_attention instead carries the
 values of an attention block through: the client's rotary positions, cache and
-attention (attention.py) between the projections q, k, v and o.
+attention (attention.py) between the projections q, k, v and o; run_decoder_layer
+those of a whole layer, with the norms and the activation (steps.py) around them.
 
 Codes are shared per shape (one privacy code per input width n, one
 verification code per output height m); P^T and Q are per matrix.  This module
@@ -30,9 +31,10 @@ from dataclasses import dataclass, field
 
 import torch
 
-from . import (FIELD, Code, Key, KVCache, PackedW, Prepared, Sequences, client_prepare_group, client_prepare_multi,
-               decode_verify, decode_verify_masked_group, encode, encode_masked, keygen, pack_weights,
-               pack_weights_group, paged_attention, rotary_append, server_eval, server_eval_group)
+from . import (FIELD, Code, Key, KVCache, PackedW, Prepared, Sequences, block_norm, client_prepare_group,
+               client_prepare_multi, decode_verify, decode_verify_masked_group, encode, encode_masked,
+               gated_activation, keygen, pack_weights, pack_weights_group, paged_attention, rotary_append,
+               server_eval, server_eval_group)
 
 # (name, m, n, input group)
 PROJECTIONS = (
@@ -136,6 +138,37 @@ def run_layer(layer: Layer, X: dict, ex: dict, ey: dict, tamper=None, stream=Non
     return out
 
 
+def _on_stream(stream):
+    return torch.cuda.stream(stream) if stream is not None else nullcontext()
+
+
+def _delegate(layer: Layer, group: str, x: torch.Tensor, ex: dict, ey: dict, res: dict, tamper, stream) -> None:
+    """The projections fed by one input, by delegation: res[name] = (Y, accept, Xhat, Yhat)."""
+    names = stage(group)
+    xh = encode(layer.keys[names[0]], x, ex[group][0], ex[group][1], stream=stream)
+    for name, yh in evaluate_stage(layer, group, xh, stream=stream).items():
+        if tamper is not None:
+            tamper(name, yh)
+        Y, acc, _, _ = decode_verify(layer.keys[name], xh, yh, ex[group][0], ex[group][1], ey[name][0], ey[name][1],
+                                     stream=stream)
+        res[name] = (Y, acc, xh, yh)
+
+
+def _copy_of(t: torch.Tensor) -> torch.Tensor:
+    c = torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device)
+    return c.copy_(t)
+
+
+def _take_if_accepted(old: torch.Tensor, new: torch.Tensor, res: dict) -> None:
+    """old = new if every accept bit is set, decided on the device."""
+    # seen[1]: some bit is not set (a fill by index: library sums clear scratch
+    # memory in a way that a captured graph must not)
+    seen = torch.zeros(2, device=old.device)
+    for _, accept, _, _ in res.values():
+        seen.index_fill_(0, (accept != 1).long(), 1.0)
+    old.copy_(torch.where(seen[1] == 0, new, old))
+
+
 def run_attention(layer: Layer, X: torch.Tensor, ex: dict, ey: dict, cache: KVCache, seqs: Sequences,
                   positions: torch.Tensor, rot: torch.Tensor, field_scale: float, out_scale: float,
                   layout: str = "half", weights: torch.Tensor | None = None, tamper=None, stream=None):
@@ -157,42 +190,57 @@ def run_attention(layer: Layer, X: torch.Tensor, ex: dict, ey: dict, cache: KVCa
     T = X.shape[0]
     res = {}
 
-    def on_stream():
-        return torch.cuda.stream(stream) if stream is not None else nullcontext()
-
-    def delegate(group, x):
-        names = stage(group)
-        xh = encode(layer.keys[names[0]], x, ex[group][0], ex[group][1], stream=stream)
-        for name, yh in evaluate_stage(layer, group, xh, stream=stream).items():
-            if tamper is not None:
-                tamper(name, yh)
-            Y, acc, _, _ = decode_verify(layer.keys[name], xh, yh, ex[group][0], ex[group][1], ey[name][0],
-                                         ey[name][1], stream=stream)
-            res[name] = (Y, acc, xh, yh)
-
-    delegate("attn_in", X)
+    _delegate(layer, "attn_in", X, ex, ey, res, tamper, stream)
     q, k, v = (res[name][0].view(T, HEADS, HEAD_DIM) for name in ("q", "k", "v"))
     p = layer.keys["q"].p
     # (what does not outlive the call belongs to the stream that uses it)
-    with on_stream():
+    with _on_stream(stream):
         q = rotary_append(q, k, v, positions, rot, cache, seqs, layout=layout, field_scale=field_scale, p=p,
                           stream=stream)
-        collected = None
-        if weights is not None:
-            collected = torch.empty_strided(weights.shape, weights.stride(), dtype=weights.dtype, device=weights.device)
-            collected.copy_(weights)
+        collected = _copy_of(weights) if weights is not None else None
         x = paged_attention(q, cache, seqs, out_dtype=FIELD, field_scale=out_scale, weights=weights,
                             weights_out=collected, p=p, stream=stream)
-    delegate("attn_out", x.view(T, HEADS * HEAD_DIM))
+    _delegate(layer, "attn_out", x.view(T, HEADS * HEAD_DIM), ex, ey, res, tamper, stream)
     if weights is not None:
-        with on_stream():
-            # seen[1]: some bit is not set (a fill by index: library sums clear scratch
-            # memory in a way that a captured graph must not)
-            seen = torch.zeros(2, device=weights.device)
-            for _, accept, _, _ in res.values():
-                seen.index_fill_(0, (accept != 1).long(), 1.0)
-            weights.copy_(torch.where(seen[1] == 0, collected, weights))
+        with _on_stream(stream):
+            _take_if_accepted(weights, collected, res)
     return res["o"][0], res
+
+
+def run_decoder_layer(layer: Layer, h: torch.Tensor, ex: dict, ey: dict, cache: KVCache, seqs: Sequences,
+                      positions: torch.Tensor, rot: torch.Tensor, norms: dict, query_scale: dict, field_scale: dict,
+                      act: str = "silu", layout: str = "half", weights: torch.Tensor | None = None, tamper=None,
+                      stream=None):
+    """One decoder layer for the new tokens' stream h (T x 4096 floats), its seven
+    projections by delegation and everything between them on the client:
+
+        h = h + after(o(attention(q, k, v of before(h))))
+        h = h + after(down(act(gate) * up of before(h)))
+
+    norms: {"attn_in": Norm, "mlp_in": Norm} before the blocks and, where a model has
+    them, "attn_out" and "mlp_out" after them.  query_scale[group]: the value of 1 in
+    the query of an input (field elements); field_scale[group]: of 1 in what its
+    projections return (the weights' scale times the query's).  The rest as in
+    run_attention (ex, ey with every input and projection).
+    Returns (h, {name: (Y, accept, Xhat, Yhat)}): a new stream, good if every accept
+    bit is set.  Otherwise, as there, `weights` is as before the call, the cache differs
+    in the new tokens' entries alone, and the call may be made again."""
+    p = layer.keys["q"].p
+    with _on_stream(stream):  # (what is allocated here is reused in that stream's order)
+        x, _ = block_norm(None, h, before=norms["attn_in"], out_dtype=FIELD, out_scale=query_scale["attn_in"], p=p)
+        collected = _copy_of(weights) if weights is not None else None
+        yo, res = run_attention(layer, x, ex, ey, cache, seqs, positions, rot, field_scale["attn_in"],
+                                query_scale["attn_out"], layout=layout, weights=collected, tamper=tamper)
+        x, mid = block_norm(yo, h, before=norms["mlp_in"], after=norms.get("attn_out"),
+                            field_scale=field_scale["attn_out"], out_dtype=FIELD, out_scale=query_scale["mlp_in"], p=p)
+        _delegate(layer, "mlp_in", x, ex, ey, res, tamper, None)
+        x = gated_activation(res["gate"][0], res["up"][0], act=act, field_scale=field_scale["mlp_in"],
+                             out_dtype=FIELD, out_scale=query_scale["mlp_out"], p=p)
+        _delegate(layer, "mlp_out", x, ex, ey, res, tamper, None)
+        _, out = block_norm(res["down"][0], mid, after=norms.get("mlp_out"), field_scale=field_scale["mlp_out"], p=p)
+        if weights is not None:
+            _take_if_accepted(weights, collected, res)
+    return out, res
 
 
 def prepare_input(layer: Layer, group: str, ex: dict, ey: dict, preps: dict, flag: torch.Tensor | None = None,
@@ -391,5 +439,5 @@ def macs_per_layer(B: int) -> int:
 
 
 __all__ = ["PROJECTIONS", "INPUTS", "Layer", "LayerOutputs", "build_layer", "evaluate_stage", "check_stage",
-           "run_layer", "run_attention", "HEADS", "HEAD_DIM", "prepare_input", "prepare_layer", "run_layer_prepared", "run_pass_overlapped", "codes_for",
+           "run_layer", "run_attention", "run_decoder_layer", "HEADS", "HEAD_DIM", "prepare_input", "prepare_layer", "run_layer_prepared", "run_pass_overlapped", "codes_for",
            "input_width", "stage", "macs_per_layer", "Code"]
