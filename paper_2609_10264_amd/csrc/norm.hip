@@ -161,7 +161,10 @@ __global__ __launch_bounds__(kThreads) void block_norm(NormArgs a) {
         for (int i = 0; i < kEach; ++i) v[i] = V{};
         if (a.x.p) {
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) v[i] = x[i].template values<A>(a.x.type, a.x_scale) * (A)(count[i] ? 1 : 0);
+            for (int i = 0; i < kEach; ++i) {
+                v[i] = x[i].template values<A>(a.x.type, a.x_scale);
+                if (!count[i]) v[i] = V{};
+            }
             if (a.after.on)
                 apply_norm<A, kEach>(v, count, a.after, share, part, turn,
                                      [&](const void* p, int i) { return load_params<A>(p, a.after.type, at[i]); });
@@ -276,6 +279,7 @@ hipError_t launch_norm_of(const NormArgs& a, hipStream_t s) {
     if (chunks <= 1024 && a.T <= 512) return go(block_norm<A, 1024, 1, kX, kS>, 1024, 1);
     if (chunks <= 512) return go(block_norm<A, 256, 2, kX, kS>, 256, 2);
     if (chunks <= 1024) return go(block_norm<A, 512, 2, kX, kS>, 512, 2);
+    if (chunks <= 2048) return go(block_norm<A, 1024, 2, kX, kS>, 1024, 2);
     return go(block_norm<A, 1024, 4, kX, kS>, 1024, 4);
 }
 

@@ -227,6 +227,28 @@ def test_not_finite_rows_stay_by_themselves():
     assert bool((f[1] == 0).all())
 
 
+@pytest.mark.parametrize("n", [72, 77, 600, 9000])
+def test_an_infinite_value_is_over_its_own_root_only(n):
+    """v / inf: zeros but for the infinite value itself."""
+    c = Case(3, n, x=F32, res=F32, before=False, gate="none", weight=False)
+    c.x[1, 2] = math.inf
+    _, h = c.call()
+    want = c.res[1].clone()
+    want[2] = math.nan
+    assert torch.equal(h[1].cpu().isnan(), want.isnan())
+    assert torch.equal(h[1].cpu().nan_to_num(0), want.nan_to_num(0))
+
+
+@pytest.mark.parametrize("n", [8200, 8201, 12288, 16392, 24576, 32761])
+@pytest.mark.parametrize("x,res", [(BF, F32), (FIELD, BF)])
+def test_wide_rows_in_32_and_64_bits(n, x, res):
+    c = Case(3, n, x=x, res=res, kind="layer", gate="token")
+    y, h = c.call()
+    c.check(y, h)
+    y, h = c.call(out_dtype=FIELD, out_scale=2.0**-20)
+    c.check(y, h, 2.0**-20)
+
+
 def test_zero_rows_and_large_values():
     for eps in (1e-6, 1e-12):
         c = Case(4, 256, x=F32, res=F32, after=False, gate="none", scale=1.0, eps=eps)
