@@ -956,7 +956,7 @@ typedef struct mvk_sampling {
  * every doubling of n), so sums are exact and have no order.
  * Errors: MVK_EINVAL (null, n zero, outputs in each other's or the inputs' memory,
  * field_scale not finite and positive), MVK_ERANGE (R or n above 2^24, buffers
- * above 2^62 bytes), MVK_ENOMEM, MVK_ECAPTURE (workspace).
+ * above 2^62 bytes).
  */
 mvk_status mvk_sample_tokens(const mvk_rows *logits, uint32_t R, uint32_t n, float field_scale,
                              const mvk_sampling *how, const float *u, int32_t *tokens, float *probs, void *stream);

@@ -1590,10 +1590,7 @@ mvk_status mvk_sample_tokens(const mvk_rows* logits, uint32_t R, uint32_t n, flo
     }
     if (R == 0) return MVK_OK;
     DrawArgs a = {matrix_of(logits, R), R, n, field_scale, *how, u, tokens, probs};
-    void* ws = nullptr;
-    const size_t bytes = draw_bytes(a);
-    if (bytes && (st = workspace((hipStream_t)stream, bytes, &ws))) return st;
-    return hip_status(launch_draw(a, ws, (hipStream_t)stream));
+    return hip_status(launch_draw(a, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -840,9 +840,7 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
 
 }  // namespace
 
-size_t draw_bytes(const DrawArgs&) { return 0; }
-
-hipError_t launch_draw(const DrawArgs& a, void*, hipStream_t s) {
+hipError_t launch_draw(const DrawArgs& a, hipStream_t s) {
     uint32_t bits = 17;  // sums of n weights stay below 2^62
     while ((1ull << bits) < a.n) ++bits;
     const dim3 grid(a.R < (1u << 20) ? a.R : 1u << 20);

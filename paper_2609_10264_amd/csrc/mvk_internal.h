@@ -323,9 +323,7 @@ struct GatedArgs;
 struct DrawArgs;
 hipError_t launch_block_norm(const NormArgs& a, hipStream_t s);
 hipError_t launch_gated(const GatedArgs& a, hipStream_t s);
-// ws: draw_bytes.
-size_t draw_bytes(const DrawArgs& a);
-hipError_t launch_draw(const DrawArgs& a, void* ws, hipStream_t s);
+hipError_t launch_draw(const DrawArgs& a, hipStream_t s);
 
 inline uint32_t ceil_div(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
 

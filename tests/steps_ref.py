@@ -3,6 +3,7 @@ bits on the CPU."""
 from __future__ import annotations
 
 import math
+from fractions import Fraction
 
 import torch
 
@@ -61,9 +62,10 @@ def token(x, u, t, k, p, least):
     if 0 < k < n:
         order = order[:k]
     if p < 1:
-        total, sum_, kept = math.fsum(w(i) for i in order), 0.0, 0
+        # (the product is not rounded: 0.9 in 64 bits is above 0.9, so 72 of 80 alike are less than 0.9 of them)
+        need, sum_, kept = Fraction(p) * Fraction(math.fsum(w(i) for i in order)), 0.0, 0
         for i in order:
-            if kept and sum_ >= p * total:
+            if kept and sum_ >= need:
                 break
             sum_ += w(i)
             kept += 1

@@ -180,6 +180,64 @@ def test_rows_and_strides():
     assert torch.equal(mvk.sample(one, _u(4, 2).cuda()), _check(x[:1].repeat(4, 1), _u(4, 2)))
 
 
+@pytest.mark.parametrize("dtype", [BF, F32, FIELD])
+def test_neighbours_in_a_large_vocabulary(dtype):
+    """What is kept lies close together, in values and in the vocabulary."""
+    n = 200003
+    g = torch.Generator().manual_seed(1)
+    x = torch.rand((4, n), generator=g) * -20 - 8
+    x[0, 5000:5100] = torch.rand(100, generator=g)
+    x[1, 131072:131272] = torch.rand(200, generator=g)
+    x[2, :] = -30.0
+    x[2, 70000:70090] = 1.0
+    x[2, 7] = 60.0  # far above: the others share a bin of values
+    x[3, 199903:] = 3.0 + torch.rand(100, generator=g) * 1e-3
+    x = ref.embed((x.double() * 2**16).round().long()) if dtype == FIELD else x.to(dtype)
+    for u in (0.0, 0.37, 0.81, 1 - 2.0**-24):
+        for how in (dict(k=90), dict(k=300, top_p=0.7), dict(top_p=0.6), dict(least=0.3), dict(k=80, t=30.0, top_p=0.9)):
+            _check(x, torch.full((4,), u), **how)
+
+
+@pytest.mark.parametrize("dtype", [F32, FIELD])
+@pytest.mark.parametrize("far", [3.0, 1000.0, 16000.0])
+def test_values_close_together_below_one_far_above(dtype, far):
+    """More than a thousand in one bin of values: their order bit by bit."""
+    n = 3000
+    x = torch.rand((3, n), generator=torch.Generator().manual_seed(2), dtype=torch.float64)
+    x[:, 1234] = far
+    x = ref.embed((x * 2**16).round().long()) if dtype == FIELD else x.to(dtype)
+    u = torch.tensor([0.1, 0.5, 0.9999])
+    for how in (dict(k=200), dict(k=900, t=1e4), dict(k=900, t=1e4, top_p=0.33), dict(top_p=0.4, t=1e4), dict(least=0.9, t=1e4)):
+        _check(x, u, **how)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("k", [1399, 1400, 1401, 2047, 2048, 2049, 5000, 29999])
+def test_more_than_the_list_holds(dtype, k):
+    """By the row: the number kept, with ties at the border (in bfloat16 many), and top-p within it."""
+    x = torch.randn((2, 30000), generator=torch.Generator().manual_seed(k)).to(dtype)
+    _check(x, torch.tensor([0.3, 0.95]), k=k)
+    _check(x, torch.tensor([0.3, 0.95]), k=k, top_p=0.9, t=5.0)
+    _check(x, torch.tensor([0.3, 0.95]), k=k, top_p=0.1, least=0.2)
+
+
+def test_all_alike_beyond_the_list():
+    x = torch.full((3, 20000), -4.5)
+    u = torch.tensor([0.0, 0.5, 1 - 2.0**-24])
+    assert _check(x, u, k=7000).tolist() == [0, 3500, 6999]
+    assert _check(x, u, top_p=0.25).tolist() == [0, 2500, 4999]
+    _check(x, u, k=9000, top_p=0.25)
+    _check(x, u, least=1.0)
+    _check(x, u, k=3)
+
+
+@pytest.mark.parametrize("least", [0.0, 1e-3, 0.5])
+def test_smallest_probability_alone(least):
+    for n, spread in ((50000, 0.3), (50000, 4.0), (70, 1.0)):
+        x = torch.randn((3, n), generator=torch.Generator().manual_seed(n)) * spread
+        _check(x, torch.tensor([0.0, 0.6, 0.99]), least=least)
+
+
 @pytest.mark.parametrize("R,n", [(3, 1000), (40, 20000)])
 def test_in_a_graph_and_on_two_streams(R, n):
     import paper_2609_10264_amd as mvk
