@@ -1483,9 +1483,7 @@ mvk_status mvk_cache_evict(const mvk_kv* src, const mvk_seqs* seqs, const float*
 
 namespace {
 
-Matrix matrix_of(const mvk_rows* r, uint32_t T) {
-    return r ? Matrix{r->data, (size_t)r->token, r->type, is_wide(r->data, r->token, r->type, T)} : Matrix{};
-}
+Matrix matrix_of(const mvk_rows* r) { return r ? Matrix{r->data, (size_t)r->token, r->type} : Matrix{}; }
 
 // Do rows of a and b meet, other than as the same rows?
 bool meet(const mvk_rows* a, const mvk_rows* b, uint32_t T, uint32_t n, bool same_is_fine) {
@@ -1509,8 +1507,7 @@ mvk_status check_norm(const mvk_norm* w) {
 
 NormView norm_of(const mvk_norm* w) {
     if (!w) return NormView{};
-    const bool wide = ((uintptr_t)w->weight | (uintptr_t)w->bias) % 16 == 0;
-    return NormView{w->weight, w->bias, w->type, w->kind, w->eps, wide, true};
+    return NormView{w->weight, w->bias, w->type, w->kind, w->eps, true};
 }
 
 inline bool is_scale(float x) { return std::isfinite(x) && x > 0; }
@@ -1549,7 +1546,7 @@ mvk_status mvk_block_norm(const mvk_rows* x, float x_scale, const mvk_rows* resi
     }
     if (meet(residual_out, out, T, n, false)) return MVK_EINVAL;
     if (T == 0) return MVK_OK;
-    NormArgs a = {matrix_of(x, T), matrix_of(residual, T), matrix_of(gate, T), matrix_of(residual_out, T), matrix_of(out, T),
+    NormArgs a = {matrix_of(x), matrix_of(residual), matrix_of(gate), matrix_of(residual_out), matrix_of(out),
                   norm_of(after), norm_of(before), T, n, x_scale, scale, out_scale};
     return hip_status(launch_block_norm(a, (hipStream_t)stream));
 }
@@ -1568,7 +1565,7 @@ mvk_status mvk_gated_activation(const mvk_rows* gate, const mvk_rows* up, uint32
     // (a value is read before its place is written, by the same thread)
     if (meet(out, gate, T, n, true) || meet(out, up, T, n, true)) return MVK_EINVAL;
     if (T == 0) return MVK_OK;
-    const GatedArgs a = {matrix_of(gate, T), matrix_of(up, T), matrix_of(out, T), T, n, act, in_scale,
+    const GatedArgs a = {matrix_of(gate), matrix_of(up), matrix_of(out), T, n, act, in_scale,
                          out->type == MVK_TYPE_FIELD ? 1.f / out_scale : 1.f};
     return hip_status(launch_gated(a, (hipStream_t)stream));
 }
@@ -1589,7 +1586,7 @@ mvk_status mvk_sample_tokens(const mvk_rows* logits, uint32_t R, uint32_t n, flo
             if (p && share_memory(rows, {p, 1, 0, 1, 0, 4ull * R})) return MVK_EINVAL;
     }
     if (R == 0) return MVK_OK;
-    DrawArgs a = {matrix_of(logits, R), R, n, field_scale, *how, u, tokens, probs};
+    DrawArgs a = {matrix_of(logits), R, n, field_scale, *how, u, tokens, probs};
     return hip_status(launch_draw(a, (hipStream_t)stream));
 }
 

@@ -334,11 +334,11 @@ __global__ __launch_bounds__(256) void read_wide(KvView kv, SeqView sq, uint32_t
             } else {
                 Raw8 r;
                 r.lo = r.hi = b;
-                store8<float>(to.p, to.type, true, i, 8, values_of<float>(r, MVK_TYPE_BF16, 0.f), 1.f);
+                store8<float>(to.p, to.type, i, values_of<float>(r, MVK_TYPE_BF16, 0.f), 1.f);
             }
         } else {
             constexpr int type = __is_same(C, __bf16) ? MVK_TYPE_BF16 : __is_same(C, _Float16) ? MVK_TYPE_F16 : MVK_TYPE_F32;
-            store8<float>(to.p, to.type, true, i, 8, values_of<float>(load_raw8(pool, type, from + 8 * g), type, 0.f), 1.f);
+            store8<float>(to.p, to.type, i, values_of<float>(load_raw8(pool, type, from + 8 * g), type, 0.f), 1.f);
         }
     };
     copy(k, kv.K, page * kv.kp + h * kv.kh + at * kv.ke, kv.kx, page * kv.kxp + h * kv.kxh + at * kv.kxe);

@@ -18,15 +18,26 @@ __device__ __forceinline__ float activate(float x, int act) {
     return x > 0.f || x != x ? x : 0.f;
 }
 
-// A thread eight values of a row.
+// A thread eight values of a row, in loads of 16 bytes at any alignment.  (A value by value form for
+// rows that are no whole granules took 154 us for 4096 rows of 11007 in bfloat16; 58 those of 11008.)
 __global__ __launch_bounds__(256) void gated_activation(GatedArgs a, uint32_t chunks, uint64_t count) {
     for (uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x; id < count; id += (uint64_t)gridDim.x * 256) {
-        const uint32_t t = (uint32_t)(id / chunks), at = 8 * (uint32_t)(id % chunks), c = min(8u, a.n - at);
-        f32x8 g = load8<float>(a.gate.p, a.gate.type, a.gate.wide, t * a.gate.stride + at, c, a.in_scale);
-        const f32x8 u = load8<float>(a.up.p, a.up.type, a.up.wide, t * a.up.stride + at, c, a.in_scale);
+        const uint32_t t = (uint32_t)(id / chunks);
+        const size_t g0 = t * a.gate.stride, u0 = t * a.up.stride, o0 = t * a.out.stride;
+        f32x8 g, u;
+        if (a.n < 8) {
+            g = load_some<float>(a.gate.p, a.gate.type, g0, a.n, a.in_scale);
+            u = load_some<float>(a.up.p, a.up.type, u0, a.n, a.in_scale);
+        }
+        const Piece p = a.n < 8 ? Piece{0, 8 - a.n} : piece_of((uint32_t)(id % chunks), a.n);
+        if (a.n >= 8) {
+            g = values_of<float>(load_raw8(a.gate.p, a.gate.type, g0 + p.at), a.gate.type, a.in_scale);
+            u = values_of<float>(load_raw8(a.up.p, a.up.type, u0 + p.at), a.up.type, a.in_scale);
+        }
 #pragma unroll
         for (int k = 0; k < 8; ++k) g[k] = activate(g[k], a.act) * u[k];
-        store8<float>(a.out.p, a.out.type, a.out.wide, t * a.out.stride + at, c, g, a.inv_scale);
+        if (a.n < 8) store_some<float>(a.out.p, a.out.type, o0, 0, a.n, g, a.inv_scale);
+        else store_piece<float>(a.out.p, a.out.type, o0, p, g, a.inv_scale);
     }
 }
 

@@ -5,6 +5,9 @@
 // A workgroup takes a row and keeps it in registers, so that every input is read
 // and every output written once; the sums of a norm go across its waves by way of
 // LDS.  Bound by memory for many rows, by the chain load, sums, store for few.
+// Loads and stores are of 16 bytes at any alignment; where a row is no whole chunks of eight, its
+// last thread takes the last eight values and skips those of the one before it (4096 rows of 8190
+// in bfloat16, both norms: 66 us, 60.5 of 8192; value by value 292).
 // Values and sums are in 32 bits, in 64 with a FIELD output: its whole numbers are
 // chosen next to borders and reach 2^30, beyond what 32 bits hold.  (There h in a 16-bit
 // residual_out is rounded by way of 32 bits: 2^-16 of a step more at most in bfloat16.)
@@ -45,7 +48,7 @@ struct Chunk;
 template <>
 struct Chunk<2> {
     u32x4_ r;
-    __device__ __forceinline__ void load(const void* p, size_t i) { r = *(const u32x4_*)((const uint16_t*)p + i); }
+    __device__ __forceinline__ void load(const void* p, size_t i) { r = *(const u32x4_at2*)((const uint16_t*)p + i); }
     template <typename A>
     __device__ __forceinline__ typename Eight<A>::V values(int type, float) const {
         typedef __bf16 B8 __attribute__((ext_vector_type(8)));
@@ -62,8 +65,8 @@ template <>
 struct Chunk<4> {
     u32x4_ lo, hi;
     __device__ __forceinline__ void load(const void* p, size_t i) {
-        lo = ((const u32x4_*)((const uint32_t*)p + i))[0];
-        hi = ((const u32x4_*)((const uint32_t*)p + i))[1];
+        lo = ((const u32x4_at4*)((const uint32_t*)p + i))[0];
+        hi = ((const u32x4_at4*)((const uint32_t*)p + i))[1];
     }
     template <typename A>
     __device__ __forceinline__ typename Eight<A>::V values(int type, float scale) const {
@@ -91,10 +94,10 @@ __device__ __forceinline__ typename Eight<A>::V load_params(const void* p, int t
     return c.values<A>(type, 0.f);
 }
 
-// A norm of v, rows of n = 1 / share values (zeros where a chunk is not `live`), by parameters as
+// A norm of v, rows of n = 1 / share values (zeros for what a thread skips), by parameters as
 // `params` loads them.
 template <typename A, int kEach, typename Params>
-__device__ __forceinline__ void apply_norm(typename Eight<A>::V (&v)[kEach], const uint32_t (&count)[kEach], const NormView& w, A share,
+__device__ __forceinline__ void apply_norm(typename Eight<A>::V (&v)[kEach], const Piece (&at)[kEach], const NormView& w, A share,
                                            A (*part)[16], uint32_t& turn, Params params) {
     if (w.kind == MVK_NORM_LAYER) {
         A sum = 0;
@@ -106,7 +109,7 @@ __device__ __forceinline__ void apply_norm(typename Eight<A>::V (&v)[kEach], con
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
 #pragma unroll
-            for (uint32_t k = 0; k < 8; ++k) v[i][k] = k < count[i] ? v[i][k] - mean : (A)0;
+            for (uint32_t k = 0; k < 8; ++k) v[i][k] = k >= at[i].skip ? v[i][k] - mean : (A)0;
     }
     A sq = 0;
 #pragma unroll
@@ -126,33 +129,43 @@ __device__ __forceinline__ void apply_norm(typename Eight<A>::V (&v)[kEach], con
     }
 }
 
-// Rows of whole aligned granules.  kEach chunks of eight values a thread: chunk tid, tid +
-// threads, ...; kX, kS: element sizes of x and of the residual.
+// Rows of eight values and more, of any alignment.  kEach chunks of eight values a thread: chunk
+// tid, tid + threads, ...; kX, kS: element sizes of x and of the residual.
 template <typename A, int kThreads, int kEach, int kX, int kS>
 __global__ __launch_bounds__(kThreads) void block_norm(NormArgs a) {
     typedef typename Eight<A>::V V;
     __shared__ A part[2][16];
     uint32_t turn = 0;
     const uint32_t n = a.n;
-    uint32_t at[kEach], count[kEach];  // (a chunk beyond the row reads the first one, as zeros)
+    Piece at[kEach];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const uint32_t p = 8 * (threadIdx.x + i * blockDim.x);
-        count[i] = p < n ? 8u : 0u;
-        at[i] = p < n ? p : 0u;
-    }
+    for (int i = 0; i < kEach; ++i) at[i] = piece_of(threadIdx.x + i * blockDim.x, n);
     const A share = (A)1 / (A)n;
     Chunk<kX> x[kEach];
     Chunk<kS> res[kEach];
     auto load = [&](uint32_t t) {
         if (a.x.p) {
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) x[i].load(a.x.p, t * a.x.stride + at[i]);
+            for (int i = 0; i < kEach; ++i) x[i].load(a.x.p, t * a.x.stride + at[i].at);
         }
         if (a.res.p) {
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) res[i].load(a.res.p, t * a.res.stride + at[i]);
+            for (int i = 0; i < kEach; ++i) res[i].load(a.res.p, t * a.res.stride + at[i].at);
         }
+    };
+    // zeros for what another thread has: values, and what residual and biases made of them
+    auto skip = [&](V (&v)[kEach]) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (at[i].skip) {
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k) v[i][k] = k >= at[i].skip ? v[i][k] : (A)0;
+            }
+    };
+    auto store = [&](const Matrix& m, uint32_t t, const V (&v)[kEach], A inv_scale) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (at[i].skip < 8) store_piece<A>(m.p, m.type, t * m.stride, at[i], v[i], inv_scale);
     };
     if (blockIdx.x < a.T) load(blockIdx.x);
     for (uint32_t t = blockIdx.x; t < a.T; t += gridDim.x) {
@@ -161,16 +174,14 @@ __global__ __launch_bounds__(kThreads) void block_norm(NormArgs a) {
         for (int i = 0; i < kEach; ++i) v[i] = V{};
         if (a.x.p) {
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                v[i] = x[i].template values<A>(a.x.type, a.x_scale);
-                if (!count[i]) v[i] = V{};
-            }
+            for (int i = 0; i < kEach; ++i) v[i] = x[i].template values<A>(a.x.type, a.x_scale);
+            skip(v);
             if (a.after.on)
-                apply_norm<A, kEach>(v, count, a.after, share, part, turn,
-                                     [&](const void* p, int i) { return load_params<A>(p, a.after.type, at[i]); });
+                apply_norm<A, kEach>(v, at, a.after, share, part, turn,
+                                     [&](const void* p, int i) { return load_params<A>(p, a.after.type, at[i].at); });
             if (a.gate.p) {
 #pragma unroll
-                for (int i = 0; i < kEach; ++i) v[i] *= load_params<A>(a.gate.p, a.gate.type, t * a.gate.stride + at[i]);
+                for (int i = 0; i < kEach; ++i) v[i] *= load_params<A>(a.gate.p, a.gate.type, t * a.gate.stride + at[i].at);
             }
 #pragma unroll
             for (int i = 0; i < kEach; ++i) v[i] *= (A)a.scale;
@@ -181,81 +192,55 @@ __global__ __launch_bounds__(kThreads) void block_norm(NormArgs a) {
         }
         // the next row's loads run behind what is left of this one
         if (t + gridDim.x < a.T) load(t + gridDim.x);
-        // (chunks beyond the row: not what the first one's residual and biases made of them)
-#pragma unroll
-        for (int i = 0; i < kEach; ++i)
-            if (!count[i]) v[i] = V{};
-        if (a.res_out.p) {
-#pragma unroll
-            for (int i = 0; i < kEach; ++i)
-                if (count[i]) store8<A>(a.res_out.p, a.res_out.type, true, t * a.res_out.stride + at[i], 8, v[i], (A)1);
-        }
+        skip(v);
+        if (a.res_out.p) store(a.res_out, t, v, (A)1);
         if (!a.out.p) continue;
         if (a.before.on)
-            apply_norm<A, kEach>(v, count, a.before, share, part, turn,
-                                 [&](const void* p, int i) { return load_params<A>(p, a.before.type, at[i]); });
-#pragma unroll
-        for (int i = 0; i < kEach; ++i)
-            if (count[i]) store8<A>(a.out.p, a.out.type, true, t * a.out.stride + at[i], 8, v[i], (A)1 / (A)a.out_scale);
+            apply_norm<A, kEach>(v, at, a.before, share, part, turn,
+                                 [&](const void* p, int i) { return load_params<A>(p, a.before.type, at[i].at); });
+        store(a.out, t, v, (A)1 / (A)a.out_scale);
     }
 }
 
-// Any width, strides and alignment: value by value.
-template <typename A, int kEach>
-__global__ __launch_bounds__(1024) void block_norm_any(NormArgs a) {
+// Rows of fewer than eight values: one thread's.
+template <typename A>
+__global__ __launch_bounds__(64) void block_norm_short(NormArgs a) {
     typedef typename Eight<A>::V V;
-    __shared__ A part[2][16];
+    __shared__ A part[2][16];  // (not used: one wave)
     uint32_t turn = 0;
-    const uint32_t n = a.n;
-    uint32_t at[kEach], count[kEach];
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        at[i] = 8 * (threadIdx.x + i * blockDim.x);
-        count[i] = at[i] < n ? min(8u, n - at[i]) : 0u;
-    }
-    const A share = (A)1 / (A)n;
-    auto load = [&](const void* p, int type, size_t row, int i, float scale) {
+    // (as a piece: the values are the last ones of the eight)
+    const uint32_t n = threadIdx.x == 0 ? a.n : 0;
+    const Piece at[1] = {{0, 8 - n}};
+    const A share = (A)1 / (A)a.n;
+    auto load = [&](const void* p, int type, size_t row, float scale) {
         V v;
-#pragma unroll 1
-        for (uint32_t k = 0; k < 8; ++k) {
-            const A x = k < count[i] ? load_one<A>(p, type, row + at[i] + k, scale) : (A)0;
-            // (no address of a register: the index is not known when this is compiled)
 #pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) v[j] = j == k ? x : v[j];
-        }
+        for (uint32_t k = 0; k < 8; ++k) v[k] = k >= 8 - n ? load_one<A>(p, type, row + k - (8 - n), scale) : (A)0;
         return v;
     };
+    auto store = [&](const Matrix& m, size_t row, V v, A inv_scale) {
+        V first = {};
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k)
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) first[j] = k >= 8 - n && k - (8 - n) == j ? v[k] : first[j];
+        store_some<A>(m.p, m.type, row, 0, n, first, inv_scale);
+    };
     for (uint32_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-        V v[kEach];
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) v[i] = V{};
+        V v[1] = {};
         if (a.x.p) {
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) v[i] = load(a.x.p, a.x.type, t * a.x.stride, i, a.x_scale);
+            v[0] = load(a.x.p, a.x.type, t * a.x.stride, a.x_scale);
             if (a.after.on)
-                apply_norm<A, kEach>(v, count, a.after, share, part, turn,
-                                     [&](const void* p, int i) { return load(p, a.after.type, 0, i, 0.f); });
-            if (a.gate.p) {
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) v[i] *= load(a.gate.p, a.gate.type, t * a.gate.stride, i, 0.f);
-            }
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) v[i] *= (A)a.scale;
+                apply_norm<A, 1>(v, at, a.after, share, part, turn, [&](const void* p, int) { return load(p, a.after.type, 0, 0.f); });
+            if (a.gate.p) v[0] *= load(a.gate.p, a.gate.type, t * a.gate.stride, 0.f);
+            v[0] *= (A)a.scale;
         }
-        if (a.res.p) {
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) v[i] += load(a.res.p, a.res.type, t * a.res.stride, i, 0.f);
-        }
-        auto store = [&](const Matrix& m, A inv_scale) {
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) store8<A>(m.p, m.type, false, t * m.stride + at[i], count[i], v[i], inv_scale);
-        };
-        if (a.res_out.p) store(a.res_out, (A)1);
+        if (a.res.p) v[0] += load(a.res.p, a.res.type, t * a.res.stride, 0.f);
+        if (a.res_out.p) store(a.res_out, t * a.res_out.stride, v[0], (A)1);
         if (!a.out.p) continue;
         if (a.before.on)
-            apply_norm<A, kEach>(v, count, a.before, share, part, turn,
-                                 [&](const void* p, int i) { return load(p, a.before.type, 0, i, 0.f); });
-        store(a.out, (A)1 / (A)a.out_scale);
+            apply_norm<A, 1>(v, at, a.before, share, part, turn, [&](const void* p, int) { return load(p, a.before.type, 0, 0.f); });
+        store(a.out, t * a.out.stride, v[0], (A)1 / (A)a.out_scale);
     }
 }
 
@@ -263,7 +248,7 @@ inline int size_of(const Matrix& m) { return m.type <= MVK_TYPE_F16 ? 2 : 4; }
 
 template <typename A, int kX, int kS>
 hipError_t launch_norm_of(const NormArgs& a, hipStream_t s) {
-    const uint32_t chunks = a.n / 8;
+    const uint32_t chunks = (a.n + 7) / 8;
     auto go = [&](auto kernel, uint32_t most, uint32_t each) {
         uint32_t threads = ((chunks + each - 1) / each + 63) / 64 * 64;
         threads = threads < most ? threads : most;
@@ -284,27 +269,21 @@ hipError_t launch_norm_of(const NormArgs& a, hipStream_t s) {
 }
 
 template <typename A>
-hipError_t launch_norm_in(const NormArgs& a, bool wide, hipStream_t s) {
-    if (wide) {
-        const int kx = a.x.p ? size_of(a.x) : 4, ks = a.res.p ? size_of(a.res) : 4;
-        if (kx == 2) return ks == 2 ? launch_norm_of<A, 2, 2>(a, s) : launch_norm_of<A, 2, 4>(a, s);
-        return ks == 2 ? launch_norm_of<A, 4, 2>(a, s) : launch_norm_of<A, 4, 4>(a, s);
+hipError_t launch_norm_in(const NormArgs& a, hipStream_t s) {
+    if (a.n < 8) {
+        hipLaunchKernelGGL(block_norm_short<A>, dim3(a.T < (1u << 20) ? a.T : 1u << 20), dim3(64), 0, s, a);
+        return hipGetLastError();
     }
-    const uint32_t chunks = (a.n + 7) / 8, each = chunks <= 1024 ? 1 : 4;
-    const uint32_t threads = ((chunks + each - 1) / each + 63) / 64 * 64;
-    const dim3 grid(a.T < (1u << 20) ? a.T : 1u << 20), block(threads < 1024 ? threads : 1024);
-    if (each == 1) hipLaunchKernelGGL((block_norm_any<A, 1>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((block_norm_any<A, 4>), grid, block, 0, s, a);
-    return hipGetLastError();
+    const int kx = a.x.p ? size_of(a.x) : 4, ks = a.res.p ? size_of(a.res) : 4;
+    if (kx == 2) return ks == 2 ? launch_norm_of<A, 2, 2>(a, s) : launch_norm_of<A, 2, 4>(a, s);
+    return ks == 2 ? launch_norm_of<A, 4, 2>(a, s) : launch_norm_of<A, 4, 4>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_block_norm(const NormArgs& a, hipStream_t s) {
-    bool wide = a.n % 8 == 0 && (!a.after.on || a.after.wide) && (!a.before.on || a.before.wide);
-    for (const Matrix* m : {&a.x, &a.res, &a.gate, &a.res_out, &a.out}) wide &= !m->p || m->wide;
-    if (a.out.p && a.out.type == MVK_TYPE_FIELD) return launch_norm_in<double>(a, wide, s);
-    return launch_norm_in<float>(a, wide, s);
+    if (a.out.p && a.out.type == MVK_TYPE_FIELD) return launch_norm_in<double>(a, s);
+    return launch_norm_in<float>(a, s);
 }
 
 }  // namespace mvk

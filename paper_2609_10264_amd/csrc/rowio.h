@@ -8,26 +8,19 @@
 
 namespace mvk {
 
-// A matrix: element i of row t at p[t * stride + i]; wide: every row is made of whole
-// aligned 16-byte granules, as far as whole eights of its values go.
+// A matrix: element i of row t at p[t * stride + i].
 struct Matrix {
     void* p;
     size_t stride;
     int type;
-    bool wide;
 };
-
-inline bool is_wide(const void* p, size_t stride, int type, uint64_t rows) {
-    const size_t per = type == MVK_TYPE_BF16 || type == MVK_TYPE_F16 ? 8 : 4;
-    return (uintptr_t)p % 16 == 0 && (rows <= 1 || stride % per == 0);
-}
 
 // A norm's parameters; on: there is one.
 struct NormView {
     const void *weight, *bias;
     int type, kind;
     float eps;
-    bool wide, on;
+    bool on;
 };
 
 // Of block_norm (norm.hip), gated_activation (gated.hip), sample_tokens (draw.hip);
@@ -55,6 +48,9 @@ struct DrawArgs {
 };
 
 typedef uint32_t u32x4_ __attribute__((ext_vector_type(4)));
+// (of any place of a row: memory takes 16 bytes at once whatever their alignment is)
+typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef double f64x8 __attribute__((ext_vector_type(8)));
 template <typename A>
@@ -88,11 +84,11 @@ struct Raw8 {
 __device__ __forceinline__ Raw8 load_raw8(const void* p, int type, size_t i) {
     Raw8 r;
     if (type <= MVK_TYPE_F16) {
-        r.lo = *(const u32x4_*)((const uint16_t*)p + i);
+        r.lo = *(const u32x4_at2*)((const uint16_t*)p + i);
         r.hi = r.lo;
     } else {
-        r.lo = ((const u32x4_*)((const uint32_t*)p + i))[0];
-        r.hi = ((const u32x4_*)((const uint32_t*)p + i))[1];
+        r.lo = ((const u32x4_at4*)((const uint32_t*)p + i))[0];
+        r.hi = ((const u32x4_at4*)((const uint32_t*)p + i))[1];
     }
     return r;
 }
@@ -119,10 +115,20 @@ __device__ __forceinline__ typename Eight<A>::V values_of(const Raw8& r, int typ
     return v;
 }
 
-// Values i .. i + 7 (count of them; the others are zero).
+// Eight consecutive values of a row of n >= 8 by one thread: chunk c, or, where the row ends
+// within it, the row's last eight, of which the first `skip` are the chunk before's (8: all).
+struct Piece {
+    uint32_t at, skip;
+};
+__device__ __forceinline__ Piece piece_of(uint32_t c, uint32_t n) {
+    const uint32_t at = 8 * c;
+    if (at + 8 <= n) return {at, 0u};
+    return at < n ? Piece{n - 8, at + 8 - n} : Piece{0u, 8u};
+}
+
+// Values i .. i + count - 1 one by one; the others are zero.
 template <typename A>
-__device__ __forceinline__ typename Eight<A>::V load8(const void* p, int type, bool wide, size_t i, uint32_t count, float scale) {
-    if (wide && count >= 8) return values_of<A>(load_raw8(p, type, i), type, scale);
+__device__ __forceinline__ typename Eight<A>::V load_some(const void* p, int type, size_t i, uint32_t count, float scale) {
     typename Eight<A>::V v;
 #pragma unroll
     for (uint32_t k = 0; k < 8; ++k) v[k] = k < count ? load_one<A>(p, type, i + k, scale) : (A)0;
@@ -138,41 +144,50 @@ __device__ __forceinline__ uint32_t field_of(double x) {
 }
 
 template <typename A>
-__device__ __forceinline__ void store8(void* p, int type, bool wide, size_t i, uint32_t count, typename Eight<A>::V v, A inv_scale) {
-    if (wide && count >= 8) {
-        if (type == MVK_TYPE_BF16) {
-            typedef __bf16 B8 __attribute__((ext_vector_type(8)));
-            B8 x;
+__device__ __forceinline__ void store8(void* p, int type, size_t i, typename Eight<A>::V v, A inv_scale) {
+    if (type == MVK_TYPE_BF16) {
+        typedef __bf16 B8 __attribute__((ext_vector_type(8)));
+        B8 x;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = (__bf16)(float)v[k];
-            *(u32x4_*)((uint16_t*)p + i) = __builtin_bit_cast(u32x4_, x);
-        } else if (type == MVK_TYPE_F16) {
-            typedef _Float16 H8 __attribute__((ext_vector_type(8)));
-            H8 x;
+        for (int k = 0; k < 8; ++k) x[k] = (__bf16)(float)v[k];
+        *(u32x4_at2*)((uint16_t*)p + i) = __builtin_bit_cast(u32x4_, x);
+    } else if (type == MVK_TYPE_F16) {
+        typedef _Float16 H8 __attribute__((ext_vector_type(8)));
+        H8 x;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = (_Float16)(float)v[k];
-            *(u32x4_*)((uint16_t*)p + i) = __builtin_bit_cast(u32x4_, x);
-        } else {
-            const bool field = type == MVK_TYPE_FIELD;
-            u32x4_ lo, hi;
+        for (int k = 0; k < 8; ++k) x[k] = (_Float16)(float)v[k];
+        *(u32x4_at2*)((uint16_t*)p + i) = __builtin_bit_cast(u32x4_, x);
+    } else {
+        const bool field = type == MVK_TYPE_FIELD;
+        u32x4_ lo, hi;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                lo[k] = field ? field_of(v[k] * inv_scale) : __float_as_uint((float)v[k]);
-                hi[k] = field ? field_of(v[k + 4] * inv_scale) : __float_as_uint((float)v[k + 4]);
-            }
-            ((u32x4_*)((uint32_t*)p + i))[0] = lo;
-            ((u32x4_*)((uint32_t*)p + i))[1] = hi;
+        for (int k = 0; k < 4; ++k) {
+            lo[k] = field ? field_of(v[k] * inv_scale) : __float_as_uint((float)v[k]);
+            hi[k] = field ? field_of(v[k + 4] * inv_scale) : __float_as_uint((float)v[k + 4]);
         }
-        return;
+        ((u32x4_at4*)((uint32_t*)p + i))[0] = lo;
+        ((u32x4_at4*)((uint32_t*)p + i))[1] = hi;
     }
+}
+
+// Values [from, to) of them one by one.
+template <typename A>
+__device__ __forceinline__ void store_some(void* p, int type, size_t i, uint32_t from, uint32_t to, typename Eight<A>::V v, A inv_scale) {
 #pragma unroll
     for (uint32_t k = 0; k < 8; ++k) {
-        if (k >= count) break;
+        if (k < from || k >= to) continue;
         if (type == MVK_TYPE_BF16) ((__bf16*)p)[i + k] = (__bf16)(float)v[k];
         else if (type == MVK_TYPE_F16) ((_Float16*)p)[i + k] = (_Float16)(float)v[k];
         else if (type == MVK_TYPE_F32) ((float*)p)[i + k] = (float)v[k];
         else ((uint32_t*)p)[i + k] = field_of(v[k] * inv_scale);
     }
+}
+
+// What a thread has of a piece.
+template <typename A>
+__device__ __forceinline__ void store_piece(void* p, int type, size_t row, const Piece& at, typename Eight<A>::V v, A inv_scale) {
+    if (at.skip == 0) store8<A>(p, type, row + at.at, v, inv_scale);
+    else store_some<A>(p, type, row + at.at, at.skip, 8, v, inv_scale);
 }
 
 }  // namespace mvk

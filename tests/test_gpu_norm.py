@@ -414,3 +414,40 @@ def test_gated_refusals():
                 dict(out=x[:1].expand(4, 64)), dict(out_dtype=FIELD, out_scale=-1.0)):
         with pytest.raises(mvk.MvkError):
             mvk.gated_activation(**{"gate": x, "up": x, **bad})
+
+
+@pytest.mark.parametrize("n", [1, 5, 8, 9, 15, 77, 521, 4097, 8191, 16383])
+@pytest.mark.parametrize("x,res", [(BF, BF), (F32, F32), (FIELD, HF)])
+def test_odd_rows_in_place_and_next_to_others(n, x, res):
+    """The threads of a row's last values share some of them: each is read before it is written,
+    and written once, and rows that begin anywhere leave what lies around them."""
+    T = 70
+    for norms in (True, False):  # (without them no barrier lies between the reads and the writes)
+        c = Case(T, n, x=x, res=res, before=norms, after=norms, gate="token")
+        kw = dict(out_dtype=FIELD if x == FIELD else x, out_scale=2.0**-16)
+        y, h = c.call(**kw)
+        kinds = {"x": c.x, "residual": c.res, "gate": c.gate}
+        whole = {k: torch.full((T, n + 3), 5.0).to(t.dtype).cuda() for k, t in kinds.items()}
+        views = {k: b[:, 1:1 + n] for k, b in whole.items()}
+        for k, v in views.items():
+            v.copy_(kinds[k])
+        got = c.call(**views, out=views["x"], residual_out=views["residual"], out_scale=2.0**-16)
+        assert torch.equal(got[0], y) and torch.equal(got[1], h) and torch.equal(views["gate"].cpu(), c.gate)
+        for b in whole.values():
+            assert bool((b[:, :1] == 5).all()) and bool((b[:, 1 + n:] == 5).all())
+
+
+@pytest.mark.parametrize("n", [1, 7, 9, 15, 1001, 11007])
+@pytest.mark.parametrize("dtype", [BF, F32, FIELD])
+def test_gated_odd_rows_in_place(n, dtype):
+    import paper_2609_10264_amd as mvk
+    g, u = _make((70, n), dtype, 1, 3.0).cuda(), _make((70, n), dtype, 2).cuda()
+    kw = dict(field_scale=2.0**-16, out_scale=2.0**-16)
+    want = mvk.gated_activation(g, u, out_dtype=dtype, **kw)
+    for i in (0, 1):
+        both = torch.full((70, 2 * n + 5), 5.0).to(dtype).cuda()
+        parts = both[:, 1:1 + n], both[:, n + 2:2 * n + 2]
+        parts[0].copy_(g), parts[1].copy_(u)
+        out = mvk.gated_activation(*parts, out=parts[i], **kw)
+        assert torch.equal(out, want) and torch.equal(parts[1 - i], (g, u)[1 - i])
+        assert bool((both[:, :1] == 5).all()) and bool((both[:, n + 1] == 5).all()) and bool((both[:, 2 * n + 2:] == 5).all())
