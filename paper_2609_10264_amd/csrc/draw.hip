@@ -17,8 +17,12 @@
 // reaches it, and thresholds and the draw are found there: with top-k, the kth largest
 // maximum is a bound that k logits at least reach (and not many more); with min-p alone, its
 // border; with top-p alone, a histogram of the weights by the first digit of the key, for
-// which the row is read again, says where to cut.  Where the list would not hold them, the
-// digits of the row's keys are searched to the last.
+// which the row is read again, says where to cut.  Where the list would not hold them, digits
+// of the row's keys are searched until it holds those of one bin, and the token is found by
+// sums of the row's parts (1 x 131071 in bfloat16: top-k of 50 13 us, every token 76, top-k of
+// 20000 154).  A row then is one compute unit's work, 60 instructions a weight: bound by
+// their issue, not by memory.  (Bins of values in place of the first digit: a top-p that the
+// list holds 25 -> 38 us at 32000, scattered additions to LDS cost more than equal ones.)
 #include "mvk_internal.h"
 #include "rowio.h"
 
@@ -127,11 +131,12 @@ struct Weights {
     uint32_t top, shift;
     float scale;
 };
+// (of keys above `floor`; the others have none)
 template <typename S>
-__device__ __forceinline__ uint64_t weight(const Weights& a, uint32_t key) {
+__device__ __forceinline__ uint64_t weight(const Weights& a, uint32_t key, uint32_t floor = 0) {
     if (key == a.top) return 1ull << a.shift;
     const double y = (Logit<S>::value(key, a.scale) - a.top_value) * a.c;
-    if (key == 0u || !(y > -47.) || !(y <= 0.)) return 0;  // (-inf below a +inf; 0 inf: none)
+    if (key <= floor || !(y > -47.) || !(y <= 0.)) return 0;  // (-inf below a +inf; 0 inf: none)
     const uint64_t m = __builtin_bit_cast(uint64_t, y + 384.);  // 256 (1 + m 2^-52): steps of 2^-44
     const uint32_t e = ((uint32_t)(m >> 44) & 0xffu) - 128u + a.shift;
     const float g = (float)(uint32_t)(m >> 2) * 0x1.62e43p-43f;  // (the last 34 bits, times ln 2)
@@ -148,6 +153,10 @@ constexpr uint32_t kBins = 2048;  // of a digit: two a thread
 // Largest top-k by way of the maxima: of 4096 groups of values without an order, the
 // kth largest maximum is reached by -4096 ln(1 - k / 4096) values, 1712 here.
 constexpr uint32_t kMaxima = 1400;
+
+// A value that all lanes have (to the compiler too, which then keeps it apart from the lanes' own).
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) { return (uint64_t)uniform((uint32_t)(x >> 32)) << 32 | uniform((uint32_t)x); }
 
 // Sums of a wave's lanes up to and with each: within rows of 16 lanes, then by each row's last.
 template <int kCtrl, int kRows>
@@ -227,11 +236,12 @@ struct Shared {
     double table[kTable];
     uint64_t mass[kBins];
     uint32_t num[kBins];
-    uint32_t key[kList], index[kList], group[kList];
+    uint32_t key[kList], index[kList];
+    uint16_t group[4 * kThreads];
     uint64_t wave_mass[kWaves];
     uint32_t wave_num[kWaves], wave_low[kWaves];
     uint64_t found_above, found_mass;
-    uint32_t found_bin, found_num, low, groups, listed, members;
+    uint32_t found_bin, found_num, found_before, low, groups, listed, members;
     uint64_t member_mass[kMembers];
     uint32_t member_key[kMembers], rank[64];
     uint64_t before[64], start[64];
@@ -244,7 +254,7 @@ struct Sums {
 };
 template <typename N>
 __device__ __forceinline__ Sums<N> group_incl(N (&waves)[kWaves], N x) {
-    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const N mine = wave_incl(x);
     __syncthreads();  // (the sums of the call before have been read)
     if (lane == 63) waves[wave] = mine;
@@ -268,28 +278,34 @@ struct Cut {
 };
 constexpr Cut kAll = {0u, 0u};  // (keys of 0 have no weight)
 
-// One digit of a search: of the bins in sh (bin 0: the largest keys) the one where the sum
+// One round of a search: of the bins in sh (bin 0: the largest keys) the one where the sum
 // of counts, or of weights, from `above` on reaches `need`.
 struct Found {
     bool any;
-    uint32_t bin, num;  // it, and its keys
-    uint64_t above;     // the sum before it
+    uint32_t bin, num;     // it, and its keys
+    uint32_t before;       // keys of the bins before it (if there is none, of all)
+    uint64_t above, mass;  // the sum before it, and the weight of the bins before it (of all)
 };
 __device__ __forceinline__ Found find_bin(Shared& sh, bool by_mass, uint64_t need, uint64_t above) {
     const uint32_t b = 2 * threadIdx.x;
     __syncthreads();  // (the bins are filled)
     const uint32_t n0 = sh.num[b], n1 = sh.num[b + 1];
-    const uint64_t v0 = by_mass ? sh.mass[b] : n0, v1 = by_mass ? sh.mass[b + 1] : n1;
-    const Sums<uint64_t> s = group_incl<uint64_t>(sh.wave_mass, v0 + v1);
-    const uint64_t end = above + s.incl, mid = end - v1, begin = mid - v0;
+    const uint64_t m0 = sh.mass[b], m1 = sh.mass[b + 1];
+    const Scan sc = group_incl(sh, n0 + n1, m0 + m1);
+    const uint64_t v0 = by_mass ? m0 : n0, v1 = by_mass ? m1 : n1;
+    const uint64_t end = above + (by_mass ? sc.mass : sc.num), mid = end - v1, begin = mid - v0;
     if (begin < need && need <= end) {
         const bool second = mid < need;
         sh.found_bin = b + second;
         sh.found_num = second ? n1 : n0;
         sh.found_above = second ? mid : begin;
+        sh.found_before = sc.num - n1 - (second ? 0u : n0);
+        sh.found_mass = sc.mass - m1 - (second ? 0u : m0);
     }
     __syncthreads();
-    return Found{above + s.all >= need, sh.found_bin, sh.found_num, sh.found_above};
+    const bool any = above + (by_mass ? sc.all_mass : sc.all_num) >= need;
+    return Found{any, uniform(sh.found_bin), uniform(sh.found_num), any ? uniform(sh.found_before) : sc.all_num, uniform(sh.found_above),
+                 any ? uniform(sh.found_mass) : sc.all_mass};
 }
 
 // The bin of a value, the largest in the first.  (Of not-a-numbers, which infinities make: the first.)
@@ -306,7 +322,7 @@ __device__ __forceinline__ Found find_count(Shared& sh, uint32_t need) {
     const uint32_t end = s.incl, all = s.all;
     if (end - n0 - n1 < need && need <= end) sh.found_bin = b + (end - n1 < need);
     __syncthreads();
-    return Found{all >= need, sh.found_bin, 0, 0};
+    return Found{all >= need, sh.found_bin};
 }
 
 __device__ __forceinline__ void clear_bins(Shared& sh) {
@@ -392,6 +408,7 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
         __syncthreads();
 #pragma unroll
         for (uint32_t w = 0; w < kWaves; ++w) top = max(top, sh.wave_num[w]), low = min(low, sh.wave_low[w]);
+        top = uniform(top), low = uniform(low);
         if (top == 0u) {  // no logit above -inf
             if (tid == 0) {
                 a.tokens[r] = -1;
@@ -411,21 +428,19 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
             const uint64_t w = part_of(s.p, z, left) + (left ? 1u : 0u);
             return w ? w : 1u;
         };
-        // The list, of the groups whose maximum reaches `from`; false if it does not hold them.
-        auto collect = [&]() {
+        // The list: of the keys from `lo` on, of the groups whose maximum reaches it, or (`every`) of those
+        // in [lo, hi], of all groups; false if it does not hold them.
+        auto collect = [&](uint32_t lo, uint32_t hi, bool every) {
             __syncthreads();
             if (tid == 0) sh.groups = sh.listed = 0;
             __syncthreads();
 #pragma unroll
             for (uint32_t q = 0; q < kAhead; ++q)
-                if (mine[q] >= from) {
-                    const uint32_t to = atomicAdd(&sh.groups, 1u);
-                    if (to < kList) sh.group[to] = q * kThreads + tid;
-                }
+                if (every || mine[q] >= lo) sh.group[atomicAdd(&sh.groups, 1u)] = (uint16_t)(q * kThreads + tid);
             __syncthreads();
-            const uint32_t groups = sh.groups;
-            if (groups > kList) return false;
-            const N least_number = Logit<S>::number_of(from);
+            const uint32_t groups = uniform(sh.groups);
+            if (!every && groups > kList) return false;
+            const N least_number = Logit<S>::number_of(lo), most_number = Logit<S>::number_of(hi);
             const uint32_t items = groups * steps;  // granules (below 2^21)
             constexpr uint32_t kFlight = 4;
 #pragma unroll 1
@@ -447,7 +462,7 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
                     uint32_t hits = 0;
 #pragma unroll
                     for (uint32_t e = 0; e < kVec; ++e)
-                        hits |= Logit<S>::number(x[e]) >= least_number && first + e >= own && first + e < a.n ? 1u << e : 0u;
+                        hits |= Logit<S>::number(x[e]) >= least_number && Logit<S>::number(x[e]) <= most_number && first + e >= own && first + e < a.n ? 1u << e : 0u;
                     if (it + u * kThreads >= items) hits = 0;
                     while (hits) {
                         const uint32_t e = (uint32_t)__ffs((int)hits) - 1;
@@ -459,95 +474,110 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
                 }
             }
             __syncthreads();
-            listed = sh.listed;
+            listed = uniform(sh.listed);
             return listed <= kList;
         };
         // The least prefix of the row with `need` keys or units of weight (`of_whole`: with top-p's part of
-        // the whole): its cut, or false and where the list begins as soon as that can hold it.
+        // the whole): its cut and its weight (`reach`, where top-p asks for it), or false and where the
+        // list begins as soon as that can hold it.
+        // By digits of the keys, of the row until the list holds those of one bin.
+        uint64_t reach = 0;
         auto search_row = [&](bool by_mass, uint64_t need, bool of_whole) {
             uint32_t lo = 1, hi = top, number = 0;  // number: keys above hi
-            uint64_t above = 0;
+            uint64_t above = 0, above_mass = 0;
+            const bool weigh = s.p < 1.;
+            bool in_list = false;
+#pragma unroll 1
             for (;;) {
                 const uint32_t width = width_of(lo, hi);
                 clear_bins(sh);
-                row.each([&](uint32_t key) {
+                auto count = [&](uint32_t key) {
                     if (key < lo || key > hi) return;
                     const uint32_t b = (hi - key) >> width;
                     atomicAdd(&sh.num[b], 1u);
-                    if (by_mass) atomicAdd((unsigned long long*)&sh.mass[b], (unsigned long long)weight<S>(ws, key));
-                }, [](uint32_t) {});
+                    if (weigh) atomicAdd((unsigned long long*)&sh.mass[b], (unsigned long long)weight<S>(ws, key));
+                };
+                if (in_list) {
+#pragma unroll 1
+                    for (uint32_t e = tid; e < listed; e += kThreads) count(sh.key[e]);
+                } else {
+                    row.each(count, [](uint32_t) {});
+                }
                 __syncthreads();
                 if (of_whole) {
                     need_p = need = part_p(group_incl<uint64_t>(sh.wave_mass, sh.mass[tid] + sh.mass[tid + kThreads]).all);
                     of_whole = false;
                 }
                 const Found f = find_bin(sh, by_mass, need, above);
-                const uint32_t past = f.any ? f.bin : kBins - 1;
-                uint32_t c = 0;
-                for (uint32_t b = tid; b <= past; b += kThreads) c += sh.num[b];
-                const uint32_t all = group_incl<uint32_t>(sh.wave_num, c).all;
                 if (f.any) enter_bin(lo, hi, f.bin, width);
-                if (number + all <= kList) {
+                if (number + f.before + (f.any ? f.num : 0u) <= kList) {
                     from = lo;
                     return false;
                 }
+                above_mass += f.mass;
                 if (!f.any) {  // (fewer keys than top-k asks for)
                     cut = kAll;
+                    reach = above_mass;
                     return true;
                 }
-                number += all - f.num;
+                number += f.before;
                 above = f.above;
                 if (width == 0) {
-                    cut = {hi, ties_of(need, above, by_mass ? weight<S>(ws, hi) : 1u, f.num)};
+                    const uint64_t w = weight<S>(ws, hi);
+                    cut = {hi, ties_of(need, above, by_mass ? w : 1u, f.num)};
+                    reach = above_mass + cut.ties * w;
                     return true;
                 }
+                if (!in_list && f.num <= kList) in_list = collect(lo, hi, true);
             }
         };
 
         bool list_k = false, list_p = false, list_m = false;  // which settings are left to the list
-        if (s.k) {
-            if (s.k <= kMaxima) {
-                // The kth largest of the maxima, or a little less: bins by value, of which any
-                // order would do, and the least maximum in those that hold k.  (The bins are zero.)
-                const float high_f = Logit<S>::coarse(top), per = (float)(kBins - 1) / (high_f - Logit<S>::coarse(low));
-                uint32_t b[kAhead];
+        bool begun = false;                                   // `from` is known
+        if (s.k && s.k <= kMaxima) {
+            // The kth largest of the maxima, or a little less: bins by value, of which any
+            // order would do, and the least maximum in those that hold k.  (The bins are zero.)
+            const float high_f = Logit<S>::coarse(top), per = (float)(kBins - 1) / (high_f - Logit<S>::coarse(low));
+            uint32_t b[kAhead];
 #pragma unroll
-                for (uint32_t q = 0; q < kAhead; ++q) {
-                    b[q] = bin_of(high_f, per, Logit<S>::coarse(mine[q]));
-                    if (mine[q]) atomicAdd(&sh.num[b[q]], 1u);
-                }
-                const Found f = find_count(sh, s.k);
-                if (f.any) {
-                    low = 0xffffffffu;
-#pragma unroll
-                    for (uint32_t q = 0; q < kAhead; ++q)
-                        if (mine[q] && b[q] <= f.bin) low = min(low, mine[q]);
-#pragma unroll
-                    for (int d = 32; d >= 1; d >>= 1) low = min(low, (uint32_t)__shfl_xor((int)low, d));
-                    if (lane == 0) atomicMin(&sh.low, low);
-                    __syncthreads();
-                    from = sh.low;
-                }
-                list_k = collect();
+            for (uint32_t q = 0; q < kAhead; ++q) {
+                b[q] = bin_of(high_f, per, Logit<S>::coarse(mine[q]));
+                if (mine[q]) atomicAdd(&sh.num[b[q]], 1u);
             }
-            if (!list_k) {
-                if (!search_row(false, s.k, false)) {
-                    list_k = collect();
-                } else if (s.p < 1.) {
-                    // the weight of what top-k leaves
-                    uint64_t z = 0;
-                    row.each([&](uint32_t key) { z += key > cut.key ? weight<S>(ws, key) : 0u; }, [](uint32_t) {});
-                    need_p = part_p(group_incl<uint64_t>(sh.wave_mass, z).all + (uint64_t)cut.ties * weight<S>(ws, cut.key));
-                    if (!search_row(true, need_p, false)) list_p = collect();
-                }
+            const Found f = find_count(sh, s.k);
+            if (f.any) {
+                uint32_t bound = 0xffffffffu;
+#pragma unroll
+                for (uint32_t q = 0; q < kAhead; ++q)
+                    if (mine[q] && b[q] <= f.bin) bound = min(bound, mine[q]);
+#pragma unroll
+                for (int d = 32; d >= 1; d >>= 1) bound = min(bound, (uint32_t)__shfl_xor((int)bound, d));
+                if (lane == 0) atomicMin(&sh.low, bound);
+                __syncthreads();
+                from = uniform(sh.low);
             }
-            list_p |= list_k && s.p < 1.;
-        } else if (s.p < 1.) {
-            if (!search_row(true, 0, true)) list_p = collect();
-        } else if (least) {
+            begun = true;
+        } else if (!s.k && !(s.p < 1.) && least) {
             // (weights next to the border are looked at again)
-            from = min(top, Logit<S>::key_below(ws.top_value + (log2(s.least) - 0x1p-20) / s.c, a.scale));
-            list_m = collect();
+            from = min(top, Logit<S>::key_below(ws.top_value + ((double)log2f((float)s.least) - 0x1p-16) / s.c, a.scale));
+            begun = true;
+        }
+        bool held = begun && collect(from, top, false);
+        if (held) list_k = s.k != 0, list_p = s.p < 1., list_m = !s.k && !list_p;
+        // Else by the row: top-k, then top-p of what it leaves.
+        if (__builtin_expect(!held && (s.k || s.p < 1.), 0)) {
+            bool by_mass = !s.k;
+#pragma unroll 1
+            for (uint32_t round = 0; round < 2; ++round) {  // (one copy of the code)
+                if (!search_row(by_mass, by_mass ? need_p : (uint64_t)s.k, !s.k)) {
+                    collect(from, top, false);  // (which holds them)
+                    list_k = !by_mass, list_p = s.p < 1.;
+                    break;
+                }
+                if (by_mass || !(s.p < 1.)) break;
+                need_p = part_p(reach);
+                by_mass = true;
+            }
         }
 
         uint64_t z = 0, want = 0;
@@ -561,7 +591,7 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
             if (a.probs) a.probs[r] = (float)((double)w / (double)z);
         };
 
-        if (list_k || list_p || list_m) {
+        if (__builtin_expect(list_k || list_p || list_m, 1)) {
             if (listed <= 64) {
                 // An entry a lane, in every wave: order, thresholds and draw by comparison with four of
                 // them a wave.
@@ -785,55 +815,61 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
             continue;
         }
 
-        uint32_t first = 0;  // value that the passes begin with
-        uint64_t first_sum = 0;
-        int first_pass = 0;
-        if (cut.key == 0u) {
-            // The whole row: the sums of its parts, two blocks each (2048 parts at most), then the part that
-            // the token is in.
-            clear_bins(sh);
+        // By the row: the sums of its parts, two blocks each (2048 parts at most), without and with the
+        // first ties, then the part that the token is in.
+        clear_bins(sh);
+        const uint64_t tie_w = cut.key ? weight<S>(ws, cut.key) : 0u, tie = tie_w < least ? 0u : tie_w;
+        {
             uint64_t own = 0;
+            uint32_t same = 0;
+            const uint32_t tie_key = cut.key ? cut.key : 0xffffffffu;
+            Weights over = ws;
+            if (cut.key == top) over.top = 0xffffffffu;  // (no key: the ties are counted)
             row.each([&](uint32_t key) {
-                const uint64_t w = weight<S>(ws, key);
+                const uint64_t w = weight<S>(over, key, cut.key);
                 own += w < least ? 0u : w;
+                same += key == tie_key ? 1u : 0u;
             }, [&](uint32_t block) {
                 const uint64_t of_wave = wave_incl(own);
                 if (lane == 63) atomicAdd((unsigned long long*)&sh.mass[block / 2], (unsigned long long)of_wave);
                 own = 0;
+                if (cut.key) {
+                    const uint32_t ties = wave_incl(same);
+                    if (lane == 63) atomicAdd(&sh.num[block / 2], ties);
+                    same = 0;
+                }
             });
-            __syncthreads();
-            const uint64_t m0 = sh.mass[2 * tid], m1 = sh.mass[2 * tid + 1];
-            const Sums<uint64_t> sc = group_incl<uint64_t>(sh.wave_mass, m0 + m1);
-            draw_of(sc.all);
-            if (sc.incl - m0 - m1 <= want && want < sc.incl) {
-                const bool second = sc.incl - m1 <= want;
-                sh.found_bin = 2 * tid + second;
-                sh.found_above = second ? sc.incl - m1 : sc.incl - m1 - m0;
-            }
-            __syncthreads();
-            first = sh.found_bin * 2 * Row::kBlock, first_sum = sh.found_above, first_pass = 1;
         }
-        // The kept weights in the order of the vocabulary: their total, then the token.
+        __syncthreads();
+        const uint32_t n0 = sh.num[2 * tid], n1 = sh.num[2 * tid + 1];
+        const uint32_t tied = group_incl<uint32_t>(sh.wave_num, n0 + n1).incl;  // up to and with this thread's parts
+        auto kept_of = [&](uint32_t before, uint32_t num) { return (uint64_t)min(num, cut.ties - min(cut.ties, before)) * tie; };
+        const uint64_t m0 = sh.mass[2 * tid] + kept_of(tied - n0 - n1, n0), m1 = sh.mass[2 * tid + 1] + kept_of(tied - n1, n1);
+        const Sums<uint64_t> sc = group_incl<uint64_t>(sh.wave_mass, m0 + m1);
+        draw_of(sc.all);
+        if (sc.incl - m0 - m1 <= want && want < sc.incl) {
+            const bool second = sc.incl - m1 <= want;
+            sh.found_bin = 2 * tid + second;
+            sh.found_above = second ? sc.incl - m1 : sc.incl - m1 - m0;
+            sh.found_num = second ? tied - n1 : tied - n1 - n0;
+        }
+        __syncthreads();
+        uint32_t seen = sh.found_num;  // ties before
+        uint64_t sum = sh.found_above;
 #pragma unroll 1
-        for (int pass = first_pass; pass < 2; ++pass) {
-            uint32_t seen = 0;  // ties before
-            uint64_t sum = first_sum;
-#pragma unroll 1
-            for (uint32_t i0 = first; i0 < a.n; i0 += kThreads) {
-                const uint32_t i = i0 + tid;
-                const N f = i < a.n ? Logit<S>::number(row.x[i]) : Logit<S>::least();
-                const uint32_t key = f == Logit<S>::least() ? 0u : Logit<S>::key(f), tie = key == cut.key && key ? 1u : 0u;
-                const uint64_t w = key >= cut.key ? weight<S>(ws, key) : 0u;
-                const Sums<uint32_t> t = group_incl<uint32_t>(sh.wave_num, tie);
-                const bool keep = w >= least && (key > cut.key || (tie && seen + t.incl - 1 < cut.ties));
-                seen += t.all;
-                const Sums<uint64_t> m = group_incl<uint64_t>(sh.wave_mass, keep ? w : 0u);
-                const uint64_t end = sum + m.incl;
-                sum += m.all;
-                if (pass == 1 && keep && end - w <= want && want < end) put(i, w);
-                if (pass == 1 && sum > want) break;  // (for all alike)
-            }
-            if (pass == 0) draw_of(sum);
+        for (uint32_t i0 = sh.found_bin * 2 * Row::kBlock; i0 < a.n; i0 += kThreads) {
+            const uint32_t i = i0 + tid;
+            const N f = i < a.n ? Logit<S>::number(row.x[i]) : Logit<S>::least();
+            const uint32_t key = f == Logit<S>::least() ? 0u : Logit<S>::key(f), equal = key == cut.key && key ? 1u : 0u;
+            const uint64_t w = key >= cut.key ? weight<S>(ws, key) : 0u;
+            const Sums<uint32_t> t = group_incl<uint32_t>(sh.wave_num, equal);
+            const bool keep = w >= least && (key > cut.key || (equal && seen + t.incl - 1 < cut.ties));
+            seen += t.all;
+            const Sums<uint64_t> m = group_incl<uint64_t>(sh.wave_mass, keep ? w : 0u);
+            const uint64_t end = sum + m.incl;
+            sum += m.all;
+            if (keep && end - w <= want && want < end) put(i, w);
+            if (sum > want) break;  // (for all alike)
         }
     }
 }

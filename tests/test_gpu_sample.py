@@ -288,3 +288,22 @@ def test_refusals():
                 dict(probs=x[0, :4]), dict(logits=x[:, :0])):
         with pytest.raises(mvk.MvkError):
             mvk.sample(**{"logits": x, "u": u, **bad})
+
+
+@pytest.mark.parametrize("dtype", [BF, F32, FIELD])
+@pytest.mark.parametrize("spread", [0.02, 2.2, 60.0])
+def test_prefixes_that_no_list_holds(dtype, spread):
+    """By bins of values, then by digits: narrow and wide rows, and one whose values lie far below its
+    first few."""
+    n = 40000
+    x = torch.randn((4, n), generator=torch.Generator().manual_seed(3), dtype=torch.float64) * spread
+    x[1] -= 9 * spread
+    x[1, 100:103] = 9 * spread
+    x[2] = x[2].sign() * 3.0 * spread  # two values
+    x[3, ::2] = x[3, 1]
+    x = ref.embed((x * 2**16).round().long()) if dtype == FIELD else x.to(dtype)
+    u = torch.tensor([0.0, 0.3, 0.9, 0.999])
+    for how in (dict(top_p=0.7, t=spread), dict(k=9000, t=spread), dict(k=25000, top_p=0.5, t=3 * spread),
+                dict(k=9000, least=0.3, t=spread), dict(k=9000, top_p=0.99, t=1e6), dict(top_p=0.999, t=0.01 * spread)):
+        _check(x, u, **how)
+        _check(x.flip(0), u, **how)
