@@ -55,6 +55,17 @@
 // rows 46.9 / 30.9; 32 over 8000, 96 rows 566 / 244.  From 33 to 64 rows long contexts
 // would gain a fifth by the tokens form and short ones lose half; their lengths are
 // on the device, so the bound is where no context loses.
+//
+// Caches held in 8 bits (a code times a power of two of its row, exact in bfloat16)
+// are widened on the way to the same products.  Tokens form: a lane has a key and half
+// of its dims, 16 codes a load, and widens them in the operands' registers; V goes by
+// way of registers to LDS.  Chunks form: it has no registers for that while it
+// computes, so the codes go straight to LDS and each wave widens its own part of a tile
+// in place at the end of a step.  Measured: the 48 sequences above 161 us in E4M3 (227
+// in bfloat16; 118 are its bytes), a chunk of 512 over 16000 entries with 64 + 8 heads
+// 364 us (304 in bfloat16): the widening, two conversions and an LDS pass a value, is
+// paid once a workgroup and tile and adds to steps that the products already fill.  I8
+// takes 10 to 18 % longer than E4M3, which one instruction converts by pairs.
 #include "kv.h"
 #include "mvk_internal.h"
 #include "quant.h"
@@ -1148,8 +1159,10 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
 // over the same entries, and their sums are added in order: a tile is a chain of load,
 // products and weights, and one group's fill another's gaps.
 // Measured: single tokens of 8 sequences over 4096 to 12000 entries, 32 + 8 heads of
-// 128, 35 us (3.5 TB/s of K); a chunk of 256 over 6000, 46 us, 280 TFLOP/s: 392
-// workgroups, so some compute units have two and others one.
+// 128, 35 us (3.5 TB/s of K); 21 mixed sequences of up to 701 new tokens over up to
+// 5003 entries (28 + 4 heads of 80, I8) 263 us of the whole call with one group and
+// 164 with four; a chunk of 256 over 6000 in bfloat16 115 and 109.  (A step of 32 rows
+// with one group is its chain's latency: deeper rings of loads did not help.)
 constexpr uint32_t kWeightKeys = 128;
 template <typename T, typename C, uint32_t kDim, uint32_t kGroups>
 __global__ __launch_bounds__(256 * kGroups) void weights_tile(TileArgs a, const float* __restrict__ lse, const float* w_in,
