@@ -322,6 +322,7 @@ struct NormArgs;
 struct GatedArgs;
 struct DrawArgs;
 hipError_t launch_block_norm(const NormArgs& a, hipStream_t s);
+hipError_t launch_block_norm_ragged(const NormArgs& a, hipStream_t s);
 hipError_t launch_gated(const GatedArgs& a, hipStream_t s);
 hipError_t launch_draw(const DrawArgs& a, hipStream_t s);
 
