@@ -23,6 +23,7 @@ passes pointers, strides and the stream.
 from __future__ import annotations
 
 import ctypes
+from contextlib import nullcontext
 from dataclasses import dataclass
 
 import torch
@@ -223,7 +224,9 @@ def cache_read(cache: KVCache, seqs: Sequences, tokens: int | None = None, dtype
     if k_out is None and v_out is None:
         if tokens is None:
             raise ValueError("tokens is needed where neither k_out nor v_out is given")
-        k_out, v_out = (torch.zeros((tokens, cs.kv_heads, cs.dim), dtype=dtype, device=cache.K.device) for _ in range(2))
+        k_out, v_out = (torch.empty((tokens, cs.kv_heads, cs.dim), dtype=dtype, device=cache.K.device) for _ in range(2))
+        with torch.cuda.stream(stream) if stream is not None else nullcontext():  # (where the rows are written)
+            k_out.zero_(), v_out.zero_()
     T = (k_out if k_out is not None else v_out).shape[0]
     if tokens is not None and tokens != T:
         raise ValueError(f"the rows have {T} tokens, not {tokens}")
