@@ -807,7 +807,10 @@ mvk_status mvk_rotary_append(const mvk_rows *q, const mvk_rows *k, const mvk_row
  * that mvk_rotary_append writes for token t (rows of tokens without one, or whose page
  * is outside the pool, are left alone), rounded once to the rows' type.
  *   k, v           : T x cache->kv_heads x cache->dim, BF16, F16 or F32; either may
- *                    be NULL; they share no memory with each other or the cache.
+ *                    be NULL; they share no memory with each other or the cache
+ *                    (MVK_EINVAL where rows meet each other, a page's entries of a head
+ *                    or their exponents; with another token than page stride, where
+ *                    their extents do).
  * Errors: MVK_EINVAL, MVK_ERANGE (as mvk_rotary_append).
  */
 mvk_status mvk_cache_read(const mvk_kv *cache, const mvk_seqs *seqs, uint32_t T, const mvk_rows *k,

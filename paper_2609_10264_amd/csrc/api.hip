@@ -1273,6 +1273,22 @@ mvk_status check_kv(const mvk_kv* kv) {
     return MVK_OK;
 }
 
+// Do rows lie in the memory of a cache?  (The entries of a page and head count as one row.)
+bool in_pools(const RowSet& rows, const mvk_kv* kv) {
+    auto meets = [&](const void* p, uint64_t page, uint64_t head, uint64_t entry, uint64_t elem, uint64_t dim) {
+        return share_memory(rows, {p, kv->pages, elem * page, kv->kv_heads, elem * head,
+                                   elem * ((kv->page_size - 1) * entry + dim)});
+    };
+    const uint64_t e = type_size(kv->type);
+    if (meets(kv->K, kv->k_page, kv->k_head, kv->k_entry, e, kv->dim) ||
+        meets(kv->V, kv->v_page, kv->v_head, kv->v_entry, e, kv->dim))
+        return true;
+    if (!in_8_bits(kv)) return false;
+    const mvk_kv8* x = (const mvk_kv8*)kv;
+    return meets(x->k_exp, x->kx_page, x->kx_head, x->kx_entry, 1, 1) ||
+           meets(x->v_exp, x->vx_page, x->vx_head, x->vx_entry, 1, 1);
+}
+
 // rows: the call has token rows, so q_start is read.
 mvk_status check_seqs(const mvk_seqs* sq, const mvk_kv* kv, bool rows) {
     if (!sq || !sq->count || !sq->width || !sq->table || !sq->lens || (rows && !sq->q_start)) return MVK_EINVAL;
@@ -1388,6 +1404,9 @@ mvk_status mvk_cache_read(const mvk_kv* cache, const mvk_seqs* seqs, uint32_t T,
     }
     if (k && v && share_memory(row_set(k, T, cache->kv_heads, cache->dim), row_set(v, T, cache->kv_heads, cache->dim)))
         return MVK_EINVAL;
+    // entries are read while rows are written
+    for (const mvk_rows* r : {k, v})
+        if (r && in_pools(row_set(r, T, cache->kv_heads, cache->dim), cache)) return MVK_EINVAL;
     if (T == 0) return MVK_OK;
     Rows rk = {}, rv = {};
     if (k) rk = view_of(k);
