@@ -1155,13 +1155,13 @@ __global__ __launch_bounds__(256, kDim > 128 ? 1 : 2) void attend_tile(TileArgs 
 // p = exp(scale S - lse).  K is read once and stays in registers; the rows pass
 // through LDS 32 at a time, one tile in flight, for the four waves together.
 // A launch of its own, since a weight needs its row's whole sum; without atomics.
-// With many rows a sequence kGroups groups of four waves take the tiles of rows in turn,
-// over the same entries, and their sums are added in order: a tile is a chain of load,
+// Where chains of tiles are long (in_groups) kGroups groups of four waves take the tiles of rows
+// in turn, over the same entries, and their sums are added in order: a tile is a chain of load,
 // products and weights, and one group's fill another's gaps.
 // Measured: single tokens of 8 sequences over 4096 to 12000 entries, 32 + 8 heads of
 // 128, 35 us (3.5 TB/s of K); 21 mixed sequences of up to 701 new tokens over up to
-// 5003 entries (28 + 4 heads of 80, I8) 263 us of the whole call with one group and
-// 164 with four; a chunk of 256 over 6000 in bfloat16 115 and 109.  (A step of 32 rows
+// 5003 entries (28 + 4 heads of 80, I8) 261 us of the whole call with one group and
+// 143 with four; a chunk of 256 over 6000 in bfloat16 116 and 109.  (A step of 32 rows
 // with one group is its chain's latency: deeper rings of loads did not help.)
 constexpr uint32_t kWeightKeys = 128;
 template <typename T, typename C, uint32_t kDim, uint32_t kGroups>
@@ -1360,15 +1360,38 @@ TileArgs tile_args(const Rows& q, uint32_t tokens, uint32_t heads, const KvView&
 
 }  // namespace
 
+// Are the collected weights taken by several groups of waves a workgroup?  (blocks: of kWeightKeys
+// entries that a table's row holds.)  Groups shorten a chain of tiles.  But a workgroup of them fills
+// a compute unit where three of one group fit, so sequences of few rows lose, and one that finds no
+// entries costs four times as much.
+// Up to 128 dims: groups where the longest chain, about 1 us a tile, takes longer than all tiles
+// do on 256 compute units, three at a time, and sequences have rows enough, 192 on average.  The
+// whole call by one group and by four, us, 128 dims: 21 mixed sequences of up to 701 new tokens
+// (28 + 4 heads) 260 and 139, a chunk of 1000 beside 20 of 32 247 and 193, a prompt of 2048 380 and
+// 189, four of them 505 and 415; but 48 single tokens 147 and 338, 47 beside a chunk of 256 220 and
+// 415, 48 sequences of 32 new 259 and 390 (312 and 786 with a table 32 times as wide), 16 of 256 574
+// and 603 (64 dims: 328 and 403).
+// Above: one group's 96 KB of LDS leave room for one workgroup, two groups' 64 KB for two.  By one
+// and by two, 256 dims: 48 of 32 new 753 and 645, 16 of 256 1695 and 1347; but 48 single tokens 439
+// and 477, 47 beside a chunk 615 and 632, and with a table 32 times as wide 48 of 32 840 and 855, 21
+// of up to 200 new 262 and 277.
+static bool in_groups(uint64_t tokens, uint64_t grp, uint64_t kv_heads, uint64_t count, uint64_t blocks, uint64_t max_new, uint32_t dim) {
+    const double rows = (double)(tokens * grp), launch = (double)(count * kv_heads) * (double)blocks;
+    if (dim > 128) return rows >= 96. * (double)count && launch <= 14. * rows;
+    // (a bound that is all tokens of several sequences says nothing about one: spread evenly)
+    const double most = (double)(count > 1 && max_new >= tokens ? tokens / count : max_new < tokens ? max_new : tokens);
+    const double tiles = (rows / 32. + (double)count) * (double)kv_heads * (double)blocks;
+    return rows >= 192. * (double)count && most * (double)grp / 32. > tiles / 768.;
+}
+
 hipError_t launch_weights_tile(const Rows& q, uint32_t tokens, uint32_t heads, const KvView& kv, const SeqView& sq,
                                float scale, const float* lse, const float* w_in, float* w_out, size_t w_seq,
                                size_t w_head, uint32_t max_new, hipStream_t s) {
     const TileArgs a = tile_args(q, tokens, heads, kv, sq, scale);
     const uint64_t cap = (uint64_t)sq.width << kv.shift;
     const dim3 grid((uint32_t)((cap + kWeightKeys - 1) / kWeightKeys), kv.heads, sq.count);
-    // four tiles of rows and more in a sequence, as far as the caller knows: groups (one launch takes
-    // fewer than 2^32 threads)
-    const bool many = (uint64_t)max_new * (heads / kv.heads) > 96 && cap < (1u << 28);
+    // (one launch takes fewer than 2^32 threads)
+    const bool many = cap < (1u << 28) && in_groups(tokens, heads / kv.heads, kv.heads, sq.count, grid.x, max_new, kv.dim);
     auto go = [&](auto one, auto several, uint32_t groups) {
         hipLaunchKernelGGL(many ? several : one, grid, dim3(many ? 256 * groups : 256), 0, s, a, lse, w_in, w_out, w_seq, w_head);
         return hipGetLastError();
