@@ -917,10 +917,11 @@ mvk_status mvk_block_norm(const mvk_rows *x, float x_scale, const mvk_rows *resi
 #define MVK_ACT_RELU 3      /* max(g, 0) */
 
 /*
- * out = act(gate) * up, value by value, in 32 bits.
+ * out = act(gate) * up, value by value, in 32 bits (FIELD inputs count with 24 bits).
  *   gate, up : T x n, one type, floats or FIELD times in_scale
- *   out      : floats, or FIELD (over out_scale, rounded to nearest and clamped); may be
- *              gate or up itself (same type and stride), else shares no memory with them
+ *   out      : floats, or FIELD (the 32-bit value over out_scale, any positive number, rounded
+ *              to nearest and clamped); may be gate or up itself (same type and stride), else
+ *              shares no memory with them
  * Errors: MVK_EINVAL, MVK_ERANGE (T or n above 2^31 - 1, buffers above 2^62 bytes).
  */
 mvk_status mvk_gated_activation(const mvk_rows *gate, const mvk_rows *up, uint32_t T, uint32_t n, int32_t act,

@@ -1584,8 +1584,7 @@ mvk_status mvk_gated_activation(const mvk_rows* gate, const mvk_rows* up, uint32
     // (a value is read before its place is written, by the same thread)
     if (meet(out, gate, T, n, true) || meet(out, up, T, n, true)) return MVK_EINVAL;
     if (T == 0) return MVK_OK;
-    const GatedArgs a = {matrix_of(gate), matrix_of(up), matrix_of(out), T, n, act, in_scale,
-                         out->type == MVK_TYPE_FIELD ? 1.f / out_scale : 1.f};
+    const GatedArgs a = {matrix_of(gate), matrix_of(up), matrix_of(out), T, n, act, in_scale, out_scale};
     return hip_status(launch_gated(a, (hipStream_t)stream));
 }
 

@@ -35,7 +35,7 @@ struct GatedArgs {
     Matrix gate, up, out;
     uint32_t T, n;
     int act;
-    float in_scale, inv_scale;
+    float in_scale, out_scale;
 };
 struct DrawArgs {
     Matrix x;
