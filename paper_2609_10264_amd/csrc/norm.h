@@ -10,8 +10,7 @@
 // in bfloat16, both norms and a gate: 120 us, 4.5 TB/s; 8 rows of 4096 9.3 us, 5.6 of kernel; 4096 rows of 8190
 // in bfloat16, both norms: 66 us, 60.5 of 8192; value by value 292).
 // Values and sums are in 32 bits, in 64 with a FIELD output: its whole numbers are
-// chosen next to borders and reach 2^30, beyond what 32 bits hold.  (There h in a 16-bit
-// residual_out is rounded by way of 32 bits: 2^-16 of a step more at most in bfloat16.)
+// chosen next to borders and reach 2^30, beyond what 32 bits hold.
 #pragma once
 #include "mvk_internal.h"
 #include "rowio.h"

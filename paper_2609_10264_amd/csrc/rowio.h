@@ -143,19 +143,20 @@ __device__ __forceinline__ uint32_t field_of(double x) {
     return i < 0 ? kP + (uint32_t)i : (uint32_t)i;
 }
 
+// (64 bits to 16 in one rounding, not by way of 32)
 template <typename A>
 __device__ __forceinline__ void store8(void* p, int type, size_t i, typename Eight<A>::V v, A inv_scale) {
     if (type == MVK_TYPE_BF16) {
         typedef __bf16 B8 __attribute__((ext_vector_type(8)));
         B8 x;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = (__bf16)(float)v[k];
+        for (int k = 0; k < 8; ++k) x[k] = (__bf16)v[k];
         *(u32x4_at2*)((uint16_t*)p + i) = __builtin_bit_cast(u32x4_, x);
     } else if (type == MVK_TYPE_F16) {
         typedef _Float16 H8 __attribute__((ext_vector_type(8)));
         H8 x;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = (_Float16)(float)v[k];
+        for (int k = 0; k < 8; ++k) x[k] = (_Float16)v[k];
         *(u32x4_at2*)((uint16_t*)p + i) = __builtin_bit_cast(u32x4_, x);
     } else {
         const bool field = type == MVK_TYPE_FIELD;
@@ -176,8 +177,8 @@ __device__ __forceinline__ void store_some(void* p, int type, size_t i, uint32_t
 #pragma unroll
     for (uint32_t k = 0; k < 8; ++k) {
         if (k < from || k >= to) continue;
-        if (type == MVK_TYPE_BF16) ((__bf16*)p)[i + k] = (__bf16)(float)v[k];
-        else if (type == MVK_TYPE_F16) ((_Float16*)p)[i + k] = (_Float16)(float)v[k];
+        if (type == MVK_TYPE_BF16) ((__bf16*)p)[i + k] = (__bf16)v[k];
+        else if (type == MVK_TYPE_F16) ((_Float16*)p)[i + k] = (_Float16)v[k];
         else if (type == MVK_TYPE_F32) ((float*)p)[i + k] = (float)v[k];
         else ((uint32_t*)p)[i + k] = field_of(v[k] * inv_scale);
     }
