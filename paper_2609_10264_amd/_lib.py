@@ -225,6 +225,12 @@ class MvkSampling(ctypes.Structure):
     ]
 
 
+def count(n: int) -> int:
+    """A number of rows or values as the library takes it, in 32 bits: ctypes would pass the last
+    32 of more, and no call takes 2^32 - 1, so this is refused (MVK_ERANGE)."""
+    return n if n < 1 << 32 else (1 << 32) - 1
+
+
 class MvkError(RuntimeError):
     def __init__(self, fn: str, status: int, msg: str):
         super().__init__(f"{fn} failed: {msg} (status {status})")

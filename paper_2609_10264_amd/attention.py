@@ -142,7 +142,7 @@ class Sequences:
         lens = _dev(self.lens, torch.int32, (count,), "lens")
         starts = _dev(starts, torch.int32, (count + 1,), "q_start") if starts is not None else None
         most = rows if self.max_new is None or self.max_new > rows else int(self.max_new)
-        return _lib.MvkSeqs(table.data_ptr(), stride, count, width, lens, starts, most)
+        return _lib.MvkSeqs(table.data_ptr(), stride, count, width, lens, starts, _lib.count(most))
 
 
 def rotary_table(rot: int, rows: int, base: float = 10000.0, scaling: str | None = None, factor: float = 1.0,
@@ -183,7 +183,7 @@ def _rotary_call(q, k, v, positions, table, cache, seqs, layout, field_scale, ou
         field_scale = 0.0
     rows, rot = table.shape
     _lib.check("mvk_rotary_append", _lib.load(p).mvk_rotary_append(
-        qs, ks, vs, T, heads, dim, rot, _LAYOUTS[layout], _dev(positions, torch.int32, (T,), "positions"),
+        qs, ks, vs, _lib.count(T), heads, dim, rot, _LAYOUTS[layout], _dev(positions, torch.int32, (T,), "positions"),
         _dev(table, torch.float32, None, "table"), rows, field_scale, os_, cs, ss, _stream(stream)))
 
 
@@ -234,7 +234,8 @@ def cache_read(cache: KVCache, seqs: Sequences, tokens: int | None = None, dtype
     hk, dim = cs.kv_heads, cs.dim
     ks = ref(_rows(k_out, "k_out", T, hk, dim)) if k_out is not None else None
     vs = ref(_rows(v_out, "v_out", T, hk, dim)) if v_out is not None else None
-    _lib.check("mvk_cache_read", _lib.load(p).mvk_cache_read(ref(cs), ref(seqs.struct(T)), T, ks, vs, _stream(stream)))
+    _lib.check("mvk_cache_read", _lib.load(p).mvk_cache_read(ref(cs), ref(seqs.struct(T)), _lib.count(T), ks, vs,
+                                                             _stream(stream)))
     return k_out, v_out
 
 
@@ -268,7 +269,8 @@ def paged_attention(q: torch.Tensor, cache: KVCache, seqs: Sequences, scale: flo
                 raise ValueError("weights and weights_out must have the same strides")
     ref = ctypes.byref
     _lib.check("mvk_paged_attention", _lib.load(p).mvk_paged_attention(
-        ref(qs), T, heads, ref(cs), ref(ss), dim**-0.5 if scale is None else scale, ref(os_), field_scale or 0.0,
+        ref(qs), _lib.count(T), heads, ref(cs), ref(ss), dim**-0.5 if scale is None else scale, ref(os_),
+        field_scale or 0.0,
         _dev(lse, torch.float32, (T, heads), "lse") if lse is not None else None, w_in, w_out, w_seq, w_head,
         _stream(stream)))
     return out

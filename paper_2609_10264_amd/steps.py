@@ -147,7 +147,8 @@ def block_norm(x: torch.Tensor | None, residual: torch.Tensor | None = None, bef
             gs = _matrix(gate, "gate", shape, device)
     _lib.check("mvk_block_norm", _lib.load(p).mvk_block_norm(
         ref(xs) if xs is not None else None, _scale_of(xs.type, field_scale, "field_scale") if xs is not None else 0.0,
-        ref(rs) if rs is not None else None, T, n, ref(after.struct(n, device)) if after is not None else None,
+        ref(rs) if rs is not None else None, _lib.count(T), _lib.count(n),
+        ref(after.struct(n, device)) if after is not None else None,
         ref(gs) if gs is not None else None, scale, ref(ho), ref(before.struct(n, device)) if before is not None else None,
         ref(os_) if os_ is not None else None,
         _scale_of(os_.type, out_scale, "out_scale") if os_ is not None else 0.0, raw))
@@ -175,8 +176,8 @@ def gated_activation(gate: torch.Tensor, up: torch.Tensor, act: str = "silu", fi
     os_ = _matrix(out, "out", shape, device)
     ref = ctypes.byref
     _lib.check("mvk_gated_activation", _lib.load(p).mvk_gated_activation(
-        ref(gs), ref(us), T, n, _ACTS[act], _scale_of(gs.type, field_scale, "field_scale"), ref(os_),
-        _scale_of(os_.type, out_scale, "out_scale"), raw))
+        ref(gs), ref(us), _lib.count(T), _lib.count(n), _ACTS[act], _scale_of(gs.type, field_scale, "field_scale"),
+        ref(os_), _scale_of(os_.type, out_scale, "out_scale"), raw))
     return out
 
 
@@ -217,6 +218,6 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_
                                            _each(top_p, "top_p", f32, R, device), _each(min_p, "min_p", f32, R, device))
     how = _lib.MvkSampling(t, pp, m, max(min(k, 2**31 - 1), 0), ts, ps, ms, ks)
     _lib.check("mvk_sample_tokens", _lib.load(p).mvk_sample_tokens(
-        ctypes.byref(rows), R, n, _scale_of(rows.type, field_scale, "field_scale"), ctypes.byref(how), *at,
-        raw))
+        ctypes.byref(rows), _lib.count(R), _lib.count(n), _scale_of(rows.type, field_scale, "field_scale"),
+        ctypes.byref(how), *at, raw))
     return out
