@@ -678,8 +678,9 @@ mvk_status mvk_decode_verify_seeded(const mvk_key *key, const mvk_st *st, const 
  * fixed-point numbers: the centred residue (p - x stands for -x) times a scale.
  * Unlike the rest of this library these calls round; sums, softmax statistics
  * and angles are held in 32 bits or more, every output is rounded once.  The
- * softmax's weights are rounded to a 16-bit cache's type before the product with
- * the values (mvk_paged_attention), whatever the output's type is.
+ * softmax's weights are rounded to a 16-bit cache's type, or to BF16 for a cache
+ * held in 8 bits, before the product with the values (mvk_paged_attention),
+ * whatever the output's type is.
  */
 #define MVK_TYPE_BF16 0
 #define MVK_TYPE_F16 1
@@ -717,10 +718,11 @@ typedef struct mvk_kv {
  * What a row x (the dim values of an entry and head) is held as: the exponent is
  * the least in [MVK_EXP_LEAST, MVK_EXP_MOST] with max |x_d| <= M 2^exponent over
  * the finite x_d (M = 448 for E4M3, 127 for I8), and the codes are the nearest to
- * x_d / 2^exponent (ties to even; clamped to M).  The rotation before it is in
- * 64 bits, so the codes are the nearest of the exact values.  An infinity or a not-a-number
- * becomes a not-a-number: that value in E4M3, the row in I8, whose exponent then
- * is MVK_EXP_NAN.  Every other value is exact in bfloat16, the type that
+ * x_d / 2^exponent (ties to even; clamped to M).  Field elements are scaled and keys
+ * rotated in 64 bits before it: x_d is within 2^-51 of the exact value (of its pair's
+ * length, where it is rotated), and a code next to a border is chosen by that.  An
+ * infinity or a not-a-number becomes a not-a-number: that value in E4M3, the row in
+ * I8, whose exponent then is MVK_EXP_NAN.  Every other value is exact in bfloat16, the type that
  * attention over such a cache computes in: queries are BF16.  Exponents outside
  * the range give unspecified values.
  */
@@ -957,7 +959,9 @@ typedef struct mvk_sampling {
  *   probs  : NULL, or device, R floats: the token's share of the kept weights
  * A not-a-number counts as -inf, which is never drawn; logits of +inf share all
  * the weight.  Weights are whole multiples of 2^-44 (n up to 2^17; one bit less for
- * every doubling of n), so sums are exact and have no order.
+ * every doubling of n), so sums are exact and have no order; each is within 2^-33 of its
+ * size and half a multiple of the exponential.  The three thresholds and u are compared
+ * with these: what is closer to a border than that falls to one side, always the same.
  * Errors: MVK_EINVAL (null, n zero, outputs in each other's or the inputs' memory,
  * field_scale not finite and positive), MVK_ERANGE (R or n above 2^24, buffers
  * above 2^62 bytes).

@@ -5,8 +5,8 @@
 //   codes = nearest(x / 2^e)
 //
 // Queries are rotated in 32 bits, as with other caches.  Keys are rotated in 64: a
-// code is chosen next to borders, and what is written then is the nearest code of the
-// exact value whatever the order of operations.
+// code is chosen next to borders, and 64 bits are within 2^-51 of the pair's length of the
+// exact value, so that nearly every code is its nearest.
 //
 // Bound by memory where calls are large: each value is read once and written once.  A
 // row's exponent is a maximum over the 4 to 32 neighbouring lanes that hold the row, so

@@ -10,7 +10,8 @@
 // weights (top-p).  The token is found by a prefix sum in the order of the vocabulary.
 //
 // Weights are held as whole multiples of 2^-shift, so that every sum is exact, atomics
-// included, and no order of additions decides a token at a border.
+// included, and no order of additions decides a token at a border.  (That is their sums: a
+// weight itself is within 2^-33 of its exponential, see `weight`.)
 //
 // A workgroup takes a row.  It is read once for the maxima of 4096 groups of its values,
 // four a thread.  What is near the top goes to a list in LDS, from the groups whose maximum
@@ -108,7 +109,8 @@ __device__ __forceinline__ uint64_t part_of(double f, uint64_t z, bool& left) {
 
 // Weights of a row's keys in units of 2^-shift.  y = (x - top) log2(e) / temperature is
 // rounded to 2^-44; its first 10 bits after the point are looked up, the other 34 go
-// into a cubic in 32 bits, which below 2^-10 loses 2^-33 of the weight at most.
+// into a cubic in 32 bits, which below 2^-10 loses 2^-33 of the weight at most (every token of one
+// row of 131071: 76 us, 92 by exp2 in 64 bits; 64 rows with top-p of 0.9 206 and 248).
 constexpr uint32_t kTable = 1024;
 struct Powers {
     double p[kTable];  // 2^(j / kTable)
@@ -441,7 +443,7 @@ __global__ __launch_bounds__(kThreads) void draw_row(DrawArgs a, uint32_t shift)
             const uint32_t groups = uniform(sh.groups);
             if (!every && groups > kList) return false;
             const N least_number = Logit<S>::number_of(lo), most_number = Logit<S>::number_of(hi);
-            const uint32_t items = groups * steps;  // granules (below 2^21)
+            const uint32_t items = groups * steps;  // granules (2^22 at most)
             constexpr uint32_t kFlight = 4;
 #pragma unroll 1
             for (uint32_t it = tid; it < items; it += kFlight * kThreads) {

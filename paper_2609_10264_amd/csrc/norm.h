@@ -228,8 +228,10 @@ hipError_t launch_norm_of(const NormArgs& a, hipStream_t s) {
         hipLaunchKernelGGL(kernel, dim3(a.T < groups ? a.T : groups), dim3(threads), 0, s, a);
         return hipGetLastError();
     };
-    // Few rows: as many threads as the row can use.  Many: two chunks a thread (8192 rows of 8192 in
-    // bfloat16 with both norms and a gate: 126 us; one chunk 161, four 156).
+    // Few rows: as many threads as the row can use.  Many: two chunks a thread.  Kernels of both norms in
+    // bfloat16, us, by one chunk and by two: 8 rows of 4096 4.8 and 5.7, 256 of 4097 6.7 and 7.4, 512 of
+    // 4096 7.1 and 7.5; the same at 64 rows of 8192 (6.1 and 6.0), but 512 11.6 and 9.9, 8192 161 and 126
+    // (by four chunks 156).
     if (chunks <= 256) return go(block_norm<A, 256, 1, kX, kS, kWhole>, 256, 1);
     if (chunks <= 1024 && a.T <= 512) return go(block_norm<A, 1024, 1, kX, kS, kWhole>, 1024, 1);
     if (chunks <= 512) return go(block_norm<A, 256, 2, kX, kS, kWhole>, 256, 2);
