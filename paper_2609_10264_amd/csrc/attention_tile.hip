@@ -63,7 +63,7 @@
 // computes, so the codes go straight to LDS and each wave widens its own part of a tile
 // in place at the end of a step.  Measured: the 48 sequences above 161 us in E4M3 (227
 // in bfloat16; 118 are its bytes), a chunk of 512 over 16000 entries with 64 + 8 heads
-// 364 us (304 in bfloat16): the widening, two conversions and an LDS pass a value, is
+// 357 us (304 in bfloat16): the widening, two conversions and an LDS pass a value, is
 // paid once a workgroup and tile and adds to steps that the products already fill.  I8
 // takes 10 to 18 % longer than E4M3, which one instruction converts by pairs.
 #include "kv.h"
